@@ -264,7 +264,7 @@ def _own_tokens(s):
     if c["top"]:
         got.update(top_logp=f.top_logp, top_id=f.top_id)
     if c["train"]:
-        got["dlogits"] = qsr.token_logprobs_backward(s["logits"], s["tokens"], f.lse, f.entropy, s["dlogp"], s["dent"])
+        got["dlogits"] = qsr.token_logprobs_backward(s["logits"], s["tokens"], f.stats, f.entropy, s["dlogp"], s["dent"])
     return got
 
 
