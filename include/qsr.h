@@ -278,6 +278,127 @@ int qsr_clip_factors(const float *grads, int32_t K, int64_t P, float max_norm, v
 int qsr_clip_factors_static(const float *grads, int32_t K, int64_t P, float max_norm, float *coef,
                             float *norm, void *stream);
 
+/* ---------------------------------------------------------------------------------------------
+ * Operators around the matrix products of a model of the caller's own: what its local step needs besides them.
+ * Rows and tensors of K workers are handled in one call.  Types of elements are QSR_TYPE_*; strides count elements.  Argument
+ * checks happen on the host; everything else is asynchronous on `stream`, and all pointers are DEVICE pointers unless marked.
+ * --------------------------------------------------------------------------------------------- */
+enum {
+    QSR_TYPE_F32 = 0,
+    QSR_TYPE_BF16 = 1,
+    QSR_TYPE_E4M3 = 2   /* 8 bits: 4 of exponent, 3 of mantissa, largest value 448, no infinities           */
+};
+
+/* AdamW over many tensors in one launch.  A tensor of n elements is held for each of the K workers, worker k's at
+ * param + k * param_stride and so on (strides >= n, read only where K > 1).
+ *   param  float.  grad  float or bf16 (grad_type).  copy: bf16 copy of the new parameters, rounded to nearest, or NULL.
+ *   m, v   state_type QSR_TYPE_F32: float moments, as in a context.
+ *          state_type QSR_TYPE_E4M3: codes of m and of the ROOT of v, in blocks of 256 consecutive elements of a worker's tensor,
+ *          each block with a float scale (value = code * scale).  A worker's row holds whole blocks, ceil(n / 256) * 256 bytes
+ *          (state_stride a multiple of 4, rows 4-byte aligned), and as many scales as blocks.  Rounding is stochastic, from `seed`,
+ *          the number of the step and the element's place in the list, the same on every run.  What is not finite is stored as NaN.
+ * The caller zeroes the moments (and scales) for a new run or restores them. */
+typedef struct {
+    float *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale; /* QSR_TYPE_E4M3; else NULL */
+    void *copy;
+    int64_t n;
+    int64_t param_stride, grad_stride, state_stride, scale_stride, copy_stride;
+    double weight_decay;      /* decoupled, this tensor's */
+} qsr_tensor;
+
+typedef struct {
+    int32_t K, n_tensors, grad_type, state_type;
+    double beta1, beta2, eps;
+    double clip_norm;         /* > 0: gradient clipping by global norm over all tensors of a worker, as in qsr_config; 0 = off */
+    uint64_t seed;
+    const qsr_tensor *tensors; /* (host) read during qsr_adamw_init only */
+} qsr_adamw_config;
+
+typedef struct qsr_adamw qsr_adamw; /* opaque, library-owned */
+
+/* Checks a configuration on the host; *why, if given, names the offending field. */
+int qsr_adamw_validate(const qsr_adamw_config *cfg, const char **why);
+/* Keeps the list (addresses, not contents) and tables for it in device memory.  Synchronises.  On failure *out is NULL. */
+int qsr_adamw_init(const qsr_adamw_config *cfg, qsr_adamw **out);
+/* One step of all workers with learning rate eta; t: steps taken before (0, 1, ...), which sets the bias corrections.  The scalars
+ * are passed by value: a recorded step repeats the same t and eta. */
+int qsr_adamw_step(qsr_adamw *a, int64_t t, double eta, void *stream);
+/* New addresses of the n = n_tensors gradients, (host) array, from the next step on in the stream's order; types and strides stay. */
+int qsr_adamw_set_grads(qsr_adamw *a, const void *const *grads, int32_t n, void *stream);
+/* The K factors and norms of the last step's clipping: DEVICE arrays of the library's.  QSR_ESTATE without clip_norm. */
+int qsr_adamw_clip(qsr_adamw *a, const float **coef, const float **norm);
+/* Waits for the device. */
+int qsr_adamw_destroy(qsr_adamw *a);
+
+/* Root-mean-square norm of rows of d elements with the residual's addition; worker k owns rows k * rows .. (k + 1) * rows - 1:
+ *   s = x + residual (or x);  rstd = 1 / sqrt(mean(s^2) + eps);  y = s * rstd * weight_k
+ * sum: s in the rows' type (may be x or residual itself), or NULL; rstd: [K * rows] floats, or NULL; y_type: the rows' type, or
+ * QSR_TYPE_E4M3 with scale [K * rows], scale = max|y| / 448 of the row's finite entries, y = code * scale (a row of zeros has scale 0).
+ * QSR_ELIMIT above d = 16384. */
+typedef struct {
+    int32_t K, type, y_type;
+    int64_t rows, d;          /* rows of a worker, >= 0 */
+    const void *x, *residual; /* residual may be NULL */
+    const float *weight;      /* [K][d] */
+    void *sum, *y;
+    float *scale, *rstd;
+    int64_t x_stride, residual_stride, sum_stride, y_stride; /* from row to row, >= d */
+    double eps;
+} qsr_rmsnorm_args;
+int qsr_rmsnorm(const qsr_rmsnorm_args *args, void *stream);
+
+/* Its gradients, from s as it was kept: x_grad (of x and of residual alike) and weight_grad [K][d] (overwritten; sums in a fixed
+ * order).  residual_grad: what comes down the residual stream, added to x_grad, or NULL. */
+typedef struct {
+    int32_t K, type;
+    int64_t rows, d;
+    const void *y_grad, *sum;
+    const float *weight, *rstd;
+    const void *residual_grad;
+    void *x_grad;
+    float *weight_grad;
+    int64_t y_grad_stride, sum_stride, residual_grad_stride, x_grad_stride;
+} qsr_rmsnorm_backward_args;
+int qsr_rmsnorm_workspace_bytes(int32_t K, int64_t rows, int64_t d, int32_t type, size_t *bytes);
+int qsr_rmsnorm_backward(const qsr_rmsnorm_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Log probabilities of given tokens from rows of logits, z = logits / temperature:
+ *   lse = log sum exp z;  logp = z[token] - lse;  entropy = -sum p log p;  the `top` best alternatives (the lower index first where
+ *   logits are equal) with their log probabilities.
+ * Any output but top_logp and top_id (with top > 0) may be NULL.  stats: [rows][2] floats for the backward pass, the largest logit m
+ * and log sum exp((logits - m) / temperature).
+ * A token outside 0..vocab-1 stands for none: logp = 0.  Logits of -inf have probability 0; a row of nothing else has
+ * lse = logp = -inf and entropy 0.  A row with a NaN or +inf has NaN for all of these, and its alternatives leave NaN aside.
+ * QSR_ELIMIT for top above 64. */
+typedef struct {
+    int64_t rows, vocab, stride;
+    int32_t type, top;
+    const void *logits;
+    const int64_t *tokens;    /* [rows] */
+    double temperature;       /* > 0 */
+    float *logp, *entropy, *lse, *stats;
+    float *top_logp;          /* [rows][top] */
+    int32_t *top_id;          /* [rows][top] */
+} qsr_token_logprobs_args;
+int qsr_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t type, int32_t top, size_t *bytes);
+int qsr_token_logprobs(const qsr_token_logprobs_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* The gradient with respect to the logits, in their type (grad may be logits itself), for the gradients logp_grad and entropy_grad
+ * [rows], either of which may be NULL (zero).  Rows without a token take none from logp_grad, rows masked as a whole none at all. */
+typedef struct {
+    int64_t rows, vocab, stride, grad_stride;
+    int32_t type, reserved;
+    const void *logits;
+    const int64_t *tokens;
+    double temperature;
+    const float *stats, *entropy, *logp_grad, *entropy_grad;
+    void *grad;
+} qsr_token_logprobs_backward_args;
+int qsr_token_logprobs_backward(const qsr_token_logprobs_backward_args *args, void *stream);
+
 const char *qsr_strerror(int code);
 int qsr_last_hip_error(void); /* hipError_t of the last failed runtime call in this thread */
 

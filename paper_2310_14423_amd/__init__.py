@@ -7,6 +7,9 @@ symbols can be inspected), any compute call without the built library or a gfx95
 from .binding import (QSRError, Config, Context, average_rows, clip_factors, clip_factors_static,
                       host_schedule, lib, lib_path, validate,
                       workspace_bytes, EXPORTS)
+from .operators import (AdamW, RMSNorm, TokenLogprobs, rmsnorm, rmsnorm_backward, token_logprobs,
+                        token_logprobs_backward)
 
 __all__ = ["QSRError", "Config", "Context", "average_rows", "clip_factors", "clip_factors_static", "host_schedule", "lib", "lib_path", "validate",
-           "workspace_bytes", "EXPORTS"]
+           "workspace_bytes", "EXPORTS", "AdamW", "RMSNorm", "TokenLogprobs", "rmsnorm", "rmsnorm_backward", "token_logprobs",
+           "token_logprobs_backward"]

@@ -12,7 +12,10 @@ _lib = None
 EXPORTS = ["qsr_validate", "qsr_workspace_bytes", "qsr_host_schedule", "qsr_init", "qsr_local_step", "qsr_maybe_sync",
            "qsr_run", "qsr_get_H", "qsr_get_state", "qsr_set_state", "qsr_read_sync_log", "qsr_read_host_schedule", "qsr_eta_table", "qsr_read_loss", "qsr_restart",
            "qsr_timing", "qsr_read_timing", "qsr_read_timing_stats", "qsr_destroy", "qsr_average_rows", "qsr_clip_workspace_bytes", "qsr_clip_factors", "qsr_clip_factors_static", "qsr_strerror",
-           "qsr_last_hip_error"]
+           "qsr_last_hip_error",
+           "qsr_adamw_validate", "qsr_adamw_init", "qsr_adamw_step", "qsr_adamw_set_grads", "qsr_adamw_clip", "qsr_adamw_destroy",
+           "qsr_rmsnorm", "qsr_rmsnorm_workspace_bytes", "qsr_rmsnorm_backward",
+           "qsr_token_logprobs_workspace_bytes", "qsr_token_logprobs", "qsr_token_logprobs_backward"]
 
 OPTS = {"sgdm": 0, "adamw": 1}
 LRS = {"cosine": 0, "step": 1, "table": 2, "linear": 3, "pow2cos": 4}

@@ -1,0 +1,424 @@
+// adamw_tensors.hip -- AdamW over a list of tensors in one launch, for K workers, with the moments in 32 or in 8 bits.
+//
+// For a model of a caller's own, whose parameters are many tensors.  Tensor i holds n_i elements for each worker (rows of any stride).
+// One step, n = t + 1:
+//   g <- coef_k g                               (clip_norm: coef_k = min(1, c / (||g_k|| + 1e-6)), the norm over all tensors of worker k)
+//   m <- m + (1 - beta1)(g - m);  v <- v + (1 - beta2)(g^2 - v);  r = sqrt(v)
+//   theta <- theta - [eta lambda_i theta + eta/(1 - beta1^n) m / (r / sqrt(1 - beta2^n) + eps)]
+// with the arithmetic of the [K][P] update (opt_elem.h) where the moments are fp32: the same bits.  Where they are held in 8 bits
+// every operation that leads to a code is rounded by itself, in the order of the formulas and with no fused ones: a last bit decides
+// now and then which of two codes a moment becomes, and so the codes are those of any fp32 implementation of this comment.
+// Parameters are fp32: steps are smaller than half a unit of a bf16 parameter.  A copy of the new parameters in bf16, rounded to nearest, is written on request.
+//
+// Moments in 8 bits: each 256 consecutive elements of a worker's tensor are a block with one fp32 scale, a lane of a wavefront holds
+// four of them.  m and r (the root: half of v's range of exponents) are e4m3 codes of value * (1 / top * 448), top = max|value| over
+// the block's finite values, with the scale top * (1 / 448); a value that is not finite becomes NaN and spoils no other.  Blocks whose
+// top is below 1e-35 are stored as zeros: the factor would leave the range of floats.
+// Rounding is stochastic (v_cvt_sr_fp8_f32): up with the probability of the part of a step that is left.  An iteration moves r by a
+// relative (1 - beta2)/2 = 5e-4, less than a hundredth of a code's step (1/16 to 1/8 of the value): to nearest it would never move.
+// A root above zero does not become zero (the smallest code instead): m / r of the next step stays bounded.
+// The random words: a 32-bit multiply-xorshift mix (constants from C. Wellons' search for mixes of low bias) of the element's index,
+// counted over the padded blocks of all tensors, and the step's key; 16 bits for each of the two moments.
+#include <cmath>
+#include <cstring>
+#include <new>
+#include <vector>
+
+#include "opt_elem.h"
+#include "qsr_internal.h"
+#include "row_io.h"
+
+namespace qsr {
+
+constexpr int AT_BLOCK = 256;                  // elements that share a scale
+constexpr int AT_SPAN = 4;                     // blocks of a wavefront's trip
+
+struct AtTensor {
+    float *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    bf16_t *copy;
+    long long n, s_param, s_grad, s_state, s_scale, s_copy;   // elements, and strides from worker to worker
+    double decay;
+    long long first;                           // blocks of the tensors before this one
+};
+struct AtChunk { int tensor, block; };         // a trip's first block
+struct AtStep { double eta; float step, rsq, c1, c2, eps; uint32_t key; };
+
+// 16 random bits for either moment: index counts the worker's elements over all tensors, padded to blocks
+__device__ __forceinline__ uint32_t at_word(uint32_t index, uint32_t worker, uint32_t key)
+{
+    uint32_t x = (index + worker * 0x9E3779B9u) ^ key;
+    x ^= x >> 16; x *= 0x21F0AAADu;
+    x ^= x >> 15; x *= 0x735A2D97u;
+    return x ^ (x >> 15);
+}
+
+// The codes' factor and scale of a block whose largest finite magnitude is `top`
+__device__ __forceinline__ void at_scale(float top, float &factor, float &scale)
+{
+    const bool some = top >= 1e-35f;
+    factor = some ? 1.f / top * E4M3_MAX : 0.f;
+    scale = some ? top * (1.f / E4M3_MAX) : 0.f;
+}
+__device__ __forceinline__ float finite_or_zero(float x) { return fabsf(x) < INFINITY ? x : 0.f; }
+// The factor's rounding may take the largest value past 448, which could round to NaN; what is not finite shall become NaN.
+__device__ __forceinline__ float at_most_448(float y) { return fabsf(y) < 449.f ? fminf(fmaxf(y, -E4M3_MAX), E4M3_MAX) : y; }
+// One element with 8-bit moments: new m, v's root r and theta
+__device__ __forceinline__ void adamw_rounded(float &th, float g, float &m, float r0, float &r, float etalam, const float stepsz, float rsq,
+                                              float c1, float c2, float eps)
+{
+#pragma clang fp contract(off)
+    const float v0 = r0 * r0;
+    m = m + c1 * (g - m);
+    r = sqrtf(v0 + c2 * (g * g - v0));
+    const float upd = stepsz * m / (r * rsq + eps);
+    th = th - (etalam * th + upd);
+}
+
+template <typename G, bool FP8>
+__global__ __launch_bounds__(64) void adamw_tensors_kernel(const AtTensor *__restrict__ list, const AtChunk *__restrict__ chunks,
+                                                           AtStep st, const float *__restrict__ coef)
+{
+    const AtChunk ch = chunks[blockIdx.x];
+    const AtTensor t = list[ch.tensor];
+    const int k = blockIdx.y, lane = threadIdx.x;
+    const float gs = coef != nullptr ? coef[k] : 1.f;
+    const float etalam = (float)(st.eta * t.decay);
+    float *const th = t.param + k * t.s_param;
+    const G *const g = (const G *)t.grad + k * t.s_grad;
+    const long long e0 = (long long)ch.block * AT_BLOCK + lane * 4;
+    float a[AT_SPAN][4], b[AT_SPAN][4], c[AT_SPAN][4], d[AT_SPAN][4];
+#pragma unroll
+    for (int u = 0; u < AT_SPAN; ++u) {
+        const long long e = e0 + u * AT_BLOCK;
+        const long long left = t.n - e;
+        if (left >= 4) {
+            load_wide<float, 4, true>(th + e, a[u]);
+            load_wide<G, 4, true>(g + e, b[u]);
+        } else {
+            load_some(th + e, (int)left, a[u]);
+            load_some(g + e, (int)left, b[u]);
+        }
+        if (FP8) {
+            // rows of codes are whole blocks: no part of one is missing
+            if (t.n > e - lane * 4) {
+                const long long blk = (e - lane * 4) / AT_BLOCK;
+                const uint32_t mc = __builtin_nontemporal_load((const uint32_t *)((const uint8_t *)t.m + k * t.s_state + e));
+                const uint32_t vc = __builtin_nontemporal_load((const uint32_t *)((const uint8_t *)t.v + k * t.s_state + e));
+                const float ms = t.m_scale[k * t.s_scale + blk], vs = t.v_scale[k * t.s_scale + blk];
+                c[u][0] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 0); c[u][1] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 1);
+                c[u][2] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 2); c[u][3] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 3);
+                d[u][0] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 0); d[u][1] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 1);
+                d[u][2] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 2); d[u][3] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 3);
+            }
+        } else if (left >= 4) {
+            load_wide<float, 4, true>((const float *)t.m + k * t.s_state + e, c[u]);
+            load_wide<float, 4, true>((const float *)t.v + k * t.s_state + e, d[u]);
+        } else {
+            load_some((const float *)t.m + k * t.s_state + e, (int)left, c[u]);
+            load_some((const float *)t.v + k * t.s_state + e, (int)left, d[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < AT_SPAN; ++u) {
+        const long long e = e0 + u * AT_BLOCK;
+        const long long left = t.n - e;
+        if (t.n <= e - lane * 4) break;                    // the whole wavefront
+        float r[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (FP8) adamw_rounded(a[u][i], b[u][i] * gs, c[u][i], d[u][i], r[i], etalam, st.step, st.rsq, st.c1, st.c2, st.eps);
+            else adamw_elem(a[u][i], b[u][i] * gs, c[u][i], d[u][i], etalam, st.step, st.rsq, st.c1, st.c2, st.eps);
+            if (FP8 && i >= left) c[u][i] = r[i] = 0.f;
+        }
+        if (left >= 4) store_wide<float, 4, true>(th + e, a[u]);
+        else store_some(th + e, (int)left, a[u]);
+        if (t.copy != nullptr) {
+            bf16_t *const y = t.copy + k * t.s_copy;
+            if (left >= 4) store_wide<bf16_t, 4, true>(y + e, a[u]);
+            else store_some(y + e, (int)left, a[u]);
+        }
+        if (!FP8) {
+            float *const m = (float *)t.m + k * t.s_state, *const v = (float *)t.v + k * t.s_state;
+            if (left >= 4) { store_wide<float, 4, true>(m + e, c[u]); store_wide<float, 4, true>(v + e, d[u]); }
+            else { store_some(m + e, (int)left, c[u]); store_some(v + e, (int)left, d[u]); }
+            continue;
+        }
+        float mtop = 0.f, rtop = 0.f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            mtop = fmaxf(mtop, fabsf(finite_or_zero(c[u][i])));
+            rtop = fmaxf(rtop, finite_or_zero(r[i]));
+        }
+        mtop = wave_max(mtop); rtop = wave_max(rtop);
+        float mf, ms, rf, rs;
+        at_scale(mtop, mf, ms); at_scale(rtop, rf, rs);
+        const uint32_t index = (uint32_t)(t.first * AT_BLOCK + e);
+        int mc = 0, vc = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t w = at_word(index + i, (uint32_t)k, st.key);
+            const float x = at_most_448(c[u][i] * mf), q = at_most_448(r[i] * rf), y = q > 0.f ? fmaxf(q, E4M3_TINY) : q;
+            const uint32_t wm = w & 0xFFFF0000u, wv = w << 16;
+            if (i == 0) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 0); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 0); }
+            if (i == 1) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 1); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 1); }
+            if (i == 2) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 2); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 2); }
+            if (i == 3) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 3); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 3); }
+        }
+        __builtin_nontemporal_store((uint32_t)mc, (uint32_t *)((uint8_t *)t.m + k * t.s_state + e));
+        __builtin_nontemporal_store((uint32_t)vc, (uint32_t *)((uint8_t *)t.v + k * t.s_state + e));
+        if (lane == 0) {
+            const long long blk = e / AT_BLOCK;
+            t.m_scale[k * t.s_scale + blk] = ms;
+            t.v_scale[k * t.s_scale + blk] = rs;
+        }
+    }
+}
+
+// Sum of squares of a span of blocks of a tensor, for each worker: partial[k][span].  Lanes add at most a few hundred squares in fp32,
+// with the rounding errors (opt_elem.h), the rest is double, all in a fixed order.
+constexpr int AT_NORM_THREADS = 256;
+struct AtSpan { int tensor, block, blocks; };
+template <typename G>
+__global__ __launch_bounds__(AT_NORM_THREADS) void tensors_sqnorm_kernel(const AtTensor *__restrict__ list, const AtSpan *__restrict__ spans,
+                                                                         double *__restrict__ partial)
+{
+    __shared__ double red[AT_NORM_THREADS / 64];
+    const AtSpan sp = spans[blockIdx.x];
+    const AtTensor t = list[sp.tensor];
+    const int k = blockIdx.y;
+    const G *const g = (const G *)t.grad + k * t.s_grad;
+    const long long e0 = (long long)sp.block * AT_BLOCK, e1 = min(t.n, e0 + (long long)sp.blocks * AT_BLOCK);
+    float s[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f};
+    for (long long e = e0 + threadIdx.x * 4; e < e1; e += AT_NORM_THREADS * 4) {
+        float x[4];
+        if (e1 - e >= 4) load_wide<G, 4, false>(g + e, x);
+        else load_some(g + e, (int)(e1 - e), x);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) add_comp(s[i], c[i], x[i] * x[i]);
+    }
+    double acc = 0.0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc += (double)s[i] + (double)c[i];
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = acc;
+    __syncthreads();
+    if (threadIdx.x == 0) partial[(long long)k * gridDim.x + blockIdx.x] = (red[0] + red[1]) + (red[2] + red[3]);
+}
+
+// The gradients' addresses, which change where a backward pass allocates them anew: carried in the kernel's arguments, so that the
+// exchange is a launch like any other, in the stream's order.
+constexpr int AT_PTRS = 256;
+struct AtPtrs { const void *p[AT_PTRS]; };
+__global__ __launch_bounds__(AT_PTRS) void tensors_set_grads_kernel(AtTensor *list, AtPtrs ptrs, int first, int n)
+{
+    if ((int)threadIdx.x < n) list[first + threadIdx.x].grad = ptrs.p[threadIdx.x];
+}
+
+}  // namespace qsr
+
+using namespace qsr;
+
+struct qsr_adamw {
+    int device, K, n, grad_bf16, fp8;
+    double beta1, beta2;
+    float eps, clip;
+    uint64_t seed;
+    long long chunks, spans;
+    AtTensor *d_list;
+    AtChunk *d_chunks;
+    AtSpan *d_spans;
+    double *d_partial;
+    float *d_coef;                             // [K] factors, then [K] norms
+};
+
+#define HIP_TRY(expr)                                    \
+    do {                                                 \
+        hipError_t e_ = (expr);                          \
+        if (e_ != hipSuccess) {                          \
+            set_last_hip_error((int)e_);                 \
+            return QSR_EHIP;                             \
+        }                                                \
+    } while (0)
+
+static bool unaligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+
+extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
+{
+    const char *w = nullptr;
+    auto finite_ge0 = [](double x) { return std::isfinite(x) && x >= 0.0; };
+    if (!c) w = "cfg is NULL";
+    else if (c->K < 1 || c->K > 65535) w = "K";
+    else if (c->n_tensors < 1 || c->n_tensors > (1 << 20) || !c->tensors) w = "tensors";
+    else if (c->grad_type != QSR_TYPE_F32 && c->grad_type != QSR_TYPE_BF16) w = "grad_type";
+    else if (c->state_type != QSR_TYPE_F32 && c->state_type != QSR_TYPE_E4M3) w = "state_type";
+    else if (!(finite_ge0(c->beta1) && c->beta1 < 1.0 && finite_ge0(c->beta2) && c->beta2 < 1.0)) w = "beta1/beta2";
+    else if (!(std::isfinite(c->eps) && c->eps > 0.0)) w = "eps";
+    else if (!finite_ge0(c->clip_norm) || c->clip_norm > 1e38 || (c->clip_norm > 0.0 && c->clip_norm < 1e-37)) w = "clip_norm";
+    const bool fp8 = !w && c->state_type == QSR_TYPE_E4M3;
+    const uintptr_t ga = !w && c->grad_type == QSR_TYPE_BF16 ? 2 : 4;
+    long long blocks = 0;
+    for (int i = 0; !w && i < c->n_tensors; ++i) {
+        const qsr_tensor &t = c->tensors[i];
+        if (t.n < 1 || t.n > ((long long)1 << 35)) { w = "a tensor's n"; break; }
+        const long long nb = (t.n + AT_BLOCK - 1) / AT_BLOCK;
+        blocks += nb;
+        const bool many = c->K > 1;
+        if (!t.param || unaligned(t.param, 4) || !t.grad || unaligned(t.grad, ga)) w = "a tensor's param/grad";
+        else if (!t.m || !t.v || unaligned(t.m, 4) || unaligned(t.v, 4)) w = "a tensor's m/v";
+        else if (fp8 && (!t.m_scale || !t.v_scale || unaligned(t.m_scale, 4) || unaligned(t.v_scale, 4))) w = "a tensor's m_scale/v_scale";
+        else if (t.copy && unaligned(t.copy, 2)) w = "a tensor's copy";
+        else if (many && (t.param_stride < t.n || t.grad_stride < t.n || (t.copy && t.copy_stride < t.n))) w = "a tensor's param_stride/grad_stride/copy_stride";
+        else if (many && !fp8 && t.state_stride < t.n) w = "a tensor's state_stride";
+        else if (many && fp8 && (t.state_stride < nb * AT_BLOCK || t.state_stride % 4 != 0 || t.scale_stride < nb)) w = "a tensor's state_stride/scale_stride";
+        else if (!finite_ge0(t.weight_decay)) w = "a tensor's weight_decay";
+    }
+    if (!w && blocks > ((long long)1 << 27)) w = "tensors (above 2^35 elements together)";     // the grid's limit of 2^32 threads
+    if (why) *why = w ? w : "ok";
+    return w ? QSR_EINVAL : QSR_OK;
+}
+
+static void free_adamw(qsr_adamw *a)
+{
+    if (!a) return;
+    if (a->d_list) (void)hipFree(a->d_list);
+    if (a->d_chunks) (void)hipFree(a->d_chunks);
+    if (a->d_spans) (void)hipFree(a->d_spans);
+    if (a->d_partial) (void)hipFree(a->d_partial);
+    if (a->d_coef) (void)hipFree(a->d_coef);
+    delete a;
+}
+
+static int init_adamw(qsr_adamw *a, const qsr_adamw_config *c)
+{
+    HIP_TRY(hipGetDevice(&a->device));
+    hipDeviceProp_t prop;
+    HIP_TRY(hipGetDeviceProperties(&prop, a->device));
+    if (std::strncmp(prop.gcnArchName, "gfx950", 6) != 0) return QSR_ENOGPU;
+    std::vector<AtTensor> list((size_t)c->n_tensors);
+    std::vector<AtChunk> chunks;
+    std::vector<AtSpan> spans;
+    long long blocks = 0;
+    for (int i = 0; i < c->n_tensors; ++i) {
+        const qsr_tensor &t = c->tensors[i];
+        list[i] = AtTensor{t.param, t.grad, t.m, t.v, t.m_scale, t.v_scale, (bf16_t *)t.copy, t.n, t.param_stride, t.grad_stride,
+                           t.state_stride, t.scale_stride, t.copy_stride, t.weight_decay, blocks};
+        const long long nb = (t.n + AT_BLOCK - 1) / AT_BLOCK;
+        for (long long b = 0; b < nb; b += AT_SPAN) chunks.push_back(AtChunk{i, (int)b});
+        blocks += nb;
+    }
+    a->chunks = (long long)chunks.size();
+    HIP_TRY(hipMalloc((void **)&a->d_list, list.size() * sizeof(AtTensor)));
+    HIP_TRY(hipMalloc((void **)&a->d_chunks, chunks.size() * sizeof(AtChunk)));
+    HIP_TRY(hipMemcpy(a->d_list, list.data(), list.size() * sizeof(AtTensor), hipMemcpyHostToDevice));
+    HIP_TRY(hipMemcpy(a->d_chunks, chunks.data(), chunks.size() * sizeof(AtChunk), hipMemcpyHostToDevice));
+    if (a->clip > 0.f) {
+        // spans of 64 blocks, longer where that would leave more than 4096 partial sums to a worker
+        const long long per = blocks / 4096 > 64 ? (blocks + 4095) / 4096 : 64;
+        for (int i = 0; i < c->n_tensors; ++i) {
+            const long long nb = (c->tensors[i].n + AT_BLOCK - 1) / AT_BLOCK;
+            for (long long b = 0; b < nb; b += per) spans.push_back(AtSpan{i, (int)b, (int)(nb - b < per ? nb - b : per)});
+        }
+        a->spans = (long long)spans.size();
+        HIP_TRY(hipMalloc((void **)&a->d_spans, spans.size() * sizeof(AtSpan)));
+        HIP_TRY(hipMemcpy(a->d_spans, spans.data(), spans.size() * sizeof(AtSpan), hipMemcpyHostToDevice));
+        HIP_TRY(hipMalloc((void **)&a->d_partial, (size_t)a->K * spans.size() * sizeof(double)));
+        HIP_TRY(hipMalloc((void **)&a->d_coef, 2 * (size_t)a->K * sizeof(float)));
+    }
+    return QSR_OK;
+}
+
+extern "C" int qsr_adamw_init(const qsr_adamw_config *cfg, qsr_adamw **out)
+{
+    if (!out) return QSR_EINVAL;
+    *out = nullptr;
+    int rc = qsr_adamw_validate(cfg, nullptr);
+    if (rc != QSR_OK) return rc;
+    qsr_adamw *a = new (std::nothrow) qsr_adamw();
+    if (!a) return QSR_ENOMEM;
+    a->K = cfg->K; a->n = cfg->n_tensors;
+    a->grad_bf16 = cfg->grad_type == QSR_TYPE_BF16; a->fp8 = cfg->state_type == QSR_TYPE_E4M3;
+    a->beta1 = cfg->beta1; a->beta2 = cfg->beta2; a->eps = (float)cfg->eps; a->clip = (float)cfg->clip_norm;
+    a->seed = cfg->seed;
+    try {
+        rc = init_adamw(a, cfg);
+    } catch (...) {                            // the host's tables did not fit its memory
+        rc = QSR_ENOMEM;
+    }
+    if (rc != QSR_OK) { free_adamw(a); return rc; }
+    *out = a;
+    return QSR_OK;
+}
+
+// The step's key: high half of a 64-bit mix (splitmix64: Steele, Lea, Flood, OOPSLA 2014) of the seed and the number of the step
+static uint32_t step_key(uint64_t seed, long long t)
+{
+    uint64_t z = seed + (uint64_t)(t + 1) * 0x9E3779B97F4A7C15ull;
+    z = (z ^ (z >> 30)) * 0xBF58476D1CE4E5B9ull;
+    z = (z ^ (z >> 27)) * 0x94D049BB133111EBull;
+    return (uint32_t)((z ^ (z >> 31)) >> 32);
+}
+
+extern "C" int qsr_adamw_step(qsr_adamw *a, int64_t t, double eta, void *stream)
+{
+    if (!a || t < 0 || !std::isfinite(eta) || eta < 0.0) return QSR_EINVAL;
+    hipStream_t s = (hipStream_t)stream;
+    const float *coef = nullptr;
+    const unsigned K = (unsigned)a->K;
+    if (a->clip > 0.f) {
+        if (a->grad_bf16) tensors_sqnorm_kernel<bf16_t><<<dim3((unsigned)a->spans, K), AT_NORM_THREADS, 0, s>>>(a->d_list, a->d_spans, a->d_partial);
+        else tensors_sqnorm_kernel<float><<<dim3((unsigned)a->spans, K), AT_NORM_THREADS, 0, s>>>(a->d_list, a->d_spans, a->d_partial);
+        HIP_TRY(hipGetLastError());
+        HIP_TRY(launch_clip_finish(a->d_partial, a->K, (int)a->spans, a->clip, a->d_coef, a->d_coef + a->K, s));
+        coef = a->d_coef;
+    }
+    const double n = (double)(t + 1);
+    AtStep st;
+    st.eta = eta;
+    st.step = (float)(eta / (1.0 - std::pow(a->beta1, n)));
+    st.rsq = (float)(1.0 / std::sqrt(1.0 - std::pow(a->beta2, n)));
+    st.c1 = (float)(1.0 - a->beta1); st.c2 = (float)(1.0 - a->beta2); st.eps = a->eps;
+    st.key = step_key(a->seed, t);
+    const dim3 grid((unsigned)a->chunks, K);
+    if (a->fp8 && a->grad_bf16) adamw_tensors_kernel<bf16_t, true><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
+    else if (a->fp8) adamw_tensors_kernel<float, true><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
+    else if (a->grad_bf16) adamw_tensors_kernel<bf16_t, false><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
+    else adamw_tensors_kernel<float, false><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
+    HIP_TRY(hipGetLastError());
+    return QSR_OK;
+}
+
+extern "C" int qsr_adamw_set_grads(qsr_adamw *a, const void *const *grads, int32_t n, void *stream)
+{
+    if (!a || !grads || n != a->n) return QSR_EINVAL;
+    for (int i = 0; i < n; ++i)
+        if (!grads[i] || unaligned(grads[i], a->grad_bf16 ? 2 : 4)) return QSR_EINVAL;
+    for (int first = 0; first < n; first += AT_PTRS) {
+        AtPtrs p;
+        const int m = n - first < AT_PTRS ? n - first : AT_PTRS;
+        for (int i = 0; i < AT_PTRS; ++i) p.p[i] = i < m ? grads[first + i] : nullptr;
+        tensors_set_grads_kernel<<<1, AT_PTRS, 0, (hipStream_t)stream>>>(a->d_list, p, first, m);
+        HIP_TRY(hipGetLastError());
+    }
+    return QSR_OK;
+}
+
+extern "C" int qsr_adamw_clip(qsr_adamw *a, const float **coef, const float **norm)
+{
+    if (!a) return QSR_EINVAL;
+    if (!a->d_coef) return QSR_ESTATE;
+    if (coef) *coef = a->d_coef;
+    if (norm) *norm = a->d_coef + a->K;
+    return QSR_OK;
+}
+
+extern "C" int qsr_adamw_destroy(qsr_adamw *a)
+{
+    if (!a) return QSR_EINVAL;
+    (void)hipDeviceSynchronize();
+    free_adamw(a);
+    return QSR_OK;
+}

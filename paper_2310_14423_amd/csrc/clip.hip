@@ -66,7 +66,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void sqnorm_partial_kernel(
 }
 
 // coef[k] = min(1, max_norm / (sqrt(sum_b partial[k][b]) + 1e-6)); norm[k] = that square root.  One workgroup per
-// row (nb <= 1024: at most four partial sums per lane, then a fixed tree; one lane adding them all took 12-15 us);
+// row (nb <= 1024 for a flat row: at most four partial sums per lane, then a fixed tree; one lane adding them all took 12-15 us);
 // same_rows: row 0's sum serves all rows.
 __global__ __launch_bounds__(CLIP_THREADS) void clip_coef_kernel(const double *__restrict__ partial, int nb, float max_norm,
                                                                  int same_rows, float *__restrict__ coef, float *__restrict__ norm)
@@ -106,6 +106,12 @@ hipError_t launch_clip_coef(const float *g, int K, long long P, float max_norm, 
     sqnorm_partial_kernel<<<dim3((unsigned)nb, same_rows ? 1u : (unsigned)K), CLIP_THREADS, 0, s>>>(g, P, chunk, partial);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
+    return launch_clip_finish(partial, K, nb, max_norm, coef, norm, s, same_rows);
+}
+
+hipError_t launch_clip_finish(const double *partial, int K, int nb, float max_norm, float *coef, float *norm, hipStream_t s,
+                              bool same_rows)
+{
     clip_coef_kernel<<<K, CLIP_THREADS, 0, s>>>(partial, nb, max_norm, same_rows ? 1 : 0, coef, norm);
     return hipGetLastError();
 }

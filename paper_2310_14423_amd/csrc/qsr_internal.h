@@ -141,6 +141,9 @@ hipError_t launch_update_adamw_sync(float *theta, const float *g, float *m, floa
 int clip_blocks_per_row(long long P);
 hipError_t launch_clip_coef(const float *g, int K, long long P, float max_norm, double *partial, float *coef,
                             float *norm, hipStream_t s, bool same_rows = false);
+// the second half of it: factors and norms from nb partial sums of squares of each worker
+hipError_t launch_clip_finish(const double *partial, int K, int nb, float max_norm, float *coef, float *norm, hipStream_t s,
+                              bool same_rows = false);
 // device address, on the current device, of the partial-sum array inside the library's image
 // (qsr_clip_factors_static); looked up at the first call on a device.  Returns a QSR_* code.
 int clip_static_setup(double **out);

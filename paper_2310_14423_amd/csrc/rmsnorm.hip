@@ -1,0 +1,406 @@
+// rmsnorm.hip -- root-mean-square norm of rows with the residual's addition, for K workers with a weight each, and its gradients.
+//
+//   s = x + res (or x);  rstd = 1 / sqrt(mean(s^2) + eps);  y = s rstd w_k
+//   h = s rounded to the rows' type, the residual stream behind;  y in the rows' type, or as e4m3 codes with one fp32 scale for each
+//   row, scale = max|y| / 448 over the row's finite entries (for a product with scales by rows)
+// and backward, from h as it is kept, with u = dy w and dres what comes down the residual stream:
+//   dx = rstd (u - h rstd^2 mean(u h)) + dres  (the gradient of x and of res);  dw_k = sum over the worker's rows of dy h rstd
+// All arithmetic is fp32; y is taken from s before its rounding, which is in the registers anyway.
+// Bound by memory: every row is read once and lies in the registers of its lanes until both passes over it are done.
+#include <cmath>
+
+#include "qsr_internal.h"
+#include "row_io.h"
+
+namespace qsr {
+
+struct RmsArgs {
+    const void *x, *res;
+    const float *w;
+    void *sum, *y;
+    float *scale, *rstd;
+    long long rows, s_x, s_res, s_sum, s_y;    // rows of a worker; strides from row to row
+    int d;
+    float eps;
+};
+
+// Sum and maximum over the W wavefronts of a row: red holds W words, and the barrier behind keeps them until all have read
+template <int W>
+__device__ __forceinline__ float group_sum(float v, float *red)
+{
+    v = wave_sum(v);
+    if (W == 1) return v;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float r = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) r += red[i];
+    __syncthreads();
+    return r;
+}
+template <int W>
+__device__ __forceinline__ float group_max(float v, float *red)
+{
+    v = wave_max(v);
+    if (W == 1) return v;
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    __syncthreads();
+    float r = red[0];
+#pragma unroll
+    for (int i = 1; i < W; ++i) r = fmaxf(r, red[i]);
+    __syncthreads();
+    return r;
+}
+
+// A lane's part of a row of d elements in W wavefronts: up to NV runs of 16 bytes' worth, 64 W runs apart, and one of the d % E
+// elements behind the whole runs.  What a lane has no part in is zero.
+template <typename T, int NV> struct RowPart { float v[NV][wide_of<T>()], t; };
+
+template <typename T, int W, int NV, bool NT>
+__device__ __forceinline__ void load_row(const T *p, int lane, int d, RowPart<T, NV> &r)
+{
+    constexpr int E = wide_of<T>();
+    const int runs = d / E, rest = d - runs * E;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int i = lane + c * 64 * W;
+#pragma unroll
+        for (int u = 0; u < E; ++u) r.v[c][u] = 0.f;
+        if (i < runs) load_wide<T, E, NT>(p + i * E, r.v[c]);
+    }
+    r.t = lane < rest ? (float)p[runs * E + lane] : 0.f;
+}
+template <typename T, int W, int NV, bool NT>
+__device__ __forceinline__ void store_row(T *p, int lane, int d, const RowPart<T, NV> &r)
+{
+    constexpr int E = wide_of<T>();
+    const int runs = d / E, rest = d - runs * E;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int i = lane + c * 64 * W;
+        if (i < runs) store_wide<T, E, NT>(p + i * E, r.v[c]);
+    }
+    if (lane < rest) p[runs * E + lane] = (T)r.t;
+}
+// fp32 words (the weight, its gradient) in the lanes of a row of T
+template <typename T, int W, int NV>
+__device__ __forceinline__ void load_words(const float *p, int lane, int d, RowPart<T, NV> &r)
+{
+    constexpr int E = wide_of<T>();
+    const int runs = d / E, rest = d - runs * E;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int i = lane + c * 64 * W;
+#pragma unroll
+        for (int u = 0; u < E; ++u) r.v[c][u] = 0.f;
+        if (i < runs) {
+#pragma unroll
+            for (int q = 0; q < E; q += 4) {
+                float f[4];
+                load_wide<float, 4, false>(p + i * E + q, f);
+#pragma unroll
+                for (int u = 0; u < 4; ++u) r.v[c][q + u] = f[u];
+            }
+        }
+    }
+    r.t = lane < rest ? p[runs * E + lane] : 0.f;
+}
+template <typename T, int W, int NV>
+__device__ __forceinline__ void store_words(float *p, int lane, int d, const RowPart<T, NV> &r)
+{
+    constexpr int E = wide_of<T>();
+    const int runs = d / E, rest = d - runs * E;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int i = lane + c * 64 * W;
+        if (i < runs) {
+#pragma unroll
+            for (int q = 0; q < E; q += 4) {
+                const float f[4] = {r.v[c][q], r.v[c][q + 1], r.v[c][q + 2], r.v[c][q + 3]};
+                store_wide<float, 4, false>(p + i * E + q, f);
+            }
+        }
+    }
+    if (lane < rest) p[runs * E + lane] = r.t;
+}
+// f(element of a, element of b) for all of them
+template <typename T, int NV, typename F>
+__device__ __forceinline__ void each(RowPart<T, NV> &a, RowPart<T, NV> &b, F f)
+{
+#pragma unroll
+    for (int c = 0; c < NV; ++c)
+#pragma unroll
+        for (int u = 0; u < wide_of<T>(); ++u) f(a.v[c][u], b.v[c][u]);
+    f(a.t, b.t);
+}
+
+// W wavefronts to a row, a workgroup of one row (W > 1) or of four (W == 1)
+template <int W> constexpr int rms_threads() { return W == 1 ? 256 : 64 * W; }
+
+template <typename T, int W, int NV, bool FP8>
+__device__ __forceinline__ void rmsnorm_row(const RmsArgs &a, int k, long long row, int lane, float *red)
+{
+    constexpr int E = wide_of<T>();
+    RowPart<T, NV> s, w;
+    load_row<T, W, NV, true>((const T *)a.x + row * a.s_x, lane, a.d, s);
+    if (a.res != nullptr) {
+        load_row<T, W, NV, true>((const T *)a.res + row * a.s_res, lane, a.d, w);
+        each(s, w, [](float &x, float &r) { x += r; });
+    }
+    load_words<T, W, NV>(a.w + (long long)k * a.d, lane, a.d, w);
+    float q = 0.f;
+    each(s, w, [&](float &x, float &) { q = fmaf(x, x, q); });
+    if (a.sum != nullptr) store_row<T, W, NV, false>((T *)a.sum + row * a.s_sum, lane, a.d, s);
+    const float rstd = 1.f / sqrtf(group_sum<W>(q, red) / (float)a.d + a.eps);
+    if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
+    float top = 0.f;
+    each(s, w, [&](float &x, float &wx) {
+        x = x * rstd * wx;
+        if (FP8 && fabsf(x) < INFINITY) top = fmaxf(top, fabsf(x));
+    });
+    if (!FP8) {
+        store_row<T, W, NV, false>((T *)a.y + row * a.s_y, lane, a.d, s);
+        return;
+    }
+    top = group_max<W>(top, red);
+    const float scale = top >= 1e-35f ? top * (1.f / E4M3_MAX) : 0.f;      // less would leave the range of floats
+    if (lane == 0) a.scale[row] = scale;
+    const float f = scale > 0.f ? 1.f / scale : 0.f;
+    // a rounding above 448 at most, which still becomes 448; what is not finite becomes NaN
+    each(s, w, [&](float &x, float &) { x *= f; });
+    uint8_t *const y = (uint8_t *)a.y + row * a.s_y;
+    const int runs = a.d / E, rest = a.d - runs * E;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        const int i = lane + c * 64 * W;
+        typedef typename Wide<uint8_t, E>::vec Codes;
+        union { uint32_t w[E / 4]; uint8_t b[E]; } code;
+#pragma unroll
+        for (int g = 0; g < E; g += 4) code.w[g / 4] = e4m3_near4(&s.v[c][g]);
+        Codes out;
+#pragma unroll
+        for (int u = 0; u < E; ++u) out[u] = code.b[u];
+        if (i < runs) *(Codes *)(y + i * E) = out;
+    }
+    if (lane < rest) {
+        const float one[4] = {s.t, 0.f, 0.f, 0.f};
+        y[runs * E + lane] = (uint8_t)e4m3_near4(one);
+    }
+}
+
+template <typename T, int W, int NV, bool FP8>
+__global__ __launch_bounds__(rms_threads<W>()) void rmsnorm_kernel(RmsArgs a)
+{
+    __shared__ float red[W];
+    const int k = blockIdx.y, lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int side = W == 1 ? 4 : 1, at = W == 1 ? threadIdx.x >> 6 : 0;
+    for (long long r = (long long)blockIdx.x * side + at; r < a.rows; r += (long long)gridDim.x * side)
+        rmsnorm_row<T, W, NV, FP8>(a, k, k * a.rows + r, lane, red);
+}
+
+struct RmsBackArgs {
+    const void *dy, *h;
+    const float *w, *rstd;
+    const void *dres;
+    void *dx;
+    float *partial;                            // [K][groups][d]
+    long long rows, s_dy, s_h, s_dres, s_dx;
+    int d;
+};
+
+// A workgroup takes every gridDim.x-th row (W == 1: four of them at a time) and keeps its part of the weight's gradient in registers.
+template <typename T, int W, int NV>
+__global__ __launch_bounds__(rms_threads<W>()) void rmsnorm_back_kernel(RmsBackArgs a)
+{
+    constexpr int E = wide_of<T>();
+    __shared__ float red[W];
+    __shared__ float side_dw[W == 1 ? 3 * 64 * (NV * E + 1) : 1];
+    const int k = blockIdx.y, lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
+    const int side = W == 1 ? 4 : 1, at = W == 1 ? threadIdx.x >> 6 : 0;
+    RowPart<T, NV> w, dw;
+    load_words<T, W, NV>(a.w + (long long)k * a.d, lane, a.d, w);
+    each(dw, w, [](float &x, float &) { x = 0.f; });
+    for (long long r = (long long)blockIdx.x * side + at; r < a.rows; r += (long long)gridDim.x * side) {
+        const long long row = k * a.rows + r;
+        RowPart<T, NV> g, h, e;
+        load_row<T, W, NV, true>((const T *)a.dy + row * a.s_dy, lane, a.d, g);
+        load_row<T, W, NV, true>((const T *)a.h + row * a.s_h, lane, a.d, h);
+        if (a.dres != nullptr) load_row<T, W, NV, true>((const T *)a.dres + row * a.s_dres, lane, a.d, e);
+        else each(e, e, [](float &x, float &) { x = 0.f; });
+        const float rstd = a.rstd[row];
+        each(h, h, [&](float &x, float &) { x *= rstd; });
+        float q = 0.f;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+#pragma unroll
+            for (int u = 0; u < wide_of<T>(); ++u) {
+                dw.v[c][u] = fmaf(g.v[c][u], h.v[c][u], dw.v[c][u]);
+                g.v[c][u] *= w.v[c][u];
+                q = fmaf(g.v[c][u], h.v[c][u], q);
+            }
+        dw.t = fmaf(g.t, h.t, dw.t);
+        g.t *= w.t;
+        q = fmaf(g.t, h.t, q);
+        const float mean = group_sum<W>(q, red) / (float)a.d;
+        each(g, h, [&](float &x, float &n) { x = rstd * fmaf(-n, mean, x); });
+        each(g, e, [&](float &x, float &y) { x += y; });
+        store_row<T, W, NV, true>((T *)a.dx + row * a.s_dx, lane, a.d, g);
+    }
+    if (W == 1) {                              // the four wavefronts' sums become one, in their order
+        float *const mine = side_dw + ((at - 1) * 64 + lane) * (NV * E + 1);
+        int n = 0;
+        if (at > 0) each(dw, w, [&](float &x, float &) { mine[n++] = x; });
+        __syncthreads();
+        if (at > 0) return;
+#pragma unroll
+        for (int o = 0; o < 3; ++o) {
+            const float *const other = side_dw + (o * 64 + lane) * (NV * E + 1);
+            n = 0;
+            each(dw, w, [&](float &x, float &) { x += other[n++]; });
+        }
+    }
+    store_words<T, W, NV>(a.partial + ((long long)k * gridDim.x + blockIdx.x) * a.d, lane, a.d, dw);
+}
+
+// dw[k][j] = sum over the parts: 32 columns and 8 runs of parts, four of each in flight, to a workgroup; a fixed order
+__global__ __launch_bounds__(256) void rmsnorm_weight_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dw)
+{
+    __shared__ float red[8][32];
+    const int k = blockIdx.y, col = threadIdx.x & 31, run = threadIdx.x >> 5;
+    const int j = blockIdx.x * 32 + col;
+    const float *p = partial + (long long)k * parts * d + j;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (j < d)
+        for (int i = run; i < parts; i += 32)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u * 8 < parts) s[u] += p[(long long)(i + u * 8) * d];
+    red[run][col] = (s[0] + s[1]) + (s[2] + s[3]);
+    __syncthreads();
+    if (run != 0 || j >= d) return;
+    float sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum += red[i][col];
+    dw[(long long)k * d + j] = sum;
+}
+
+constexpr int RMS_MAX_D = 16384;
+
+// Workgroups of a worker in the forward pass: one trip each
+static long long fwd_groups(long long rows, int W)
+{
+    const long long need = W == 1 ? (rows + 3) / 4 : rows;
+    return need < (1 << 20) ? need : 1 << 20;
+}
+// Workgroups of a worker in the backward pass
+static long long back_groups(int K, long long rows, int W)
+{
+    const long long side = W == 1 ? 4 : 1;
+    long long most = (1024 + K - 1) / K;
+    const long long need = (rows + side - 1) / side;
+    if (most > need) most = need;
+    return most < 1 ? 1 : most;
+}
+
+// Wavefronts of a row, and runs of a lane: eight or sixteen elements to a lane
+#define RMS_BY_WIDTH(T, d, F) do { constexpr int E_ = wide_of<T>(); \
+    if ((d) <= 512) F(T, 1, 8 / E_); else if ((d) <= 1024) F(T, 1, 16 / E_); else if ((d) <= 2048) F(T, 4, 8 / E_); \
+    else if ((d) <= 4096) F(T, 4, 16 / E_); else if ((d) <= 8192) F(T, 8, 16 / E_); else F(T, 16, 16 / E_); } while (0)
+static int rms_waves(long long d) { return d <= 1024 ? 1 : d <= 4096 ? 4 : d <= 8192 ? 8 : 16; }
+
+template <typename T>
+static hipError_t launch_rms(const RmsArgs &a, int K, bool fp8, hipStream_t s)
+{
+#define RMS_FWD(T, W, NV) do { const dim3 grid((unsigned)fwd_groups(a.rows, W), (unsigned)K); \
+    if (fp8) rmsnorm_kernel<T, W, NV, true><<<grid, rms_threads<W>(), 0, s>>>(a); \
+    else rmsnorm_kernel<T, W, NV, false><<<grid, rms_threads<W>(), 0, s>>>(a); } while (0)
+    RMS_BY_WIDTH(T, a.d, RMS_FWD);
+#undef RMS_FWD
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_rms_back(const RmsBackArgs &a, int K, float *dw, hipStream_t s)
+{
+    const int W = rms_waves(a.d);
+    const long long groups = back_groups(K, a.rows, W);
+#define RMS_BACK(T, W, NV) rmsnorm_back_kernel<T, W, NV><<<dim3((unsigned)groups, (unsigned)K), rms_threads<W>(), 0, s>>>(a)
+    RMS_BY_WIDTH(T, a.d, RMS_BACK);
+#undef RMS_BACK
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    rmsnorm_weight_kernel<<<dim3((unsigned)((a.d + 31) / 32), (unsigned)K), 256, 0, s>>>(a.partial, (int)groups, a.d, dw);
+    return hipGetLastError();
+}
+
+}  // namespace qsr
+
+using namespace qsr;
+
+static int finish(hipError_t e)
+{
+    if (e == hipSuccess) return QSR_OK;
+    set_last_hip_error((int)e);
+    return QSR_EHIP;
+}
+static bool off(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+static uintptr_t size_of(int type) { return type == QSR_TYPE_F32 ? 4 : 2; }
+static bool sizes_ok(int32_t K, int64_t rows, int64_t d)
+{
+    return K >= 1 && K <= 65535 && rows >= 0 && rows <= ((long long)1 << 31) && d >= 1;
+}
+
+extern "C" int qsr_rmsnorm(const qsr_rmsnorm_args *q, void *stream)
+{
+    if (!q || !sizes_ok(q->K, q->rows, q->d)) return QSR_EINVAL;
+    if (q->type != QSR_TYPE_F32 && q->type != QSR_TYPE_BF16) return QSR_EINVAL;
+    const bool fp8 = q->y_type == QSR_TYPE_E4M3;
+    if (!fp8 && q->y_type != q->type) return QSR_EINVAL;
+    const uintptr_t es = size_of(q->type);
+    if (!(std::isfinite(q->eps) && q->eps >= 0.0)) return QSR_EINVAL;
+    if (q->d > RMS_MAX_D) return QSR_ELIMIT;
+    if (q->rows == 0) return QSR_OK;
+    if (!q->x || off(q->x, es) || off(q->residual, es) || !q->weight || off(q->weight, 4) || off(q->sum, es) || !q->y ||
+        (!fp8 && off(q->y, es)) || off(q->rstd, 4) || off(q->scale, 4) || (fp8 && !q->scale))
+        return QSR_EINVAL;
+    if (q->x_stride < q->d || q->y_stride < q->d || (q->residual && q->residual_stride < q->d) || (q->sum && q->sum_stride < q->d))
+        return QSR_EINVAL;
+    const RmsArgs a{q->x, q->residual, q->weight, q->sum, q->y, fp8 ? q->scale : nullptr, q->rstd, q->rows, q->x_stride,
+                    q->residual_stride, q->sum_stride, q->y_stride, (int)q->d, (float)q->eps};
+    return finish(q->type == QSR_TYPE_F32 ? launch_rms<float>(a, q->K, fp8, (hipStream_t)stream)
+                                          : launch_rms<bf16_t>(a, q->K, fp8, (hipStream_t)stream));
+}
+
+extern "C" int qsr_rmsnorm_workspace_bytes(int32_t K, int64_t rows, int64_t d, int32_t type, size_t *bytes)
+{
+    if (!bytes) return QSR_EINVAL;
+    *bytes = 0;
+    if (!sizes_ok(K, rows, d) || (type != QSR_TYPE_F32 && type != QSR_TYPE_BF16)) return QSR_EINVAL;
+    if (d > RMS_MAX_D) return QSR_ELIMIT;
+    const int W = rms_waves(d);
+    *bytes = (size_t)K * (size_t)back_groups(K, rows, W) * (size_t)d * sizeof(float);
+    return QSR_OK;
+}
+
+extern "C" int qsr_rmsnorm_backward(const qsr_rmsnorm_backward_args *q, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q || !sizes_ok(q->K, q->rows, q->d)) return QSR_EINVAL;
+    if (q->type != QSR_TYPE_F32 && q->type != QSR_TYPE_BF16) return QSR_EINVAL;
+    const uintptr_t es = size_of(q->type);
+    if (!q->weight || off(q->weight, 4) || !q->weight_grad || off(q->weight_grad, 4)) return QSR_EINVAL;
+    if (q->rows > 0 && (!q->y_grad || off(q->y_grad, es) || !q->sum || off(q->sum, es) || !q->rstd || off(q->rstd, 4) ||
+                        off(q->residual_grad, es) || !q->x_grad || off(q->x_grad, es)))
+        return QSR_EINVAL;
+    if (q->y_grad_stride < q->d || q->sum_stride < q->d || q->x_grad_stride < q->d ||
+        (q->residual_grad && q->residual_grad_stride < q->d))
+        return QSR_EINVAL;
+    size_t need = 0;
+    const int rc = qsr_rmsnorm_workspace_bytes(q->K, q->rows, q->d, q->type, &need);
+    if (rc != QSR_OK) return rc;
+    if (!workspace || off(workspace, 4)) return QSR_EINVAL;
+    if (workspace_bytes < need) return QSR_ENOMEM;
+    const RmsBackArgs a{q->y_grad, q->sum, q->weight, q->rstd, q->residual_grad, q->x_grad, (float *)workspace, q->rows,
+                        q->y_grad_stride, q->sum_stride, q->residual_grad_stride, q->x_grad_stride, (int)q->d};
+    return finish(q->type == QSR_TYPE_F32 ? launch_rms_back<float>(a, q->K, q->weight_grad, (hipStream_t)stream)
+                                          : launch_rms_back<bf16_t>(a, q->K, q->weight_grad, (hipStream_t)stream));
+}
