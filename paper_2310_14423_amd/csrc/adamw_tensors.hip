@@ -31,7 +31,7 @@
 namespace qsr {
 
 constexpr int AT_BLOCK = 256;                  // elements that share a scale
-constexpr int AT_SPAN = 4;                     // blocks of a wavefront's trip
+constexpr int AT_SPAN = 2;                     // blocks of a wavefront's trip (four: 900 against 869 us for 2 x 85e6 with fp32 moments)
 
 struct AtTensor {
     float *param;
@@ -47,34 +47,207 @@ struct AtChunk { int tensor, block; };         // a trip's first block
 struct AtStep { double eta; float step, rsq, c1, c2, eps; uint32_t key; };
 
 // 16 random bits for either moment: index counts the worker's elements over all tensors, padded to blocks
-__device__ __forceinline__ uint32_t at_word(uint32_t index, uint32_t worker, uint32_t key)
+// (plus the worker's number times an odd constant)
+__device__ __forceinline__ uint32_t at_word(uint32_t index, uint32_t key)
 {
-    uint32_t x = (index + worker * 0x9E3779B9u) ^ key;
+    uint32_t x = index ^ key;
     x ^= x >> 16; x *= 0x21F0AAADu;
     x ^= x >> 15; x *= 0x735A2D97u;
     return x ^ (x >> 15);
 }
 
-// The codes' factor and scale of a block whose largest finite magnitude is `top`
-__device__ __forceinline__ void at_scale(float top, float &factor, float &scale)
+// A trip's rows, as pointers to its first element
+template <typename G> struct AtRows {
+    float *th;
+    const G *g;
+    bf16_t *copy;
+    __device__ __forceinline__ AtRows(const AtTensor &t, long long k, long long e)
+        : th(global(t.param) + k * t.s_param + e), g(global((const G *)t.grad) + k * t.s_grad + e),
+          copy(t.copy != nullptr ? global(t.copy) + k * t.s_copy + e : nullptr) {}
+};
+
+// FULL: the trip's elements are all there.  Otherwise `left` are, of which a lane may have four, some or none in each block.
+template <typename T, bool FULL>
+__device__ __forceinline__ void at_load(const T *p, long long left, float (&v)[4])
 {
-    const bool some = top >= 1e-35f;
-    factor = some ? 1.f / top * E4M3_MAX : 0.f;
-    scale = some ? top * (1.f / E4M3_MAX) : 0.f;
+    if (FULL || left >= 4) load_wide<T, 4, true>(p, v);
+    else load_some(p, (int)left, v);
+}
+template <typename T, bool FULL>
+__device__ __forceinline__ void at_store(T *p, long long left, const float (&v)[4])
+{
+    if (FULL || left >= 4) store_wide<T, 4, true>(p, v);
+    else store_some(p, (int)left, v);
+}
+
+template <typename G, bool FULL>
+__device__ __forceinline__ void at_trip_f32(const AtTensor &t, const AtStep &st, long long k, long long e0, float gs)
+{
+    const int lane = threadIdx.x;
+    const AtRows<G> q(t, k, e0);
+    float *const m = global((float *)t.m) + k * t.s_state + e0, *const v = global((float *)t.v) + k * t.s_state + e0;
+    const float etalam = (float)(st.eta * t.decay);
+    float a[AT_SPAN][4], b[AT_SPAN][4], c[AT_SPAN][4], d[AT_SPAN][4];
+#pragma unroll
+    for (int u = 0; u < AT_SPAN; ++u) {
+        const int i = u * AT_BLOCK + lane * 4;
+        const long long left = t.n - e0 - i;
+        at_load<float, FULL>(q.th + i, left, a[u]);
+        at_load<float, FULL>(m + i, left, c[u]);
+        at_load<float, FULL>(v + i, left, d[u]);
+        at_load<G, FULL>(q.g + i, left, b[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < AT_SPAN; ++u) {
+        const int i = u * AT_BLOCK + lane * 4;
+        const long long left = t.n - e0 - i;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            adamw_elem(a[u][j], b[u][j] * gs, c[u][j], d[u][j], etalam, st.step, st.rsq, st.c1, st.c2, st.eps);
+        at_store<float, FULL>(q.th + i, left, a[u]);
+        at_store<float, FULL>(m + i, left, c[u]);
+        at_store<float, FULL>(v + i, left, d[u]);
+        if (q.copy != nullptr) at_store<bf16_t, FULL>(q.copy + i, left, a[u]);
+    }
+}
+
+// The square root, rounded to nearest where x >= 2^-96 (an ulp below that), by trying the neighbours of the instruction's result:
+// x lies above s (s + ulp) where s + ulp is nearer, and not above s (s - ulp) where s - ulp is
+__device__ __forceinline__ float root(float x)
+{
+    const float s = __builtin_amdgcn_sqrtf(x);
+    const float lo = __int_as_float(__float_as_int(s) - 1), hi = __int_as_float(__float_as_int(s) + 1);
+    float r = fmaf(-lo, s, x) <= 0.f ? lo : s;
+    r = fmaf(-hi, s, x) > 0.f ? hi : r;
+    return r;
+}
+// One element with 8-bit moments: m, the root r of v, and theta.  What leads to a code is rounded operation by operation; the step
+// itself is not held to that (a reciprocal within an ulp).
+__device__ __forceinline__ void adamw_rounded(float &th, float g, float &m, float &r, float etalam, const AtStep &st)
+{
+    {
+#pragma clang fp contract(off)
+        const float v = r * r;
+        m = m + st.c1 * (g - m);
+        r = root(v + st.c2 * (g * g - v));
+    }
+    th = th - fmaf(etalam, th, st.step * m * __builtin_amdgcn_rcpf(fmaf(r, st.rsq, st.eps)));
 }
 __device__ __forceinline__ float finite_or_zero(float x) { return fabsf(x) < INFINITY ? x : 0.f; }
-// The factor's rounding may take the largest value past 448, which could round to NaN; what is not finite shall become NaN.
-__device__ __forceinline__ float at_most_448(float y) { return fabsf(y) < 449.f ? fminf(fmaxf(y, -E4M3_MAX), E4M3_MAX) : y; }
-// One element with 8-bit moments: new m, v's root r and theta
-__device__ __forceinline__ void adamw_rounded(float &th, float g, float &m, float r0, float &r, float etalam, const float stepsz, float rsq,
-                                              float c1, float c2, float eps)
+
+// The codes of four elements, x * factor to the value below or above; ROOTS: what is not zero does not become zero
+template <bool FINITE, bool ROOTS>
+__device__ __forceinline__ uint32_t at_codes(const float (&x)[4], float factor, const uint32_t (&word)[4])
 {
-#pragma clang fp contract(off)
-    const float v0 = r0 * r0;
-    m = m + c1 * (g - m);
-    r = sqrtf(v0 + c2 * (g * g - v0));
-    const float upd = stepsz * m / (r * rsq + eps);
-    th = th - (etalam * th + upd);
+    int code = 0;
+    float y[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        y[j] = x[j] * factor;
+        // the factor's rounding may take the largest value past 448, which could round to NaN; what is not finite shall become NaN
+        y[j] = __builtin_amdgcn_fmed3f(y[j], ROOTS ? E4M3_TINY : -E4M3_MAX, E4M3_MAX);
+        if (ROOTS) y[j] = x[j] > 0.f ? y[j] : 0.f;
+        if (!FINITE && !(fabsf(x[j]) < INFINITY)) y[j] = NAN;
+    }
+    code = __builtin_amdgcn_cvt_sr_fp8_f32(y[0], ROOTS ? word[0] << 16 : word[0] & 0xFFFF0000u, code, 0);
+    code = __builtin_amdgcn_cvt_sr_fp8_f32(y[1], ROOTS ? word[1] << 16 : word[1] & 0xFFFF0000u, code, 1);
+    code = __builtin_amdgcn_cvt_sr_fp8_f32(y[2], ROOTS ? word[2] << 16 : word[2] & 0xFFFF0000u, code, 2);
+    code = __builtin_amdgcn_cvt_sr_fp8_f32(y[3], ROOTS ? word[3] << 16 : word[3] & 0xFFFF0000u, code, 3);
+    return (uint32_t)code;
+}
+
+// Lane 2u + s < 2 AT_SPAN holds what belongs to block u of the trip and to m (s = 0) or r (s = 1): the scales, and the divisions
+// behind the factors, are one for all blocks.
+template <typename G, bool FULL>
+__device__ __forceinline__ void at_trip_fp8(const AtTensor &t, const AtStep &st, long long k, long long e0, float gs)
+{
+    const int lane = threadIdx.x;
+    const AtRows<G> q(t, k, e0);
+    uint8_t *const mc = global((uint8_t *)t.m) + k * t.s_state + e0, *const vc = global((uint8_t *)t.v) + k * t.s_state + e0;
+    const float etalam = (float)(st.eta * t.decay);
+    const int blocks = FULL ? AT_SPAN : min(AT_SPAN, (int)((t.n - e0 + AT_BLOCK - 1) / AT_BLOCK));
+    float *const sc = (lane & 1 ? global(t.v_scale) : global(t.m_scale)) + k * t.s_scale + e0 / AT_BLOCK + (lane >> 1);
+    const bool holds = lane < 2 * blocks;
+    float a[AT_SPAN][4], b[AT_SPAN][4], c[AT_SPAN][4], d[AT_SPAN][4];
+    uint32_t cm[AT_SPAN], cv[AT_SPAN];
+    const float scale0 = holds ? *sc : 0.f;
+#pragma unroll
+    for (int u = 0; u < AT_SPAN; ++u) {
+        const int i = u * AT_BLOCK + lane * 4;
+        const long long left = t.n - e0 - i;
+        at_load<float, FULL>(q.th + i, left, a[u]);
+        at_load<G, FULL>(q.g + i, left, b[u]);
+        // rows of codes are whole blocks: no part of one is missing
+        cm[u] = cv[u] = 0;
+        if (u < blocks) {
+            cm[u] = __builtin_nontemporal_load((const uint32_t *)(mc + i));
+            cv[u] = __builtin_nontemporal_load((const uint32_t *)(vc + i));
+        }
+    }
+    uint32_t top[2 * AT_SPAN];
+#pragma unroll
+    for (int u = 0; u < AT_SPAN; ++u) {
+        const int i = u * AT_BLOCK + lane * 4;
+        const long long left = t.n - e0 - i;
+        const float ms = lane_of(scale0, 2 * u), vs = lane_of(scale0, 2 * u + 1);
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        const f2 m01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)cm[u], false), m23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)cm[u], true);
+        const f2 v01 = __builtin_amdgcn_cvt_pk_f32_fp8((int)cv[u], false), v23 = __builtin_amdgcn_cvt_pk_f32_fp8((int)cv[u], true);
+        c[u][0] = m01.x * ms; c[u][1] = m01.y * ms; c[u][2] = m23.x * ms; c[u][3] = m23.y * ms;
+        d[u][0] = v01.x * vs; d[u][1] = v01.y * vs; d[u][2] = v23.x * vs; d[u][3] = v23.y * vs;
+        uint32_t tm = 0, tv = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            adamw_rounded(a[u][j], b[u][j] * gs, c[u][j], d[u][j], etalam, st);
+            if (!FULL && j >= left) c[u][j] = d[u][j] = 0.f;
+            tm = max(tm, __float_as_uint(c[u][j]) & 0x7FFFFFFFu);
+            tv = max(tv, __float_as_uint(d[u][j]) & 0x7FFFFFFFu);
+        }
+        at_store<float, FULL>(q.th + i, left, a[u]);
+        if (q.copy != nullptr) at_store<bf16_t, FULL>(q.copy + i, left, a[u]);
+        top[2 * u] = wave_max(tm);
+        top[2 * u + 1] = wave_max(tv);
+    }
+    // as whole numbers, magnitudes order like floats, with infinities and NaN above: then the largest of the others is looked for
+    uint32_t most = top[0];
+#pragma unroll
+    for (int u = 1; u < 2 * AT_SPAN; ++u) most = max(most, top[u]);
+    const bool finite = most < 0x7F800000u;
+    if (!finite) {
+#pragma unroll
+        for (int u = 0; u < AT_SPAN; ++u) {
+            float tm = 0.f, tv = 0.f;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                tm = fmaxf(tm, fabsf(finite_or_zero(c[u][j])));
+                tv = fmaxf(tv, finite_or_zero(d[u][j]));
+            }
+            top[2 * u] = __float_as_uint(wave_max(tm));
+            top[2 * u + 1] = __float_as_uint(wave_max(tv));
+        }
+    }
+    uint32_t mine = 0;
+#pragma unroll
+    for (int u = 0; u < 2 * AT_SPAN; ++u) mine = lane == u ? top[u] : mine;
+    const float largest = __uint_as_float(mine);
+    const bool some = largest >= 1e-35f;
+    const float factor = some ? 1.f / largest * E4M3_MAX : 0.f;
+    if (holds) *sc = some ? largest * (1.f / E4M3_MAX) : 0.f;
+    const uint32_t index = (uint32_t)((t.first * AT_BLOCK) + e0 + lane * 4) + (uint32_t)k * 0x9E3779B9u;
+#pragma unroll
+    for (int u = 0; u < AT_SPAN; ++u) {
+        const float fm = lane_of(factor, 2 * u), fv = lane_of(factor, 2 * u + 1);
+        uint32_t word[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) word[j] = at_word(index + u * AT_BLOCK + j, st.key);
+        const uint32_t nm = finite ? at_codes<true, false>(c[u], fm, word) : at_codes<false, false>(c[u], fm, word);
+        const uint32_t nv = finite ? at_codes<true, true>(d[u], fv, word) : at_codes<false, true>(d[u], fv, word);
+        if (u < blocks) {
+            const int i = u * AT_BLOCK + lane * 4;
+            __builtin_nontemporal_store(nm, (uint32_t *)(mc + i));
+            __builtin_nontemporal_store(nv, (uint32_t *)(vc + i));
+        }
+    }
 }
 
 template <typename G, bool FP8>
@@ -82,98 +255,16 @@ __global__ __launch_bounds__(64) void adamw_tensors_kernel(const AtTensor *__res
                                                            AtStep st, const float *__restrict__ coef)
 {
     const AtChunk ch = chunks[blockIdx.x];
-    const AtTensor t = list[ch.tensor];
-    const int k = blockIdx.y, lane = threadIdx.x;
+    const AtTensor &t = list[ch.tensor];
+    const long long k = blockIdx.y, e0 = (long long)ch.block * AT_BLOCK;
     const float gs = coef != nullptr ? coef[k] : 1.f;
-    const float etalam = (float)(st.eta * t.decay);
-    float *const th = t.param + k * t.s_param;
-    const G *const g = (const G *)t.grad + k * t.s_grad;
-    const long long e0 = (long long)ch.block * AT_BLOCK + lane * 4;
-    float a[AT_SPAN][4], b[AT_SPAN][4], c[AT_SPAN][4], d[AT_SPAN][4];
-#pragma unroll
-    for (int u = 0; u < AT_SPAN; ++u) {
-        const long long e = e0 + u * AT_BLOCK;
-        const long long left = t.n - e;
-        if (left >= 4) {
-            load_wide<float, 4, true>(th + e, a[u]);
-            load_wide<G, 4, true>(g + e, b[u]);
-        } else {
-            load_some(th + e, (int)left, a[u]);
-            load_some(g + e, (int)left, b[u]);
-        }
-        if (FP8) {
-            // rows of codes are whole blocks: no part of one is missing
-            if (t.n > e - lane * 4) {
-                const long long blk = (e - lane * 4) / AT_BLOCK;
-                const uint32_t mc = __builtin_nontemporal_load((const uint32_t *)((const uint8_t *)t.m + k * t.s_state + e));
-                const uint32_t vc = __builtin_nontemporal_load((const uint32_t *)((const uint8_t *)t.v + k * t.s_state + e));
-                const float ms = t.m_scale[k * t.s_scale + blk], vs = t.v_scale[k * t.s_scale + blk];
-                c[u][0] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 0); c[u][1] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 1);
-                c[u][2] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 2); c[u][3] = ms * __builtin_amdgcn_cvt_f32_fp8((int)mc, 3);
-                d[u][0] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 0); d[u][1] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 1);
-                d[u][2] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 2); d[u][3] = vs * __builtin_amdgcn_cvt_f32_fp8((int)vc, 3);
-            }
-        } else if (left >= 4) {
-            load_wide<float, 4, true>((const float *)t.m + k * t.s_state + e, c[u]);
-            load_wide<float, 4, true>((const float *)t.v + k * t.s_state + e, d[u]);
-        } else {
-            load_some((const float *)t.m + k * t.s_state + e, (int)left, c[u]);
-            load_some((const float *)t.v + k * t.s_state + e, (int)left, d[u]);
-        }
-    }
-#pragma unroll
-    for (int u = 0; u < AT_SPAN; ++u) {
-        const long long e = e0 + u * AT_BLOCK;
-        const long long left = t.n - e;
-        if (t.n <= e - lane * 4) break;                    // the whole wavefront
-        float r[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (FP8) adamw_rounded(a[u][i], b[u][i] * gs, c[u][i], d[u][i], r[i], etalam, st.step, st.rsq, st.c1, st.c2, st.eps);
-            else adamw_elem(a[u][i], b[u][i] * gs, c[u][i], d[u][i], etalam, st.step, st.rsq, st.c1, st.c2, st.eps);
-            if (FP8 && i >= left) c[u][i] = r[i] = 0.f;
-        }
-        if (left >= 4) store_wide<float, 4, true>(th + e, a[u]);
-        else store_some(th + e, (int)left, a[u]);
-        if (t.copy != nullptr) {
-            bf16_t *const y = t.copy + k * t.s_copy;
-            if (left >= 4) store_wide<bf16_t, 4, true>(y + e, a[u]);
-            else store_some(y + e, (int)left, a[u]);
-        }
-        if (!FP8) {
-            float *const m = (float *)t.m + k * t.s_state, *const v = (float *)t.v + k * t.s_state;
-            if (left >= 4) { store_wide<float, 4, true>(m + e, c[u]); store_wide<float, 4, true>(v + e, d[u]); }
-            else { store_some(m + e, (int)left, c[u]); store_some(v + e, (int)left, d[u]); }
-            continue;
-        }
-        float mtop = 0.f, rtop = 0.f;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            mtop = fmaxf(mtop, fabsf(finite_or_zero(c[u][i])));
-            rtop = fmaxf(rtop, finite_or_zero(r[i]));
-        }
-        mtop = wave_max(mtop); rtop = wave_max(rtop);
-        float mf, ms, rf, rs;
-        at_scale(mtop, mf, ms); at_scale(rtop, rf, rs);
-        const uint32_t index = (uint32_t)(t.first * AT_BLOCK + e);
-        int mc = 0, vc = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t w = at_word(index + i, (uint32_t)k, st.key);
-            const float x = at_most_448(c[u][i] * mf), q = at_most_448(r[i] * rf), y = q > 0.f ? fmaxf(q, E4M3_TINY) : q;
-            const uint32_t wm = w & 0xFFFF0000u, wv = w << 16;
-            if (i == 0) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 0); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 0); }
-            if (i == 1) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 1); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 1); }
-            if (i == 2) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 2); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 2); }
-            if (i == 3) { mc = __builtin_amdgcn_cvt_sr_fp8_f32(x, wm, mc, 3); vc = __builtin_amdgcn_cvt_sr_fp8_f32(y, wv, vc, 3); }
-        }
-        __builtin_nontemporal_store((uint32_t)mc, (uint32_t *)((uint8_t *)t.m + k * t.s_state + e));
-        __builtin_nontemporal_store((uint32_t)vc, (uint32_t *)((uint8_t *)t.v + k * t.s_state + e));
-        if (lane == 0) {
-            const long long blk = e / AT_BLOCK;
-            t.m_scale[k * t.s_scale + blk] = ms;
-            t.v_scale[k * t.s_scale + blk] = rs;
-        }
+    const bool full = t.n - e0 >= AT_SPAN * AT_BLOCK;
+    if (FP8) {
+        if (full) at_trip_fp8<G, true>(t, st, k, e0, gs);
+        else at_trip_fp8<G, false>(t, st, k, e0, gs);
+    } else {
+        if (full) at_trip_f32<G, true>(t, st, k, e0, gs);
+        else at_trip_f32<G, false>(t, st, k, e0, gs);
     }
 }
 
@@ -189,10 +280,21 @@ __global__ __launch_bounds__(AT_NORM_THREADS) void tensors_sqnorm_kernel(const A
     const AtSpan sp = spans[blockIdx.x];
     const AtTensor t = list[sp.tensor];
     const int k = blockIdx.y;
-    const G *const g = (const G *)t.grad + k * t.s_grad;
+    const G *const g = global((const G *)t.grad) + k * t.s_grad;
     const long long e0 = (long long)sp.block * AT_BLOCK, e1 = min(t.n, e0 + (long long)sp.blocks * AT_BLOCK);
     float s[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f};
-    for (long long e = e0 + threadIdx.x * 4; e < e1; e += AT_NORM_THREADS * 4) {
+    constexpr int U = 4, STEP = AT_NORM_THREADS * 4;
+    long long e = e0 + threadIdx.x * 4;
+    for (; e + (U - 1) * STEP + 4 <= e1; e += U * STEP) {
+        float x[U][4];
+#pragma unroll
+        for (int u = 0; u < U; ++u) load_wide<G, 4, false>(g + e + u * STEP, x[u]);
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add_comp(s[i], c[i], x[u][i] * x[u][i]);
+    }
+    for (; e < e1; e += STEP) {
         float x[4];
         if (e1 - e >= 4) load_wide<G, 4, false>(g + e, x);
         else load_some(g + e, (int)(e1 - e), x);
@@ -263,7 +365,7 @@ extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
     long long blocks = 0;
     for (int i = 0; !w && i < c->n_tensors; ++i) {
         const qsr_tensor &t = c->tensors[i];
-        if (t.n < 1 || t.n > ((long long)1 << 35)) { w = "a tensor's n"; break; }
+        if (t.n < 1 || t.n > ((long long)1 << 34)) { w = "a tensor's n"; break; }
         const long long nb = (t.n + AT_BLOCK - 1) / AT_BLOCK;
         blocks += nb;
         const bool many = c->K > 1;
@@ -276,7 +378,7 @@ extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
         else if (many && fp8 && (t.state_stride < nb * AT_BLOCK || t.state_stride % 4 != 0 || t.scale_stride < nb)) w = "a tensor's state_stride/scale_stride";
         else if (!finite_ge0(t.weight_decay)) w = "a tensor's weight_decay";
     }
-    if (!w && blocks > ((long long)1 << 27)) w = "tensors (above 2^35 elements together)";     // the grid's limit of 2^32 threads
+    if (!w && blocks > ((long long)1 << 26)) w = "tensors (above 2^34 elements together)";     // the grid's limit of 2^32 threads
     if (why) *why = w ? w : "ok";
     return w ? QSR_EINVAL : QSR_OK;
 }

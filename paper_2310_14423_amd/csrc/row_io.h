@@ -29,6 +29,9 @@ __device__ __forceinline__ void store_wide(T *p, const float (&v)[N])
     if (NT) __builtin_nontemporal_store(x, (V *)p);
     else *(V *)p = x;
 }
+// The address `bytes` behind p, where p is the same for a wavefront: one register for the distance instead of two for the address
+template <typename P> __device__ __forceinline__ P *behind(P *p, uint32_t bytes) { return (P *)((char *)p + bytes); }
+template <typename P> __device__ __forceinline__ const P *behind(const P *p, uint32_t bytes) { return (const P *)((const char *)p + bytes); }
 // The first `left` of N elements (left < N; none where it is not positive), the others as `fill`
 template <typename T, int N>
 __device__ __forceinline__ void load_some(const T *p, int left, float (&v)[N], float fill = 0.f)
@@ -55,18 +58,36 @@ __device__ __forceinline__ uint32_t e4m3_near4(const float *v)
 }
 constexpr float E4M3_MAX = 448.f, E4M3_TINY = 0.001953125f;         // largest value, smallest above zero (2^-9)
 
+// A pointer that was read from memory, as one into global memory: the compiler cannot know, and would use flat accesses
+template <typename T> __device__ __forceinline__ T *global(T *p) { return (T *)(__attribute__((address_space(1))) T *)(uintptr_t)p; }
+
+// Lanes exchanged within a row of 16 by the data-parallel primitives: after steps 0 to 3 of a sum or maximum every lane has its row's
+template <int STEP> __device__ __forceinline__ int row_step(int v)
+{
+    constexpr int ctrl = STEP == 0 ? 0xB1 : STEP == 1 ? 0x4E : STEP == 2 ? 0x141 : 0x140;   // xor 1, xor 2, half rows mirrored, rows mirrored
+    return __builtin_amdgcn_update_dpp(0, v, ctrl, 0xf, 0xf, true);
+}
+template <int STEP> __device__ __forceinline__ float row_step(float v) { return __int_as_float(row_step<STEP>(__float_as_int(v))); }
+__device__ __forceinline__ float lane_of(float v, int lane) { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), lane)); }
+
 // Sum and maximum over the 64 lanes of a wavefront, in every lane.  fmaxf: NaN gives way to any number.
 __device__ __forceinline__ float wave_sum(float v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-    return v;
+    v += row_step<0>(v); v += row_step<1>(v); v += row_step<2>(v); v += row_step<3>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
 __device__ __forceinline__ float wave_max(float v)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o, 64));
-    return v;
+    v = fmaxf(v, row_step<0>(v)); v = fmaxf(v, row_step<1>(v)); v = fmaxf(v, row_step<2>(v)); v = fmaxf(v, row_step<3>(v));
+    return fmaxf(fmaxf(lane_of(v, 0), lane_of(v, 16)), fmaxf(lane_of(v, 32), lane_of(v, 48)));
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v)
+{
+    v = max(v, (uint32_t)row_step<0>((int)v)); v = max(v, (uint32_t)row_step<1>((int)v));
+    v = max(v, (uint32_t)row_step<2>((int)v)); v = max(v, (uint32_t)row_step<3>((int)v));
+    const uint32_t a = max((uint32_t)__builtin_amdgcn_readlane((int)v, 0), (uint32_t)__builtin_amdgcn_readlane((int)v, 16));
+    const uint32_t b = max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48));
+    return max(a, b);
 }
 
 }  // namespace qsr
