@@ -24,51 +24,67 @@ struct RmsArgs {
     float eps;
 };
 
-// Sum and maximum over the W wavefronts of a row: red holds W words, and the barrier behind keeps them until all have read
+// Sum and maximum over the W wavefronts of a row.  red: two sets of W words that take turns (`turn`): a set is written again behind
+// the next barrier, when all have read it.
 template <int W>
-__device__ __forceinline__ float group_sum(float v, float *red)
+__device__ __forceinline__ float group_sum(float v, float (*red)[W], int turn)
 {
     v = wave_sum(v);
     if (W == 1) return v;
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) red[turn & 1][threadIdx.x >> 6] = v;
     __syncthreads();
     float r = 0.f;
 #pragma unroll
-    for (int i = 0; i < W; ++i) r += red[i];
-    __syncthreads();
+    for (int i = 0; i < W; ++i) r += red[turn & 1][i];
     return r;
 }
 template <int W>
-__device__ __forceinline__ float group_max(float v, float *red)
+__device__ __forceinline__ float group_max(float v, float (*red)[W], int turn)
 {
     v = wave_max(v);
     if (W == 1) return v;
-    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
+    if ((threadIdx.x & 63) == 0) red[turn & 1][threadIdx.x >> 6] = v;
     __syncthreads();
-    float r = red[0];
+    float r = red[turn & 1][0];
 #pragma unroll
-    for (int i = 1; i < W; ++i) r = fmaxf(r, red[i]);
-    __syncthreads();
+    for (int i = 1; i < W; ++i) r = fmaxf(r, red[turn & 1][i]);
     return r;
 }
 
-// A lane's part of a row of d elements in W wavefronts: up to NV runs of 16 bytes' worth, 64 W runs apart, and one of the d % E
-// elements behind the whole runs.  What a lane has no part in is zero.
-template <typename T, int NV> struct RowPart { float v[NV][wide_of<T>()], t; };
+// A lane's part of a row of d elements in W wavefronts, as it lies in memory: up to NV runs of 16 bytes, 64 W runs apart, and one of
+// the d % E elements behind the whole runs.  A lane without a run loads the last one again, without a branch, and its part is left out
+// where it would count: its weight is zero, its square is not added, nothing of it is stored.
+template <typename T, int NV> struct Row {
+    typename Wide<T, wide_of<T>()>::vec v[NV > 0 ? NV : 1];
+    T t;
+};
+// and in fp32.  NV = 0: rows shorter than a run, d < E.
+template <typename T, int NV> struct RowPart { float v[NV > 0 ? NV : 1][wide_of<T>()], t; };
 
 template <typename T, int W, int NV, bool NT>
-__device__ __forceinline__ void load_row(const T *p, int lane, int d, RowPart<T, NV> &r)
+__device__ __forceinline__ void load_row(const T *p, int lane, int d, Row<T, NV> &r)
 {
     constexpr int E = wide_of<T>();
-    const int runs = d / E, rest = d - runs * E;
+    typedef typename Wide<T, E>::vec V;
+    const int runs = d / E;
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
-        const int i = lane + c * 64 * W;
-#pragma unroll
-        for (int u = 0; u < E; ++u) r.v[c][u] = 0.f;
-        if (i < runs) load_wide<T, E, NT>(p + i * E, r.v[c]);
+        const V *const at = (const V *)behind(p, (uint32_t)min(lane + c * 64 * W, runs - 1) * 16);
+        r.v[c] = NT ? __builtin_nontemporal_load(at) : *at;
     }
-    r.t = lane < rest ? (float)p[runs * E + lane] : 0.f;
+    r.t = *behind(p, (uint32_t)min(runs * E + lane, d - 1) * (uint32_t)sizeof(T));
+}
+// Has the compiler forget what it made of a row: it is converted again where it is used again, instead of being held in fp32
+template <typename T, int NV>
+__device__ __forceinline__ void as_in_memory(Row<T, NV> &r)
+{
+    typedef int I4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        I4 x = __builtin_bit_cast(I4, r.v[c]);
+        asm volatile("" : "+v"(x));
+        r.v[c] = __builtin_bit_cast(typename Wide<T, wide_of<T>()>::vec, x);
+    }
 }
 template <typename T, int W, int NV, bool NT>
 __device__ __forceinline__ void store_row(T *p, int lane, int d, const RowPart<T, NV> &r)
@@ -78,7 +94,7 @@ __device__ __forceinline__ void store_row(T *p, int lane, int d, const RowPart<T
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
         const int i = lane + c * 64 * W;
-        if (i < runs) store_wide<T, E, NT>(p + i * E, r.v[c]);
+        if (i < runs) store_wide<T, E, NT>(behind(p, (uint32_t)i * 16), r.v[c]);
     }
     if (lane < rest) p[runs * E + lane] = (T)r.t;
 }
@@ -97,7 +113,7 @@ __device__ __forceinline__ void load_words(const float *p, int lane, int d, RowP
 #pragma unroll
             for (int q = 0; q < E; q += 4) {
                 float f[4];
-                load_wide<float, 4, false>(p + i * E + q, f);
+                load_wide<float, 4, false>(behind(p, (uint32_t)(i * E + q) * 4), f);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) r.v[c][q + u] = f[u];
             }
@@ -117,59 +133,67 @@ __device__ __forceinline__ void store_words(float *p, int lane, int d, const Row
 #pragma unroll
             for (int q = 0; q < E; q += 4) {
                 const float f[4] = {r.v[c][q], r.v[c][q + 1], r.v[c][q + 2], r.v[c][q + 3]};
-                store_wide<float, 4, false>(p + i * E + q, f);
+                store_wide<float, 4, false>(behind(p, (uint32_t)(i * E + q) * 4), f);
             }
         }
     }
     if (lane < rest) p[runs * E + lane] = r.t;
 }
-// f(element of a, element of b) for all of them
-template <typename T, int NV, typename F>
-__device__ __forceinline__ void each(RowPart<T, NV> &a, RowPart<T, NV> &b, F f)
+// f(element of a, the same element of b, c, ...) for all of them
+template <typename T, int NV, int W = 0> __device__ __forceinline__ float &at(RowPart<T, NV> &r, int c, int u) { return c < NV ? r.v[c][u] : r.t; }
+template <typename T, int NV, int W = 0> __device__ __forceinline__ float at(const Row<T, NV> &r, int c, int u) { return (float)(c < NV ? r.v[c][u] : r.t); }
+template <typename T, int NV, typename F, typename... R>
+__device__ __forceinline__ void each(F f, R &...r)
 {
 #pragma unroll
-    for (int c = 0; c < NV; ++c)
+    for (int c = 0; c <= NV; ++c)
 #pragma unroll
-        for (int u = 0; u < wide_of<T>(); ++u) f(a.v[c][u], b.v[c][u]);
-    f(a.t, b.t);
+        for (int u = 0; u < (c < NV ? wide_of<T>() : 1); ++u) f(at<T, NV>(r, c, u)...);
 }
 
 // W wavefronts to a row, a workgroup of one row (W > 1) or of four (W == 1)
 template <int W> constexpr int rms_threads() { return W == 1 ? 256 : 64 * W; }
 
 template <typename T, int W, int NV, bool FP8>
-__device__ __forceinline__ void rmsnorm_row(const RmsArgs &a, int k, long long row, int lane, float *red)
+__device__ __forceinline__ void rmsnorm_row(const RmsArgs &a, int k, long long row, int lane, float (*red)[W])
 {
     constexpr int E = wide_of<T>();
+    Row<T, NV> x, res;
     RowPart<T, NV> s, w;
-    load_row<T, W, NV, true>((const T *)a.x + row * a.s_x, lane, a.d, s);
-    if (a.res != nullptr) {
-        load_row<T, W, NV, true>((const T *)a.res + row * a.s_res, lane, a.d, w);
-        each(s, w, [](float &x, float &r) { x += r; });
-    }
+    load_row<T, W, NV, true>((const T *)a.x + row * a.s_x, lane, a.d, x);
+    if (a.res != nullptr) load_row<T, W, NV, true>((const T *)a.res + row * a.s_res, lane, a.d, res);
     load_words<T, W, NV>(a.w + (long long)k * a.d, lane, a.d, w);
+    each<T, NV>([](float &y, float v) { y = v; }, s, x);
+    if (a.res != nullptr) each<T, NV>([](float &y, float v) { y += v; }, s, res);
     float q = 0.f;
-    each(s, w, [&](float &x, float &) { q = fmaf(x, x, q); });
+    const int runs = a.d / E, rest = a.d - runs * E;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        float part = 0.f;
+#pragma unroll
+        for (int u = 0; u < E; ++u) part = fmaf(s.v[c][u], s.v[c][u], part);
+        q += lane + c * 64 * W < runs ? part : 0.f;
+    }
+    q += lane < rest ? s.t * s.t : 0.f;
     if (a.sum != nullptr) store_row<T, W, NV, false>((T *)a.sum + row * a.s_sum, lane, a.d, s);
-    const float rstd = 1.f / sqrtf(group_sum<W>(q, red) / (float)a.d + a.eps);
+    const float rstd = 1.f / sqrtf(group_sum<W>(q, red, 0) / (float)a.d + a.eps);
     if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
     float top = 0.f;
-    each(s, w, [&](float &x, float &wx) {
-        x = x * rstd * wx;
-        if (FP8 && fabsf(x) < INFINITY) top = fmaxf(top, fabsf(x));
-    });
+    each<T, NV>([&](float &y, float &f) {
+        y = y * rstd * f;
+        if (FP8 && fabsf(y) < INFINITY) top = fmaxf(top, fabsf(y));
+    }, s, w);
     if (!FP8) {
         store_row<T, W, NV, false>((T *)a.y + row * a.s_y, lane, a.d, s);
         return;
     }
-    top = group_max<W>(top, red);
+    top = group_max<W>(top, red, 1);
     const float scale = top >= 1e-35f ? top * (1.f / E4M3_MAX) : 0.f;      // less would leave the range of floats
     if (lane == 0) a.scale[row] = scale;
     const float f = scale > 0.f ? 1.f / scale : 0.f;
     // a rounding above 448 at most, which still becomes 448; what is not finite becomes NaN
-    each(s, w, [&](float &x, float &) { x *= f; });
+    each<T, NV>([&](float &y) { y *= f; }, s);
     uint8_t *const y = (uint8_t *)a.y + row * a.s_y;
-    const int runs = a.d / E, rest = a.d - runs * E;
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
         const int i = lane + c * 64 * W;
@@ -180,7 +204,7 @@ __device__ __forceinline__ void rmsnorm_row(const RmsArgs &a, int k, long long r
         Codes out;
 #pragma unroll
         for (int u = 0; u < E; ++u) out[u] = code.b[u];
-        if (i < runs) *(Codes *)(y + i * E) = out;
+        if (i < runs) *(Codes *)behind(y, (uint32_t)i * E) = out;
     }
     if (lane < rest) {
         const float one[4] = {s.t, 0.f, 0.f, 0.f};
@@ -191,11 +215,13 @@ __device__ __forceinline__ void rmsnorm_row(const RmsArgs &a, int k, long long r
 template <typename T, int W, int NV, bool FP8>
 __global__ __launch_bounds__(rms_threads<W>()) void rmsnorm_kernel(RmsArgs a)
 {
-    __shared__ float red[W];
+    __shared__ float red[2][W];
     const int k = blockIdx.y, lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-    const int side = W == 1 ? 4 : 1, at = W == 1 ? threadIdx.x >> 6 : 0;
-    for (long long r = (long long)blockIdx.x * side + at; r < a.rows; r += (long long)gridDim.x * side)
+    const int side = W == 1 ? 4 : 1, place = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;   // the same in a wavefront
+    for (long long r = (long long)blockIdx.x * side + place; r < a.rows; r += (long long)gridDim.x * side) {
+        if (W > 1 && !FP8 && r >= gridDim.x) __syncthreads();          // one set of words a row: it is read before it is written again
         rmsnorm_row<T, W, NV, FP8>(a, k, k * a.rows + r, lane, red);
+    }
 }
 
 struct RmsBackArgs {
@@ -209,78 +235,95 @@ struct RmsBackArgs {
 };
 
 // A workgroup takes every gridDim.x-th row (W == 1: four of them at a time) and keeps its part of the weight's gradient in registers.
+// The next row's loads are under way, as they lie in memory, while a row is worked on, where that fits the registers of four wavefronts
+// to a SIMD: w, dw and two rows of three arrays.
 template <typename T, int W, int NV>
-__global__ __launch_bounds__(rms_threads<W>()) void rmsnorm_back_kernel(RmsBackArgs a)
+__global__ __launch_bounds__(rms_threads<W>(), 4) void rmsnorm_back_kernel(RmsBackArgs a)
 {
     constexpr int E = wide_of<T>();
-    __shared__ float red[W];
+    constexpr bool AHEAD = W < 16 && NV * (2 * E + 3 * 2 * 4) <= 40;
+    __shared__ float red[2][W];
     __shared__ float side_dw[W == 1 ? 3 * 64 * (NV * E + 1) : 1];
     const int k = blockIdx.y, lane = W == 1 ? threadIdx.x & 63 : threadIdx.x;
-    const int side = W == 1 ? 4 : 1, at = W == 1 ? threadIdx.x >> 6 : 0;
+    const int side = W == 1 ? 4 : 1, place = W == 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;   // the same in a wavefront
+    const long long step = (long long)gridDim.x * side, last = (k + 1) * a.rows;
     RowPart<T, NV> w, dw;
     load_words<T, W, NV>(a.w + (long long)k * a.d, lane, a.d, w);
-    each(dw, w, [](float &x, float &) { x = 0.f; });
-    for (long long r = (long long)blockIdx.x * side + at; r < a.rows; r += (long long)gridDim.x * side) {
-        const long long row = k * a.rows + r;
-        RowPart<T, NV> g, h, e;
+    each<T, NV>([](float &x) { x = 0.f; }, dw);
+    Row<T, NV> g, h, e = {};
+    float rstd = 0.f;
+    auto load = [&](long long row) {
         load_row<T, W, NV, true>((const T *)a.dy + row * a.s_dy, lane, a.d, g);
         load_row<T, W, NV, true>((const T *)a.h + row * a.s_h, lane, a.d, h);
         if (a.dres != nullptr) load_row<T, W, NV, true>((const T *)a.dres + row * a.s_dres, lane, a.d, e);
-        else each(e, e, [](float &x, float &) { x = 0.f; });
-        const float rstd = a.rstd[row];
-        each(h, h, [&](float &x, float &) { x *= rstd; });
+        rstd = a.rstd[row];
+    };
+    long long row = k * a.rows + (long long)blockIdx.x * side + place;
+    if (row < last) load(row);
+#pragma unroll 1
+    for (int turn = 0; row < last; row += step, ++turn) {
+        Row<T, NV> g0 = g, h0 = h, e0 = e;
+        const float rs = rstd;
+        if (AHEAD) load(min(row + step, last - 1));
         float q = 0.f;
+        each<T, NV>([&](float &acc, float f, float y, float x) {
+            const float n = x * rs;
+            acc = fmaf(y, n, acc);
+            q = fmaf(y * f, n, q);
+        }, dw, w, g0, h0);
+        const float mean = group_sum<W>(q, red, turn) / (float)a.d;
+        as_in_memory(g0);
+        as_in_memory(h0);
+        auto dx = [&](float f, float y, float x, float z) { return fmaf(rs, fmaf(-(x * rs), mean, y * f), z); };
+        T *const to = (T *)a.dx + row * a.s_dx;
+        const int runs = a.d / E, rest = a.d - runs * E;
 #pragma unroll
-        for (int c = 0; c < NV; ++c)
+        for (int c = 0; c < NV; ++c) {
+            float v[E];
 #pragma unroll
-            for (int u = 0; u < wide_of<T>(); ++u) {
-                dw.v[c][u] = fmaf(g.v[c][u], h.v[c][u], dw.v[c][u]);
-                g.v[c][u] *= w.v[c][u];
-                q = fmaf(g.v[c][u], h.v[c][u], q);
-            }
-        dw.t = fmaf(g.t, h.t, dw.t);
-        g.t *= w.t;
-        q = fmaf(g.t, h.t, q);
-        const float mean = group_sum<W>(q, red) / (float)a.d;
-        each(g, h, [&](float &x, float &n) { x = rstd * fmaf(-n, mean, x); });
-        each(g, e, [&](float &x, float &y) { x += y; });
-        store_row<T, W, NV, true>((T *)a.dx + row * a.s_dx, lane, a.d, g);
+            for (int u = 0; u < E; ++u) v[u] = dx(w.v[c][u], (float)g0.v[c][u], (float)h0.v[c][u], (float)e0.v[c][u]);
+            const int i = lane + c * 64 * W;
+            if (i < runs) store_wide<T, E, true>(behind(to, (uint32_t)i * 16), v);
+        }
+        if (lane < rest) to[runs * E + lane] = (T)dx(w.t, (float)g0.t, (float)h0.t, (float)e0.t);
+        if (!AHEAD && row + step < last) load(row + step);
     }
     if (W == 1) {                              // the four wavefronts' sums become one, in their order
-        float *const mine = side_dw + ((at - 1) * 64 + lane) * (NV * E + 1);
+        float *const mine = side_dw + (place > 0 ? place - 1 : 0) * 64 * (NV * E + 1) + lane * (NV * E + 1);
         int n = 0;
-        if (at > 0) each(dw, w, [&](float &x, float &) { mine[n++] = x; });
+        if (place > 0) each<T, NV>([&](float &x) { mine[n++] = x; }, dw);
         __syncthreads();
-        if (at > 0) return;
+        if (place > 0) return;
 #pragma unroll
         for (int o = 0; o < 3; ++o) {
             const float *const other = side_dw + (o * 64 + lane) * (NV * E + 1);
             n = 0;
-            each(dw, w, [&](float &x, float &) { x += other[n++]; });
+            each<T, NV>([&](float &x) { x += other[n++]; }, dw);
         }
     }
     store_words<T, W, NV>(a.partial + ((long long)k * gridDim.x + blockIdx.x) * a.d, lane, a.d, dw);
 }
 
-// dw[k][j] = sum over the parts: 32 columns and 8 runs of parts, four of each in flight, to a workgroup; a fixed order
-__global__ __launch_bounds__(256) void rmsnorm_weight_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dw)
+// dw[k][j] = sum over the parts: 32 columns and 32 runs of parts, four of each in flight, to a workgroup; a fixed order
+constexpr int SUM_RUNS = 32;
+__global__ __launch_bounds__(32 * SUM_RUNS) void rmsnorm_weight_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dw)
 {
-    __shared__ float red[8][32];
+    __shared__ float red[SUM_RUNS][33];
     const int k = blockIdx.y, col = threadIdx.x & 31, run = threadIdx.x >> 5;
     const int j = blockIdx.x * 32 + col;
     const float *p = partial + (long long)k * parts * d + j;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (j < d)
-        for (int i = run; i < parts; i += 32)
+        for (int i = run; i < parts; i += 4 * SUM_RUNS)
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (i + u * 8 < parts) s[u] += p[(long long)(i + u * 8) * d];
+                if (i + u * SUM_RUNS < parts) s[u] += p[(long long)(i + u * SUM_RUNS) * d];
     red[run][col] = (s[0] + s[1]) + (s[2] + s[3]);
     __syncthreads();
     if (run != 0 || j >= d) return;
     float sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) sum += red[i][col];
+    for (int i = 0; i < SUM_RUNS; ++i) sum += red[i][col];
     dw[(long long)k * d + j] = sum;
 }
 
@@ -296,16 +339,19 @@ static long long fwd_groups(long long rows, int W)
 static long long back_groups(int K, long long rows, int W)
 {
     const long long side = W == 1 ? 4 : 1;
-    long long most = (1024 + K - 1) / K;
+    const long long all = 4096 / (W == 1 ? 4 : W);           // four wavefronts to a SIMD
+    long long most = (all + K - 1) / K;
     const long long need = (rows + side - 1) / side;
     if (most > need) most = need;
     return most < 1 ? 1 : most;
 }
 
-// Wavefronts of a row, and runs of a lane: eight or sixteen elements to a lane
+// Wavefronts of a row, and runs of a lane: eight or sixteen elements to a lane.  Sixteen on half the wavefronts are faster than eight
+// where both would do: 16384 rows of 4096 (to e4m3) 77.7 against 88 us, 8 x 12608 rows of 768 forward and backward 207 against 229.
 #define RMS_BY_WIDTH(T, d, F) do { constexpr int E_ = wide_of<T>(); \
-    if ((d) <= 512) F(T, 1, 8 / E_); else if ((d) <= 1024) F(T, 1, 16 / E_); else if ((d) <= 2048) F(T, 4, 8 / E_); \
-    else if ((d) <= 4096) F(T, 4, 16 / E_); else if ((d) <= 8192) F(T, 8, 16 / E_); else F(T, 16, 16 / E_); } while (0)
+    if ((d) < E_) F(T, 1, 0); else if ((d) <= 512) F(T, 1, 8 / E_); else if ((d) <= 1024) F(T, 1, 16 / E_); \
+    else if ((d) <= 2048) F(T, 4, 8 / E_); else if ((d) <= 4096) F(T, 4, 16 / E_); else if ((d) <= 8192) F(T, 8, 16 / E_); \
+    else F(T, 16, 16 / E_); } while (0)
 static int rms_waves(long long d) { return d <= 1024 ? 1 : d <= 4096 ? 4 : d <= 8192 ? 8 : 16; }
 
 template <typename T>
@@ -329,7 +375,7 @@ static hipError_t launch_rms_back(const RmsBackArgs &a, int K, float *dw, hipStr
 #undef RMS_BACK
     hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
-    rmsnorm_weight_kernel<<<dim3((unsigned)((a.d + 31) / 32), (unsigned)K), 256, 0, s>>>(a.partial, (int)groups, a.d, dw);
+    rmsnorm_weight_kernel<<<dim3((unsigned)((a.d + 31) / 32), (unsigned)K), 32 * SUM_RUNS, 0, s>>>(a.partial, (int)groups, a.d, dw);
     return hipGetLastError();
 }
 
