@@ -7,13 +7,13 @@
 // A row that is masked as a whole (all -inf) has lse = logp = -inf, H = 0 and no gradient.  A token outside 0..V-1 stands for none:
 // logp = 0 and no gradient from it.
 //
-// One pass over the logits: every lane keeps the largest logit m it has seen, s = sum e^((x - m)/T) and w = sum of t e^.. with
-// t = (x - m)/T in units of log 2, rescaled where m grows; H = ln 2 (log2 s - w / s).  m starts at the lowest float, not at -inf,
-// so that masked entries (x - m = -inf) are zeros and never NaN.  x - m is taken before the scaling: one product-sum with a rounded
-// m / T would shift all exponents of a row by its rounding.
-// Alternatives without a second pass: a lane also keeps its largest logit and where it was.  The `top` largest of these lane
-// maxima are a bound: nothing below the last of them is an alternative, and the only lanes with anything above it are their owners.
-// Those `top` lanes' logits alone are read again, from the caches.
+// One pass over the logits: every lane keeps the largest logit m it has seen, s = sum 2^t and w = sum t 2^t with t = (x - m) c,
+// c = log2 e / T, rescaled where m grows; H = ln 2 (log2 s - w / s).  m starts at the lowest float, not at -inf, so that masked entries
+// (t = -inf) are zeros and never NaN.  x - m is taken before the scaling: c x - c m in one product-sum would shift the row by the
+// rounding of c m, and a token that is certain would not have logp = H = 0.  Four wide loads of a lane are in flight and share one
+// comparison with m.
+// Alternatives without a second pass over the row: a lane's largest logit is at hand, and the few lanes that can hold alternatives have
+// their logits looked at again, from the caches (find_top).
 #include <cmath>
 
 #include "qsr_internal.h"
@@ -23,7 +23,6 @@ namespace qsr {
 
 constexpr float LOWEST = -3.402823466e38f, LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 constexpr int LP_MAX_TOP = 64;                 // alternatives: the lanes of a wavefront
-constexpr int LP_LIST = 1024;                  // logits above the bound that fit LDS
 
 // A logit and its place as one number that orders them: the larger logit, then the lower index, is larger.  NaN counts as -inf;
 // 0 is smaller than any.
@@ -44,25 +43,35 @@ __device__ __forceinline__ uint64_t key_xor(uint64_t v, int o)
     return ((uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, 64) << 32) | (uint32_t)__shfl_xor((int)(uint32_t)v, o, 64);
 }
 
+// w + t 2^t, where 2^t is e; of masked entries 0 and not 0 * -inf (2^-1000 is 0 already)
+__device__ __forceinline__ float add_part(float w, float t, float e) { return fmaf(e, fmaxf(t, -1000.f), w); }
+// m: the largest logit (the lowest float at least); s, w: see above
 struct Stat { float m, s, w; };
-__device__ __forceinline__ void merge(Stat &a, const Stat &b, float c)
+__device__ __forceinline__ void rescale(Stat &a, float m, float c)
 {
-    const float m = fmaxf(a.m, b.m);
-    // no further down than 2^-1000: a sum of zeros times -inf would be NaN
-    const float da = fmaxf((a.m - m) * c, -1000.f), db = fmaxf((b.m - m) * c, -1000.f);
-    const float fa = __builtin_amdgcn_exp2f(da), fb = __builtin_amdgcn_exp2f(db);
-    const float s = fa * a.s + fb * b.s;
-    a.w = fa * fmaf(da, a.s, a.w) + fb * fmaf(db, b.s, b.w);
-    a.s = s; a.m = m;
+    const float d = fmaxf((a.m - m) * c, -1000.f), f = __builtin_amdgcn_exp2f(d);
+    a.w = f * fmaf(d, a.s, a.w);
+    a.s *= f;
+    a.m = m;
 }
 __device__ __forceinline__ Stat wave_merge(Stat a, float c)
 {
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) {
-        const Stat b = {__shfl_xor(a.m, o, 64), __shfl_xor(a.s, o, 64), __shfl_xor(a.w, o, 64)};
-        merge(a, b, c);
-    }
+    rescale(a, wave_max(a.m), c);
+    a.s = wave_sum(a.s);
+    a.w = wave_sum(a.w);
     return a;
+}
+template <int W>
+__device__ __forceinline__ Stat merge_all(const Stat *p, float c)
+{
+    Stat a[W], r;
+    float m = p[0].m;
+#pragma unroll
+    for (int i = 0; i < W; ++i) { a[i] = p[i]; m = fmaxf(m, a[i].m); }
+    r = {m, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < W; ++i) { rescale(a[i], m, c); r.s += a[i].s; r.w += a[i].w; }
+    return r;
 }
 
 struct LpArgs {
@@ -77,23 +86,27 @@ struct LpArgs {
     uint64_t *keys;                            // [rows][splits][top]
 };
 
-// Log probabilities are taken from x - m: lse alone, as a float, has lost log s where the logits are large (a row of masks of the
-// lowest value has p = 1/V like any row of equal logits).  For the same reason `stats` keeps m and log s for the backward pass.
-__device__ __forceinline__ float lp_of(const LpArgs &a, const Stat &st, float x)
+// What a row's sums come to: ls = log sum e^((x - m)/T).  Log probabilities are taken from x - m: lse alone, as a float, has lost ls
+// where the logits are large (a row of masks of the lowest value has p = 1/V like any row of equal logits).  For the same reason
+// `stats` keeps m and ls for the backward pass.
+struct Done { float m, ls, entropy; bool empty; };
+__device__ __forceinline__ Done lp_done(const Stat &st)
 {
-    return st.s == 0.f ? -INFINITY : fmaf(-LN2, __log2f(st.s), (x - st.m) * a.inv_t);
+    const float l2 = __log2f(st.s);
+    Done r;
+    r.m = st.m;
+    r.empty = st.s == 0.f;
+    r.ls = r.empty ? -INFINITY : LN2 * l2;
+    r.entropy = r.empty ? 0.f : LN2 * (l2 - st.w / st.s);
+    return r;
 }
-__device__ __forceinline__ void lp_result(const LpArgs &a, long long row, const Stat &st)
+__device__ __forceinline__ float lp_of(const LpArgs &a, const Done &r, float x)
 {
-    const float ls = LN2 * __log2f(st.s);
-    const bool empty = st.s == 0.f;
-    if (a.lse != nullptr) a.lse[row] = empty ? -INFINITY : fmaf(st.m, a.inv_t, ls);
-    if (a.stats != nullptr) { a.stats[2 * row] = st.m; a.stats[2 * row + 1] = ls; }
-    if (a.entropy != nullptr) a.entropy[row] = empty ? 0.f : fmaf(-LN2, st.w / st.s, ls);
+    return r.empty ? -INFINITY : fmaf(x - r.m, a.inv_t, -r.ls);
 }
-__device__ __forceinline__ void lp_alternative(const LpArgs &a, long long row, int place, uint64_t key, const Stat &st)
+__device__ __forceinline__ void lp_alternative(const LpArgs &a, long long row, int place, uint64_t key, const Done &r)
 {
-    a.top_logp[row * a.top + place] = lp_of(a, st, key_value(key));
+    a.top_logp[row * a.top + place] = lp_of(a, r, key_value(key));
     a.top_id[row * a.top + place] = (int32_t)key_index(key);
 }
 __device__ __forceinline__ long long lp_token(const LpArgs &a, long long row)
@@ -102,12 +115,14 @@ __device__ __forceinline__ long long lp_token(const LpArgs &a, long long row)
     return t >= 0 && t < a.V ? t : -1;
 }
 template <typename T>
-__device__ __forceinline__ void lp_row(const LpArgs &a, long long row, const Stat &st)
+__device__ __forceinline__ void lp_row(const LpArgs &a, long long row, const Done &r)
 {
-    lp_result(a, row, st);
+    if (a.lse != nullptr) a.lse[row] = r.empty ? -INFINITY : fmaf(r.m, a.inv_t, r.ls);
+    if (a.stats != nullptr) { a.stats[2 * row] = r.m; a.stats[2 * row + 1] = r.ls; }
+    if (a.entropy != nullptr) a.entropy[row] = r.entropy;
     if (a.logp == nullptr) return;
     const long long token = lp_token(a, row);
-    a.logp[row] = token < 0 ? 0.f : lp_of(a, st, (float)((const T *)a.x)[row * a.stride + token]);
+    a.logp[row] = token < 0 ? 0.f : lp_of(a, r, (float)((const T *)a.x)[row * a.stride + token]);
 }
 
 // The runs of a split: `head` elements up to the first 16-byte boundary, whole runs, and what is left.  Lane i takes head element i,
@@ -124,160 +139,176 @@ __device__ __forceinline__ Runs runs_of(const T *p, int count)
     return r;
 }
 
-// The `top` largest keys among n in LDS, by counting how many are larger, to out[0..top) in LDS.  Keys other than 0 differ.
-template <int THREADS>
-__device__ __forceinline__ void rank_keys(const uint64_t *in, int n, int top, uint64_t *out)
+// A part of a row in a workgroup's hands: where it begins in the row, its runs, and the LDS words of the search for alternatives
+template <typename T> struct Part { const T *p, *body, *rest; int j0, count; Runs q; };
+template <int THREADS> struct Search {
+    float group[64];                           // the largest logit of each of 64 groups of lanes
+    unsigned short owner[THREADS];
+    static constexpr int LIST = THREADS > 64 ? 1024 : 256;                     // logits from the bound on that fit
+    uint64_t list[LIST], best[LP_MAX_TOP];
+    int owners, listed;
+};
+template <int G> __device__ __forceinline__ float group_most(float v)
 {
-    for (int i = threadIdx.x; i < n; i += THREADS) {
-        const uint64_t key = in[i];
-        int rank = 0;
-        for (int j = 0; j < n; ++j) rank += in[j] > key ? 1 : 0;
-        if (rank < top && key != 0) out[rank] = key;
-    }
+    if (G >= 2) v = fmaxf(v, row_step<0>(v));
+    if (G >= 4) v = fmaxf(v, row_step<1>(v));
+    if (G >= 8) v = fmaxf(v, row_step<2>(v));
+    return v;
 }
 
-// One workgroup to a split of a row.  best: the top largest keys of the split (0 where there are fewer elements).
-template <typename T, int THREADS, bool TOP>
-__global__ __launch_bounds__(THREADS) void token_logprobs_kernel(LpArgs a)
+// The `top` largest keys of a part to se.best, 0 where it has fewer elements.  mine: the lane's largest logit.
+// The `top`-th largest of 64 groups' maxima is a bound: that many logits reach it, and only lanes whose own maximum does have any that
+// do.  Their logits alone are looked at again, shared out among all lanes, and those from the bound on are put in order.  Entries of
+// -inf are below any bound; where too few others are there, the first of them follow.
+template <typename T, int THREADS>
+__device__ __forceinline__ void find_top(const Part<T> &a, float mine, int top, Search<THREADS> &se)
 {
-    constexpr int E = wide_of<T>(), W = THREADS / 64;
+    constexpr int E = wide_of<T>(), G = THREADS / 64;
+    const int tid = threadIdx.x, lane = tid & 63;
+    const float most = group_most<G>(mine);
+    if (tid % G == 0) se.group[tid / G] = most;
+    if (tid < top) se.best[tid] = 0;
+    if (tid == 0) se.owners = se.listed = 0;
+    __syncthreads();
+    const float group = se.group[lane];
+    int above = 0;
+#pragma unroll
+    for (int i = 0; i < 64; ++i) above += lane_of(group, i) > group ? 1 : 0;
+    const float bound = -wave_max(above < top ? -group : -INFINITY);               // the lowest float at least
+    if (mine >= bound) se.owner[atomicAdd(&se.owners, 1)] = (unsigned short)tid;
+    __syncthreads();
+    const int cols = (a.q.n + THREADS - 1) / THREADS + 2;                      // a lane's runs, and its elements of head and rest
+    const int items = cols * se.owners;
+    auto add = [&](float x, int j) {
+        if (x >= bound) {
+            const int slot = atomicAdd(&se.listed, 1);
+            if (slot < se.LIST) se.list[slot] = lp_key(x, a.j0 + j);
+        }
+    };
+    for (int i = tid; i < items; i += THREADS) {
+        const int owner = se.owner[i / cols], col = i % cols, run = (col - 1) * THREADS + owner;
+        if (col == 0) { if (owner < a.q.head) add((float)a.p[owner], owner); }
+        else if (col == cols - 1) { if (owner < a.q.tail) add((float)a.rest[owner], a.q.head + a.q.n * E + owner); }
+        else if (run < a.q.n) {
+            float x[E];
+            load_wide<T, E, false>(a.body + (long long)run * E, x);
+#pragma unroll
+            for (int u = 0; u < E; ++u) add(x[u], a.q.head + run * E + u);
+        }
+    }
+    __syncthreads();
+    const int n = se.listed;
+    if (n <= se.LIST) {
+        for (int i = tid; i < n; i += THREADS) {
+            const uint64_t key = se.list[i];
+            int rank = 0;
+            for (int j = 0; j < n; ++j) rank += se.list[j] > key ? 1 : 0;
+            if (rank < top) se.best[rank] = key;
+        }
+        if (n < top && tid < 64)               // masked entries (and NaN): at most n of the first n + top are others
+            for (int j0 = 0, have = n; j0 < a.count && have < top; j0 += 64) {
+                const int j = j0 + lane;
+                const float x = j < a.count ? (float)a.p[j] : 0.f;
+                const bool masked = j < a.count && !(x > -INFINITY);
+                const uint64_t mask = __ballot(masked);
+                const int place = have + __popcll(mask & ((1ull << lane) - 1));
+                if (masked && place < top) se.best[place] = lp_key(x, a.j0 + j);
+                have += __popcll(mask);
+            }
+    } else {
+        // many equal ones: one after the other, each the largest key below the one before
+        uint64_t last = ~0ull;
+        for (int place = 0; place < top; ++place) {
+            uint64_t key = 0;
+            for (int j = tid; j < a.count; j += THREADS) {
+                const uint64_t other = lp_key((float)a.p[j], a.j0 + j);
+                if (other < last && other > key) key = other;
+            }
+#pragma unroll
+            for (int o = 32; o > 0; o >>= 1) { const uint64_t other = key_xor(key, o); key = other > key ? other : key; }
+            __syncthreads();
+            if (lane == 0) se.list[tid >> 6] = key;
+            __syncthreads();
+            for (int i = 0; i < THREADS / 64; ++i) key = se.list[i] > key ? se.list[i] : key;
+            if (tid == 0) se.best[place] = key;
+            last = key;
+        }
+    }
+    __syncthreads();
+}
+
+// One workgroup to a split of a row
+template <typename T, int THREADS, bool TOP>
+__global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
+{
+    constexpr int E = wide_of<T>(), W = THREADS / 64, U = 4;
     __shared__ Stat red[W];
-    __shared__ uint64_t cand[TOP ? W * LP_MAX_TOP : 1], list[TOP ? LP_LIST : 1], best[TOP ? LP_MAX_TOP : 1];
-    __shared__ int listed;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ Search<TOP ? THREADS : 1> se;
+    const int tid = threadIdx.x;
     const float c = a.inv_t * LOG2E;
-    const int j0 = blockIdx.x * a.part, count = min(a.V - j0, a.part);
     for (long long row = blockIdx.y; row < a.rows; row += gridDim.y) {
-        const T *const p = (const T *)a.x + row * a.stride + j0;
-        const Runs q = runs_of(p, count);
-        const T *const body = p + q.head, *const rest = body + q.n * E;
+        Part<T> part;
+        part.j0 = blockIdx.x * a.part;
+        part.count = min(a.V - part.j0, a.part);
+        part.p = (const T *)a.x + row * a.stride + part.j0;
+        const Runs q = part.q = runs_of(part.p, part.count);
+        part.body = part.p + q.head;
+        part.rest = part.body + q.n * E;
         Stat st = {LOWEST, 0.f, 0.f};
-        float big = -INFINITY;
-        int big_at = -1;                       // -1: head, run, n: rest
-        bool any = false;
-        auto take = [&](float x, int at) {
-            if (x > st.m) { const Stat one = {x, 0.f, 0.f}; merge(st, one, c); }
+        auto seen = [&](float top) {
+            if (top > st.m) rescale(st, top, c);
+        };
+        auto take = [&](float x) {
             const float t = (x - st.m) * c, e = __builtin_amdgcn_exp2f(t);
             st.s += e;
-            st.w = fmaf(e, fmaxf(t, -1000.f), st.w);
-            if (TOP && (!any || x > big)) { big = fmaxf(x, -INFINITY); big_at = at; any = true; }     // (NaN: -inf)
+            st.w = add_part(st.w, t, e);
         };
-        if (tid < q.head) take((float)p[tid], -1);
-        for (int i = tid; i < q.n; i += THREADS) {
+        if (tid < q.head) { seen((float)part.p[tid]); take((float)part.p[tid]); }
+        int i = tid;
+        for (; i + (U - 1) * THREADS < q.n; i += U * THREADS) {
+            float x[U][E];
+#pragma unroll
+            for (int v = 0; v < U; ++v) load_wide<T, E, false>(part.body + (long long)(i + v * THREADS) * E, x[v]);
+            float top = x[0][0];
+#pragma unroll
+            for (int v = 0; v < U; ++v)
+#pragma unroll
+                for (int u = 0; u < E; ++u) top = fmaxf(top, x[v][u]);
+            seen(top);
+#pragma unroll
+            for (int v = 0; v < U; ++v)
+#pragma unroll
+                for (int u = 0; u < E; ++u) take(x[v][u]);
+        }
+        for (; i < q.n; i += THREADS) {
             float x[E];
-            load_wide<T, E, false>(body + (long long)i * E, x);
+            load_wide<T, E, false>(part.body + (long long)i * E, x);
             float top = x[0];
 #pragma unroll
             for (int u = 1; u < E; ++u) top = fmaxf(top, x[u]);
-            if (top > st.m) { const Stat one = {top, 0.f, 0.f}; merge(st, one, c); }
+            seen(top);
 #pragma unroll
-            for (int u = 0; u < E; ++u) {
-                const float t = (x[u] - st.m) * c, e = __builtin_amdgcn_exp2f(t);
-                st.s += e;
-                st.w = fmaf(e, fmaxf(t, -1000.f), st.w);
-            }
-            if (TOP && (!any || top > big)) { big = fmaxf(top, -INFINITY); big_at = i; any = true; }
+            for (int u = 0; u < E; ++u) take(x[u]);
         }
-        if (tid < q.tail) take((float)rest[tid], q.n);
+        if (tid < q.tail) { seen((float)part.rest[tid]); take((float)part.rest[tid]); }
+        const float mine = st.m;
         st = wave_merge(st, c);
         if (W > 1) {
-            if (lane == 0) red[wave] = st;
+            if ((tid & 63) == 0) red[tid >> 6] = st;
             __syncthreads();
-            st = red[0];
-#pragma unroll
-            for (int i = 1; i < W; ++i) merge(st, red[i], c);
+            st = merge_all<W>(red, c);
         }
         const bool alone = a.splits == 1;
-        if (tid == 0) {
-            if (alone) lp_row<T>(a, row, st);
-            else a.parts[row * a.splits + blockIdx.x] = st;
-        }
-        if (TOP) {
-            // the lane's largest: the first element of its run that has it
-            uint64_t key = 0;
-            if (any) {
-                if (big_at < 0) key = lp_key(big, j0 + tid);
-                else if (big_at == q.n) key = lp_key(big, j0 + q.head + q.n * E + tid);
-                else {
-#pragma unroll
-                    for (int u = 0; u < E; ++u) {
-                        const uint64_t other = lp_key((float)body[(long long)big_at * E + u], j0 + q.head + big_at * E + u);
-                        key = other > key ? other : key;
-                    }
-                }
-            }
-            if (tid < a.top) best[tid] = 0;
-            if (tid == 0) listed = 0;
-            // a wavefront's `top` largest lane maxima, sorted by compare and exchange
-#pragma unroll
-            for (int size = 2; size <= 64; size <<= 1)
-#pragma unroll
-                for (int o = size >> 1; o > 0; o >>= 1) {
-                    const uint64_t other = key_xor(key, o);
-                    const bool up = (lane & size) == 0, low = (lane & o) == 0;      // descending runs where `up`
-                    const bool more = other > key;
-                    key = (up == low) == more ? other : key;
-                }
-            if (lane < a.top) cand[wave * a.top + lane] = key;
-            __syncthreads();
-            rank_keys<THREADS>(cand, W * a.top, a.top, best);
-            __syncthreads();
-            // the owners' elements from the bound on
-            const uint64_t bound = best[a.top - 1];
-            const int cols = (q.n + THREADS - 1) / THREADS + 2;                      // a lane's runs, and its head and rest
-            for (int i = tid; i < cols * a.top; i += THREADS) {
-                const uint64_t own = best[i / cols];
-                if (own == 0) continue;
-                const int at = (int)key_index(own) - j0;                             // the owner, from where its largest is
-                const int owner = at < q.head ? at : at < q.head + q.n * E ? ((at - q.head) / E) % THREADS : at - q.head - q.n * E;
-                const int col = i % cols;
-                auto add = [&](float x, int j) {
-                    const uint64_t k2 = lp_key(x, j0 + j);
-                    if (k2 >= bound) {
-                        const int slot = atomicAdd(&listed, 1);
-                        if (slot < LP_LIST) list[slot] = k2;
-                    }
-                };
-                if (col == 0) { if (owner < q.head) add((float)p[owner], owner); }
-                else if (col == cols - 1) { if (owner < q.tail) add((float)rest[owner], q.head + q.n * E + owner); }
-                else {
-                    const int run = (col - 1) * THREADS + owner;
-                    if (run < q.n) {
-                        float x[E];
-                        load_wide<T, E, false>(body + (long long)run * E, x);
-#pragma unroll
-                        for (int u = 0; u < E; ++u) add(x[u], q.head + run * E + u);
-                    }
-                }
-            }
-            __syncthreads();
-            const int n = listed;
-            if (n <= LP_LIST) {
-                __syncthreads();
-                rank_keys<THREADS>(list, n, a.top, best);
-            } else {
-                // more of them than fit: one after the other, each the largest below the one before
-                uint64_t last = ~0ull;
-                for (int place = 0; place < a.top; ++place) {
-                    uint64_t most = 0;
-                    for (int j = tid; j < count; j += THREADS) {
-                        const uint64_t k2 = lp_key((float)p[j], j0 + j);
-                        if (k2 < last && k2 > most) most = k2;
-                    }
-#pragma unroll
-                    for (int o = 32; o > 0; o >>= 1) { const uint64_t other = key_xor(most, o); most = other > most ? other : most; }
-                    __syncthreads();
-                    if (lane == 0) cand[wave] = most;
-                    __syncthreads();
-                    for (int i = 0; i < W; ++i) most = cand[i] > most ? cand[i] : most;
-                    if (tid == 0) best[place] = most;
-                    last = most;
-                }
-            }
-            __syncthreads();
+        Done r = {};
+        if (alone) {
+            r = lp_done(st);
+            if (tid == 0) lp_row<T>(a, row, r);
+        } else if (tid == 0) a.parts[row * a.splits + blockIdx.x] = st;
+        if constexpr (TOP) {
+            find_top<T, THREADS>(part, mine, a.top, se);
             if (tid < a.top) {
-                if (alone) lp_alternative(a, row, tid, best[tid], st);
-                else a.keys[(row * a.splits + blockIdx.x) * a.top + tid] = best[tid];
+                if (alone) lp_alternative(a, row, tid, se.best[tid], r);
+                else a.keys[(row * a.splits + blockIdx.x) * a.top + tid] = se.best[tid];
             }
         }
         __syncthreads();                       // the LDS words serve the next row
@@ -294,18 +325,28 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
     const int lane = threadIdx.x;
     const float c = a.inv_t * LOG2E;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        Stat st = {LOWEST, 0.f, 0.f};
-        for (int i = lane; i < a.splits; i += 64) merge(st, a.parts[row * a.splits + i], c);
-        st = wave_merge(st, c);
-        if (lane == 0) lp_row<T>(a, row, st);
+        Stat st = {LOWEST, 0.f, 0.f}, mine[S];
         const uint64_t *const keys = a.keys + row * a.splits * a.top;
         uint64_t head[S];
         int place[S];
 #pragma unroll
         for (int i = 0; i < S; ++i) {
+            const int split = lane + i * 64;
             place[i] = 0;
-            head[i] = a.top > 0 && lane + i * 64 < a.splits ? keys[(lane + i * 64) * a.top] : 0;
+            mine[i] = split < a.splits ? a.parts[row * a.splits + split] : st;
+            head[i] = a.top > 0 && split < a.splits ? keys[split * a.top] : 0;
         }
+        float m = mine[0].m;
+#pragma unroll
+        for (int i = 1; i < S; ++i) m = fmaxf(m, mine[i].m);
+        m = wave_max(m);
+        st.m = m;
+#pragma unroll
+        for (int i = 0; i < S; ++i) { rescale(mine[i], m, c); st.s += mine[i].s; st.w += mine[i].w; }
+        st.s = wave_sum(st.s);
+        st.w = wave_sum(st.w);
+        const Done r = lp_done(st);
+        if (lane == 0) lp_row<T>(a, row, r);
         for (int t = 0; t < a.top; ++t) {
             uint64_t most = head[0];
 #pragma unroll
@@ -315,7 +356,7 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
 #pragma unroll
             for (int i = 0; i < S; ++i)
                 if (head[i] == most && most != 0) head[i] = ++place[i] < a.top ? keys[(lane + i * 64) * a.top + place[i]] : 0;
-            if (lane == 0) lp_alternative(a, row, t, most, st);
+            if (lane == 0) lp_alternative(a, row, t, most, r);
         }
     }
 }
@@ -373,10 +414,11 @@ static LpPlan lp_plan(long long rows, long long V, int E)
     LpPlan q;
     q.threads = V <= 64 * E * 4 ? 64 : V <= 256 * E * 8 ? 256 : 512;
     q.splits = 1;
-    if (q.threads > 64) {
-        const long long want = (1024 + rows - 1) / rows, most = (V + q.threads * E * 2 - 1) / (q.threads * E * 2);
-        q.splits = (int)(rows >= 512 ? 1 : want < most ? want : most);
+    if (q.threads > 64 && rows < 512) {
+        const long long want = (1024 + rows - 1) / rows, most = (V + 256 * E - 1) / (256 * E);
+        q.splits = (int)(want < most ? want : most);
         if (q.splits > LP_MAX_SPLITS) q.splits = LP_MAX_SPLITS;
+        if (q.splits > 1) q.threads = 256;
     }
     q.part = (int)((V + q.splits - 1) / q.splits + E - 1) / E * E;
     q.splits = (int)((V + q.part - 1) / q.part);
