@@ -89,5 +89,11 @@ __device__ __forceinline__ uint32_t wave_max(uint32_t v)
     const uint32_t b = max((uint32_t)__builtin_amdgcn_readlane((int)v, 32), (uint32_t)__builtin_amdgcn_readlane((int)v, 48));
     return max(a, b);
 }
+// the high words first, then the low ones of those that have the highest
+__device__ __forceinline__ uint64_t wave_max(uint64_t v)
+{
+    const uint32_t hi = wave_max((uint32_t)(v >> 32)), lo = wave_max((uint32_t)(v >> 32) == hi ? (uint32_t)v : 0u);
+    return ((uint64_t)hi << 32) | lo;
+}
 
 }  // namespace qsr

@@ -10,8 +10,8 @@
 // One pass over the logits: every lane keeps the largest logit m it has seen, s = sum 2^t and w = sum t 2^t with t = (x - m) c,
 // c = log2 e / T, rescaled where m grows; H = ln 2 (log2 s - w / s).  m starts at the lowest float, not at -inf, so that masked entries
 // (t = -inf) are zeros and never NaN.  x - m is taken before the scaling: c x - c m in one product-sum would shift the row by the
-// rounding of c m, and a token that is certain would not have logp = H = 0.  Four wide loads of a lane are in flight and share one
-// comparison with m.
+// rounding of c m, and a token that is certain would not have logp = H = 0.  The wide loads of a trip are in flight together and
+// share one comparison with m.
 // Alternatives without a second pass over the row: a lane's largest logit is at hand, and the few lanes that can hold alternatives have
 // their logits looked at again, from the caches (find_top).
 #include <cmath>
@@ -38,11 +38,6 @@ __device__ __forceinline__ float key_value(uint64_t key)
     return __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return ~(uint32_t)key; }
-__device__ __forceinline__ uint64_t key_xor(uint64_t v, int o)
-{
-    return ((uint64_t)(uint32_t)__shfl_xor((int)(v >> 32), o, 64) << 32) | (uint32_t)__shfl_xor((int)(uint32_t)v, o, 64);
-}
-
 // w + t 2^t, where 2^t is e; of masked entries 0 and not 0 * -inf (2^-1000 is 0 already)
 __device__ __forceinline__ float add_part(float w, float t, float e) { return fmaf(e, fmaxf(t, -1000.f), w); }
 // m: the largest logit (the lowest float at least); s, w: see above
@@ -142,7 +137,7 @@ __device__ __forceinline__ Runs runs_of(const T *p, int count)
 // A part of a row in a workgroup's hands: where it begins in the row, its runs, and the LDS words of the search for alternatives
 template <typename T> struct Part { const T *p, *body, *rest; int j0, count; Runs q; };
 template <int THREADS> struct Search {
-    float group[64];                           // the largest logit of each of 64 groups of lanes
+    float group[64], bound;                    // the largest logit of each of 64 groups of lanes
     unsigned short owner[THREADS];
     static constexpr int LIST = THREADS > 64 ? 1024 : 256;                     // logits from the bound on that fit
     uint64_t list[LIST], best[LP_MAX_TOP];
@@ -156,10 +151,28 @@ template <int G> __device__ __forceinline__ float group_most(float v)
     return v;
 }
 
-// The `top` largest keys of a part to se.best, 0 where it has fewer elements.  mine: the lane's largest logit.
+// The top-th largest of 64 numbers, by taking the largest away until that many are gone; for many by counting how many are larger.
+__device__ __forceinline__ float top_bound(const float *group, int top)
+{
+    float v = group[threadIdx.x & 63];
+    if (top <= 12) {
+        for (int gone = 0;;) {
+            const float most = wave_max(v);
+            const bool is = v == most;
+            gone += __popcll(__ballot(is));
+            if (gone >= top || most == -INFINITY) return most;
+            v = is ? -INFINITY : v;
+        }
+    }
+    int above = 0;
+    for (int i = 0; i < 64; ++i) above += group[i] > v ? 1 : 0;
+    return -wave_max(above < top ? -v : -INFINITY);
+}
+
+// The `top` largest keys of a part to se.best, 0 where it has fewer elements.  mine: the lane's largest logit, -inf if all are masked.
 // The `top`-th largest of 64 groups' maxima is a bound: that many logits reach it, and only lanes whose own maximum does have any that
 // do.  Their logits alone are looked at again, shared out among all lanes, and those from the bound on are put in order.  Entries of
-// -inf are below any bound; where too few others are there, the first of them follow.
+// -inf are left out of this; where too few others are there, the first of them follow.
 template <typename T, int THREADS>
 __device__ __forceinline__ void find_top(const Part<T> &a, float mine, int top, Search<THREADS> &se)
 {
@@ -170,23 +183,25 @@ __device__ __forceinline__ void find_top(const Part<T> &a, float mine, int top, 
     if (tid < top) se.best[tid] = 0;
     if (tid == 0) se.owners = se.listed = 0;
     __syncthreads();
-    const float group = se.group[lane];
-    int above = 0;
-#pragma unroll
-    for (int i = 0; i < 64; ++i) above += lane_of(group, i) > group ? 1 : 0;
-    const float bound = -wave_max(above < top ? -group : -INFINITY);               // the lowest float at least
-    if (mine >= bound) se.owner[atomicAdd(&se.owners, 1)] = (unsigned short)tid;
+    if (tid < 64) {                            // one wavefront: the chip's arithmetic is as short as its bandwidth here
+        const float b = top_bound(se.group, top);
+        if (tid == 0) se.bound = b;
+    }
+    if (THREADS > 64) __syncthreads();
+    const float bound = se.bound;
+    if (mine >= bound && mine > -INFINITY) se.owner[atomicAdd(&se.owners, 1)] = (unsigned short)tid;
     __syncthreads();
     const int cols = (a.q.n + THREADS - 1) / THREADS + 2;                      // a lane's runs, and its elements of head and rest
-    const int items = cols * se.owners;
+    const int shift = 32 - __builtin_clz(cols - 1), items = se.owners << shift;
     auto add = [&](float x, int j) {
-        if (x >= bound) {
+        if (x >= bound && x > -INFINITY) {
             const int slot = atomicAdd(&se.listed, 1);
             if (slot < se.LIST) se.list[slot] = lp_key(x, a.j0 + j);
         }
     };
     for (int i = tid; i < items; i += THREADS) {
-        const int owner = se.owner[i / cols], col = i % cols, run = (col - 1) * THREADS + owner;
+        const int owner = se.owner[i >> shift], col = i & ((1 << shift) - 1), run = (col - 1) * THREADS + owner;
+        if (col >= cols) continue;
         if (col == 0) { if (owner < a.q.head) add((float)a.p[owner], owner); }
         else if (col == cols - 1) { if (owner < a.q.tail) add((float)a.rest[owner], a.q.head + a.q.n * E + owner); }
         else if (run < a.q.n) {
@@ -224,8 +239,7 @@ __device__ __forceinline__ void find_top(const Part<T> &a, float mine, int top, 
                 const uint64_t other = lp_key((float)a.p[j], a.j0 + j);
                 if (other < last && other > key) key = other;
             }
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) { const uint64_t other = key_xor(key, o); key = other > key ? other : key; }
+            key = wave_max(key);
             __syncthreads();
             if (lane == 0) se.list[tid >> 6] = key;
             __syncthreads();
@@ -241,7 +255,7 @@ __device__ __forceinline__ void find_top(const Part<T> &a, float mine, int top, 
 template <typename T, int THREADS, bool TOP>
 __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
 {
-    constexpr int E = wide_of<T>(), W = THREADS / 64, U = 4;
+    constexpr int E = wide_of<T>(), W = THREADS / 64, U = (TOP ? 8 : 16) / E;      // (with alternatives sixteen logits of a trip would cost registers)
     __shared__ Stat red[W];
     __shared__ Search<TOP ? THREADS : 1> se;
     const int tid = threadIdx.x;
@@ -291,7 +305,7 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
             for (int u = 0; u < E; ++u) take(x[u]);
         }
         if (tid < q.tail) { seen((float)part.rest[tid]); take((float)part.rest[tid]); }
-        const float mine = st.m;
+        const float mine = st.s == 0.f ? -INFINITY : st.m;                     // (its own largest has 2^0 in s)
         st = wave_merge(st, c);
         if (W > 1) {
             if ((tid & 63) == 0) red[tid >> 6] = st;
@@ -316,29 +330,24 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
 }
 
 // Rows that were split: a wavefront joins a row's parts.  Alternatives: each lane keeps the largest key not yet taken of its splits,
-// whose lists are sorted; `top` times the largest of all lanes is taken.
+// whose lists are sorted and lie in LDS; `top` times the largest of all lanes is taken.
 constexpr int LP_MAX_SPLITS = 256;
 template <typename T>
 __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
 {
     constexpr int S = LP_MAX_SPLITS / 64;
-    const int lane = threadIdx.x;
+    extern __shared__ uint64_t keys[];         // [splits][top]
+    const int lane = threadIdx.x, n = a.splits * a.top;
     const float c = a.inv_t * LOG2E;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
         Stat st = {LOWEST, 0.f, 0.f}, mine[S];
-        const uint64_t *const keys = a.keys + row * a.splits * a.top;
-        uint64_t head[S];
-        int place[S];
+        for (int i = lane; i < n; i += 64) keys[i] = a.keys[row * n + i];
+        float m = LOWEST;
 #pragma unroll
         for (int i = 0; i < S; ++i) {
-            const int split = lane + i * 64;
-            place[i] = 0;
-            mine[i] = split < a.splits ? a.parts[row * a.splits + split] : st;
-            head[i] = a.top > 0 && split < a.splits ? keys[split * a.top] : 0;
+            mine[i] = lane + i * 64 < a.splits ? a.parts[row * a.splits + lane + i * 64] : st;
+            m = fmaxf(m, mine[i].m);
         }
-        float m = mine[0].m;
-#pragma unroll
-        for (int i = 1; i < S; ++i) m = fmaxf(m, mine[i].m);
         m = wave_max(m);
         st.m = m;
 #pragma unroll
@@ -347,17 +356,25 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
         st.w = wave_sum(st.w);
         const Done r = lp_done(st);
         if (lane == 0) lp_row<T>(a, row, r);
+        __syncthreads();
+        int at[S];                             // the heads of the lane's lists
+#pragma unroll
+        for (int i = 0; i < S; ++i) at[i] = (lane + i * 64) * a.top;
         for (int t = 0; t < a.top; ++t) {
-            uint64_t most = head[0];
+            uint64_t most = 0;
 #pragma unroll
-            for (int i = 1; i < S; ++i) most = head[i] > most ? head[i] : most;
-#pragma unroll
-            for (int o = 32; o > 0; o >>= 1) { const uint64_t other = key_xor(most, o); most = other > most ? other : most; }
+            for (int i = 0; i < S; ++i) {
+                const bool some = lane + i * 64 < a.splits && at[i] < (lane + i * 64 + 1) * a.top;
+                const uint64_t head = some ? keys[at[i]] : 0;
+                most = head > most ? head : most;
+            }
+            most = wave_max(most);
 #pragma unroll
             for (int i = 0; i < S; ++i)
-                if (head[i] == most && most != 0) head[i] = ++place[i] < a.top ? keys[(lane + i * 64) * a.top + place[i]] : 0;
+                if (lane + i * 64 < a.splits && at[i] < (lane + i * 64 + 1) * a.top && keys[at[i]] == most) ++at[i];
             if (lane == 0) lp_alternative(a, row, t, most, r);
         }
+        __syncthreads();
     }
 }
 
@@ -407,17 +424,20 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_back_kernel(LpBackArgs
     }
 }
 
-// How a row is shared out: workgroups of 64 lanes for short rows, 256 and 512 for longer ones; rows too few to fill the chip are split.
+// How a row is shared out: workgroups of 64 lanes for short rows, 256 for longer ones and wherever rows are many (8192 bf16 rows of
+// 32768 100 us, 106 with 512), 512 for long rows that one workgroup each just about fills the chip with (512 fp32 rows of 50020 19.0 us,
+// 22.6 with 256); rows too few to fill the chip are split, down to a run for each of 256 lanes.
 struct LpPlan { int threads, splits, part; };
-static LpPlan lp_plan(long long rows, long long V, int E)
+static LpPlan lp_plan(long long rows, long long V, int E, int top)
 {
     LpPlan q;
-    q.threads = V <= 64 * E * 4 ? 64 : V <= 256 * E * 8 ? 256 : 512;
+    q.threads = V <= 64 * E * 4 ? 64 : V <= 256 * E * 8 || rows >= 2048 ? 256 : 512;
     q.splits = 1;
     if (q.threads > 64 && rows < 512) {
         const long long want = (1024 + rows - 1) / rows, most = (V + 256 * E - 1) / (256 * E);
         q.splits = (int)(want < most ? want : most);
         if (q.splits > LP_MAX_SPLITS) q.splits = LP_MAX_SPLITS;
+        if (q.splits * top > 4096) q.splits = 4096 / top;            // the joining wavefront's LDS: 32 KiB
         if (q.splits > 1) q.threads = 256;
     }
     q.part = (int)((V + q.splits - 1) / q.splits + E - 1) / E * E;
@@ -433,7 +453,7 @@ static hipError_t launch_lp(const LpArgs &a, hipStream_t s)
     else token_logprobs_kernel<T, THREADS, false><<<grid, THREADS, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || a.splits == 1) return e;
-    token_logprobs_join_kernel<T><<<(unsigned)(a.rows < 65535 ? a.rows : 65535), 64, 0, s>>>(a);
+    token_logprobs_join_kernel<T><<<(unsigned)(a.rows < 65535 ? a.rows : 65535), 64, (size_t)a.splits * a.top * sizeof(uint64_t), s>>>(a);
     return hipGetLastError();
 }
 template <typename T>
@@ -476,7 +496,7 @@ extern "C" int qsr_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, i
     if (!sizes_ok(rows, vocab) || !type_ok(type) || top < 0 || top > vocab) return QSR_EINVAL;
     if (top > LP_MAX_TOP) return QSR_ELIMIT;
     if (rows == 0) return QSR_OK;
-    const LpPlan p = lp_plan(rows, vocab, 16 / (int)size_of(type));
+    const LpPlan p = lp_plan(rows, vocab, 16 / (int)size_of(type), top);
     if (p.splits > 1) *bytes = (size_t)rows * p.splits * ((size_t)top * sizeof(uint64_t) + sizeof(Stat));
     return QSR_OK;
 }
@@ -497,7 +517,7 @@ extern "C" int qsr_token_logprobs(const qsr_token_logprobs_args *q, void *worksp
     if (q->top > 0 && (!q->top_logp || !q->top_id || off(q->top_logp, 4) || off(q->top_id, 4))) return QSR_EINVAL;
     if (need > 0 && (!workspace || off(workspace, 8))) return QSR_EINVAL;
     if (workspace_bytes < need) return QSR_ENOMEM;
-    const LpPlan p = lp_plan(q->rows, q->vocab, 16 / (int)size_of(q->type));
+    const LpPlan p = lp_plan(q->rows, q->vocab, 16 / (int)size_of(q->type), q->top);
     uint64_t *const keys = (uint64_t *)workspace;
     const LpArgs a{q->logits, q->tokens, q->rows, q->stride, (int)q->vocab, q->top, p.splits, p.part, inv_t, q->logp, q->entropy,
                    q->lse, q->stats, q->top_logp, q->top_id, (Stat *)(keys + (p.splits > 1 ? q->rows * p.splits * q->top : 0)), keys};
