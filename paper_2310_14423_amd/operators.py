@@ -213,11 +213,11 @@ def rmsnorm_backward(y_grad, sum, weight, rstd, residual_grad=None, stream=None)
     rstd_at = _numbers(rstd, shape[:-1], sum, "rstd")
     n = C.c_size_t(0)
     _check(_functions.qsr_rmsnorm_workspace_bytes(K, rows, d, ty, n), "qsr_rmsnorm_workspace_bytes")
-    ws = torch.empty(n.value, dtype=torch.uint8, device=sum.device)
+    ws = torch.empty(n.value, dtype=torch.uint8, device=sum.device) if n.value else None
     x_grad, weight_grad = torch.empty_like(sum, memory_format=torch.contiguous_format), torch.empty_like(weight)
     a = RMSNormBackwardArgs(K, ty, rows, d, dy_at, sum.data_ptr(), weight.data_ptr(), rstd_at, res_at, x_grad.data_ptr(),
                             weight_grad.data_ptr(), dy_stride, _row_stride(sum, "sum"), res_stride, d)
-    _check(_functions.qsr_rmsnorm_backward(a, ws.data_ptr(), n, s), "qsr_rmsnorm_backward")
+    _check(_functions.qsr_rmsnorm_backward(a, None if ws is None else ws.data_ptr(), n, s), "qsr_rmsnorm_backward")
     return x_grad, weight_grad
 
 

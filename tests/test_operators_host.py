@@ -75,7 +75,7 @@ def test_rmsnorm_arguments(over, code):
 
 
 @pytest.mark.parametrize("over,ws,code", [
-    (dict(), 0, -4), (dict(), None, -1), (dict(type=2), 1 << 30, -1), (dict(y_grad=None), 1 << 30, -1), (dict(sum=P + 2), 1 << 30, -1),
+    (dict(rows=300), 0, -4), (dict(rows=300), 16, -4), (dict(rows=300), None, -1), (dict(type=2), 1 << 30, -1), (dict(y_grad=None), 1 << 30, -1), (dict(sum=P + 2), 1 << 30, -1),
     (dict(weight=None), 1 << 30, -1), (dict(rstd=None), 1 << 30, -1), (dict(residual_grad=P + 1), 1 << 30, -1),
     (dict(x_grad=None), 1 << 30, -1), (dict(weight_grad=None), 1 << 30, -1), (dict(x_grad_stride=99), 1 << 30, -1),
     (dict(y_grad_stride=99), 1 << 30, -1), (dict(sum_stride=99), 1 << 30, -1), (dict(residual_grad_stride=99), 1 << 30, -1),
