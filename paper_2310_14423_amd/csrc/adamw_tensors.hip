@@ -250,14 +250,30 @@ __device__ __forceinline__ void at_trip_fp8(const AtTensor &t, const AtStep &st,
     }
 }
 
+// How a worker's factor comes to the update: from `coef`, or, where its partial sums of squares are at most one to a lane (nb > 0),
+// from these, added up by every wavefront in the same order; the first one leaves factor and norm in coef for those who ask.
+struct AtClip { float *coef; const double *partial; int nb, K; float max_norm; };
+__device__ __forceinline__ float at_factor(const AtClip &c, int k)
+{
+    if (c.coef == nullptr) return 1.f;
+    if (c.nb == 0) return c.coef[k];
+    double sum = (int)threadIdx.x < c.nb ? c.partial[(long long)k * c.nb + threadIdx.x] : 0.0;
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o, 64);
+    const double norm = sqrt(sum), f = (double)c.max_norm / (norm + 1e-6);
+    const float factor = f < 1.0 ? (float)f : 1.0f;
+    if (blockIdx.x == 0 && threadIdx.x == 0) { c.coef[k] = factor; c.coef[c.K + k] = (float)norm; }
+    return factor;
+}
+
 template <typename G, bool FP8>
 __global__ __launch_bounds__(64) void adamw_tensors_kernel(const AtTensor *__restrict__ list, const AtChunk *__restrict__ chunks,
-                                                           AtStep st, const float *__restrict__ coef)
+                                                           AtStep st, AtClip clip)
 {
     const AtChunk ch = chunks[blockIdx.x];
     const AtTensor &t = list[ch.tensor];
     const long long k = blockIdx.y, e0 = (long long)ch.block * AT_BLOCK;
-    const float gs = coef != nullptr ? coef[k] : 1.f;
+    const float gs = at_factor(clip, blockIdx.y);
     const bool full = t.n - e0 >= AT_SPAN * AT_BLOCK;
     if (FP8) {
         if (full) at_trip_fp8<G, true>(t, st, k, e0, gs);
@@ -468,14 +484,16 @@ extern "C" int qsr_adamw_step(qsr_adamw *a, int64_t t, double eta, void *stream)
 {
     if (!a || t < 0 || !std::isfinite(eta) || eta < 0.0) return QSR_EINVAL;
     hipStream_t s = (hipStream_t)stream;
-    const float *coef = nullptr;
+    AtClip clip{nullptr, nullptr, 0, a->K, a->clip};
     const unsigned K = (unsigned)a->K;
     if (a->clip > 0.f) {
         if (a->grad_bf16) tensors_sqnorm_kernel<bf16_t><<<dim3((unsigned)a->spans, K), AT_NORM_THREADS, 0, s>>>(a->d_list, a->d_spans, a->d_partial);
         else tensors_sqnorm_kernel<float><<<dim3((unsigned)a->spans, K), AT_NORM_THREADS, 0, s>>>(a->d_list, a->d_spans, a->d_partial);
         HIP_TRY(hipGetLastError());
-        HIP_TRY(launch_clip_finish(a->d_partial, a->K, (int)a->spans, a->clip, a->d_coef, a->d_coef + a->K, s));
-        coef = a->d_coef;
+        clip.coef = a->d_coef;
+        clip.partial = a->d_partial;
+        if (a->spans <= 64) clip.nb = (int)a->spans;
+        else HIP_TRY(launch_clip_finish(a->d_partial, a->K, (int)a->spans, a->clip, a->d_coef, a->d_coef + a->K, s));
     }
     const double n = (double)(t + 1);
     AtStep st;
@@ -485,10 +503,10 @@ extern "C" int qsr_adamw_step(qsr_adamw *a, int64_t t, double eta, void *stream)
     st.c1 = (float)(1.0 - a->beta1); st.c2 = (float)(1.0 - a->beta2); st.eps = a->eps;
     st.key = step_key(a->seed, t);
     const dim3 grid((unsigned)a->chunks, K);
-    if (a->fp8 && a->grad_bf16) adamw_tensors_kernel<bf16_t, true><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
-    else if (a->fp8) adamw_tensors_kernel<float, true><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
-    else if (a->grad_bf16) adamw_tensors_kernel<bf16_t, false><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
-    else adamw_tensors_kernel<float, false><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, coef);
+    if (a->fp8 && a->grad_bf16) adamw_tensors_kernel<bf16_t, true><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, clip);
+    else if (a->fp8) adamw_tensors_kernel<float, true><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, clip);
+    else if (a->grad_bf16) adamw_tensors_kernel<bf16_t, false><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, clip);
+    else adamw_tensors_kernel<float, false><<<grid, 64, 0, s>>>(a->d_list, a->d_chunks, st, clip);
     HIP_TRY(hipGetLastError());
     return QSR_OK;
 }
