@@ -1,12 +1,14 @@
-"""Builds libqsr.so (the C-ABI library) for gfx950 with hipcc, in-tree."""
+"""Builds libqsr.so (the C-ABI library) for gfx950 with hipcc, and the Python extension that calls it with torch tensors, in-tree."""
 import glob
 import os
 import subprocess
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(os.path.dirname(PKG), "include")
 LIB = os.path.join(PKG, "libqsr.so")
+CALLS = os.path.join(PKG, "_calls.so")
 
 FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",   # no packed-fp32 instructions
@@ -26,7 +28,23 @@ def build(verbose=False):
         print(" ".join(cmd))
     subprocess.check_call(cmd)
     os.replace(LIB + ".tmp", LIB)
+    build_calls(verbose)
     return LIB
+
+
+def build_calls(verbose=False):
+    """The extension behind operators.py: host code, against torch's headers and libqsr.so."""
+    import torch
+    root = os.path.dirname(torch.__file__)
+    cmd = ["g++", "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall", "-D_GLIBCXX_USE_CXX11_ABI=%d" % torch.compiled_with_cxx11_abi(),
+           "-I", INCLUDE, "-isystem", os.path.join(root, "include"), "-isystem", os.path.join(root, "include", "torch", "csrc", "api", "include"),
+           "-isystem", sysconfig.get_paths()["include"], os.path.join(CSRC, "torch_calls.cpp"), "-o", CALLS + ".tmp",
+           "-L", PKG, "-lqsr", "-L", os.path.join(root, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10", "-Wl,-rpath,$ORIGIN"]
+    if verbose:
+        print(" ".join(cmd))
+    subprocess.check_call(cmd)
+    os.replace(CALLS + ".tmp", CALLS)
+    return CALLS
 
 
 if __name__ == "__main__":

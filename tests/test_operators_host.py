@@ -3,8 +3,8 @@ import ctypes as C
 
 import pytest
 
+import operators_abi as ops
 import paper_2310_14423_amd as qsr
-from paper_2310_14423_amd import operators as ops
 
 P = 1 << 20         # an address that nothing reads
 
