@@ -342,16 +342,17 @@ typedef struct {
     int32_t K, type, y_type;
     int64_t rows, d;          /* rows of a worker, >= 0 */
     const void *x, *residual; /* residual may be NULL */
-    const float *weight;      /* [K][d] */
+    const float *weight;      /* [K][d], rows weight_stride apart */
     void *sum, *y;
     float *scale, *rstd;
     int64_t x_stride, residual_stride, sum_stride, y_stride; /* from row to row, >= d */
+    int64_t weight_stride;    /* from worker to worker, >= d; read only where K > 1 */
     double eps;
 } qsr_rmsnorm_args;
 int qsr_rmsnorm(const qsr_rmsnorm_args *args, void *stream);
 
-/* Its gradients, from s as it was kept: x_grad (of x and of residual alike) and weight_grad [K][d] (overwritten; sums in a fixed
- * order).  residual_grad: what comes down the residual stream, added to x_grad, or NULL. */
+/* Its gradients, from s as it was kept: x_grad (of x and of residual alike) and weight_grad, [K][d] without gaps (overwritten;
+ * sums in a fixed order).  residual_grad: what comes down the residual stream, added to x_grad, or NULL. */
 typedef struct {
     int32_t K, type;
     int64_t rows, d;
@@ -360,7 +361,7 @@ typedef struct {
     const void *residual_grad;
     void *x_grad;
     float *weight_grad;
-    int64_t y_grad_stride, sum_stride, residual_grad_stride, x_grad_stride;
+    int64_t y_grad_stride, sum_stride, residual_grad_stride, x_grad_stride, weight_stride;
 } qsr_rmsnorm_backward_args;
 int qsr_rmsnorm_workspace_bytes(int32_t K, int64_t rows, int64_t d, int32_t type, size_t *bytes);
 int qsr_rmsnorm_backward(const qsr_rmsnorm_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);

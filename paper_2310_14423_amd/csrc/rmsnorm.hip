@@ -20,6 +20,7 @@ struct RmsArgs {
     void *sum, *y;
     float *scale, *rstd;
     long long rows, s_x, s_res, s_sum, s_y;    // rows of a worker; strides from row to row
+    long long s_w;                             // and from worker to worker
     int d;
     float eps;
 };
@@ -173,7 +174,7 @@ __device__ __forceinline__ void rmsnorm_row(const RmsArgs &a, int k, long long r
     RowPart<T, NV> s, w;
     load_row<T, L, W, NV, true>((const T *)a.x + row * a.s_x, lane, a.d, x);
     if (a.res != nullptr) load_row<T, L, W, NV, true>((const T *)a.res + row * a.s_res, lane, a.d, res);
-    load_words<T, L, W, NV>(a.w + (long long)k * a.d, lane, a.d, w);
+    load_words<T, L, W, NV>(a.w + k * a.s_w, lane, a.d, w);
     each<T, NV>([](float &y, float v) { y = v; }, s, x);
     if (a.res != nullptr) each<T, NV>([](float &y, float v) { y += v; }, s, res);
     float q = 0.f;
@@ -241,7 +242,7 @@ struct RmsBackArgs {
     const void *dres;
     void *dx;
     float *partial;                            // [K][groups][d]
-    long long rows, s_dy, s_h, s_dres, s_dx;
+    long long rows, s_dy, s_h, s_dres, s_dx, s_w;
     int d;
 };
 
@@ -259,7 +260,7 @@ __global__ __launch_bounds__(rms_threads<W>(), 4) void rmsnorm_back_kernel(RmsBa
     const int k = blockIdx.y, lane = rms_lane<L, W>(), place = rms_place<L, W>();
     const long long step = (long long)gridDim.x * side, last = (k + 1) * a.rows;
     RowPart<T, NV> w, dw;
-    load_words<T, L, W, NV>(a.w + (long long)k * a.d, lane, a.d, w);
+    load_words<T, L, W, NV>(a.w + k * a.s_w, lane, a.d, w);
     each<T, NV>([](float &x) { x = 0.f; }, dw);
     Row<T, NV> g, h, e = {};
     float rstd = 0.f;
@@ -438,10 +439,11 @@ extern "C" int qsr_rmsnorm(const qsr_rmsnorm_args *q, void *stream)
     if (!q->x || off(q->x, es) || off(q->residual, es) || !q->weight || off(q->weight, 4) || off(q->sum, es) || !q->y ||
         (!fp8 && off(q->y, es)) || off(q->rstd, 4) || off(q->scale, 4) || (fp8 && !q->scale))
         return QSR_EINVAL;
-    if (q->x_stride < q->d || q->y_stride < q->d || (q->residual && q->residual_stride < q->d) || (q->sum && q->sum_stride < q->d))
+    if (q->x_stride < q->d || q->y_stride < q->d || (q->residual && q->residual_stride < q->d) || (q->sum && q->sum_stride < q->d) ||
+        (q->K > 1 && q->weight_stride < q->d))
         return QSR_EINVAL;
     const RmsArgs a{q->x, q->residual, q->weight, q->sum, q->y, fp8 ? q->scale : nullptr, q->rstd, q->rows, q->x_stride,
-                    q->residual_stride, q->sum_stride, q->y_stride, (int)q->d, (float)q->eps};
+                    q->residual_stride, q->sum_stride, q->y_stride, q->weight_stride, (int)q->d, (float)q->eps};
     return finish(q->type == QSR_TYPE_F32 ? launch_rms<float>(a, q->K, fp8, (hipStream_t)stream)
                                           : launch_rms<bf16_t>(a, q->K, fp8, (hipStream_t)stream));
 }
@@ -467,7 +469,7 @@ extern "C" int qsr_rmsnorm_backward(const qsr_rmsnorm_backward_args *q, void *wo
                         off(q->residual_grad, es) || !q->x_grad || off(q->x_grad, es)))
         return QSR_EINVAL;
     if (q->y_grad_stride < q->d || q->sum_stride < q->d || q->x_grad_stride < q->d ||
-        (q->residual_grad && q->residual_grad_stride < q->d))
+        (q->residual_grad && q->residual_grad_stride < q->d) || (q->K > 1 && q->weight_stride < q->d))
         return QSR_EINVAL;
     size_t need = 0;
     const int rc = qsr_rmsnorm_workspace_bytes(q->K, q->rows, q->d, q->type, &need);
@@ -475,7 +477,7 @@ extern "C" int qsr_rmsnorm_backward(const qsr_rmsnorm_backward_args *q, void *wo
     if (need > 0 && (!workspace || off(workspace, 4))) return QSR_EINVAL;
     if (workspace_bytes < need) return QSR_ENOMEM;
     RmsBackArgs a{q->y_grad, q->sum, q->weight, q->rstd, q->residual_grad, q->x_grad, (float *)workspace, q->rows,
-                        q->y_grad_stride, q->sum_stride, q->residual_grad_stride, q->x_grad_stride, (int)q->d};
+                        q->y_grad_stride, q->sum_stride, q->residual_grad_stride, q->x_grad_stride, q->weight_stride, (int)q->d};
     return finish(q->type == QSR_TYPE_F32 ? launch_rms_back<float>(a, q->K, q->weight_grad, (hipStream_t)stream)
                                           : launch_rms_back<bf16_t>(a, q->K, q->weight_grad, (hipStream_t)stream));
 }

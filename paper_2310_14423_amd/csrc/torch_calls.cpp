@@ -75,16 +75,17 @@ at::Tensor new_rows(const at::Tensor &x, at::ScalarType type, int64_t each = 0)
     return at::empty(s, x.options().dtype(type));
 }
 
-// Workers, and rows of each
-void workers(const at::Tensor &x, const at::Tensor &w, int32_t &K, int64_t &rows)
+// Workers, rows of each, and the stride of their weights
+void workers(const at::Tensor &x, const at::Tensor &w, int32_t &K, int64_t &rows, int64_t &stride)
 {
-    need(x.dim() >= 1 && (w.dim() == 1 || w.dim() == 2) && w.size(-1) == x.size(-1) && w.scalar_type() == at::kFloat && w.is_contiguous() &&
-             w.device() == x.device(), "weight: contiguous float32 [d] or [K][d] on the rows' device");
+    need(x.dim() >= 1 && (w.dim() == 1 || w.dim() == 2) && w.size(-1) == x.size(-1) && w.scalar_type() == at::kFloat &&
+             (w.size(-1) == 1 || w.stride(-1) == 1) && w.device() == x.device(), "weight: float32 [d] or [K][d], dense, on the rows' device");
     need(w.dim() == 1 || (x.dim() >= 2 && x.size(0) == w.size(0)), "weight [K][d] goes with rows [K][...][d]");
     const int64_t k = w.dim() == 2 ? w.size(0) : 1;
     need(k >= 1 && k <= 65535 && x.size(-1) >= 1, "1 to 65535 workers and at least one element");
     K = (int32_t)k;
     rows = x.numel() / (k * x.size(-1));
+    stride = w.dim() == 2 ? w.stride(0) : 0;
 }
 
 struct Failed {};
@@ -137,7 +138,7 @@ PyObject *rmsnorm(PyObject *, PyObject *const *o, Py_ssize_t n)
         qsr_rmsnorm_args a{};
         a.type = type_of(x, "x: float32 or bfloat16");
         a.y_type = fp8 ? QSR_TYPE_E4M3 : a.type;
-        workers(x, w, a.K, a.rows);
+        workers(x, w, a.K, a.rows, a.weight_stride);
         a.d = a.y_stride = x.size(-1);
         a.eps = PyFloat_AsDouble(o[3]);
         if (PyErr_Occurred()) throw Failed{};
@@ -167,7 +168,7 @@ PyObject *rmsnorm_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
         const at::Tensor *res = maybe(o[4], "residual_grad");
         qsr_rmsnorm_backward_args a{};
         a.type = type_of(h, "sum: float32 or bfloat16");
-        workers(h, w, a.K, a.rows);
+        workers(h, w, a.K, a.rows, a.weight_stride);
         a.d = a.x_grad_stride = h.size(-1);
         a.y_grad = dy.const_data_ptr();
         a.y_grad_stride = like(dy, h, "y_grad: as sum");

@@ -74,7 +74,7 @@ RMSNorm = namedtuple("RMSNorm", "y sum rstd scale")
 
 def rmsnorm(x, weight, residual=None, eps=1e-6, out="same", sum_out=None, stream=None):
     """y = s * rstd * weight for the rows of s = x + residual (or x); x [..., d] float32 or bfloat16, rows of any even stride;
-    weight float32 [d], or [K][d] where x is [K][..., d].  Returns (y, sum, rstd, scale):
+    weight float32 [d], or [K][d] where x is [K][..., d], each worker's dense.  Returns (y, sum, rstd, scale):
       y      in x's type (out="same"), or float8_e4m3fn (out="fp8") with a float32 `scale` for each row (y = code * scale)
       sum    s in x's type, the residual stream behind (sum_out: a tensor for it, which may be x or residual); x itself
              where there is no residual

@@ -8,14 +8,14 @@ class RMSNormArgs(C.Structure):
     _fields_ = [("K", C.c_int32), ("type", C.c_int32), ("y_type", C.c_int32), ("rows", C.c_int64), ("d", C.c_int64),
                 ("x", C.c_void_p), ("residual", C.c_void_p), ("weight", C.c_void_p), ("sum", C.c_void_p), ("y", C.c_void_p),
                 ("scale", C.c_void_p), ("rstd", C.c_void_p), ("x_stride", C.c_int64), ("residual_stride", C.c_int64),
-                ("sum_stride", C.c_int64), ("y_stride", C.c_int64), ("eps", C.c_double)]
+                ("sum_stride", C.c_int64), ("y_stride", C.c_int64), ("weight_stride", C.c_int64), ("eps", C.c_double)]
 
 
 class RMSNormBackwardArgs(C.Structure):
     _fields_ = [("K", C.c_int32), ("type", C.c_int32), ("rows", C.c_int64), ("d", C.c_int64), ("y_grad", C.c_void_p),
                 ("sum", C.c_void_p), ("weight", C.c_void_p), ("rstd", C.c_void_p), ("residual_grad", C.c_void_p),
                 ("x_grad", C.c_void_p), ("weight_grad", C.c_void_p), ("y_grad_stride", C.c_int64), ("sum_stride", C.c_int64),
-                ("residual_grad_stride", C.c_int64), ("x_grad_stride", C.c_int64)]
+                ("residual_grad_stride", C.c_int64), ("x_grad_stride", C.c_int64), ("weight_stride", C.c_int64)]
 
 
 class TokenLogprobsArgs(C.Structure):

@@ -130,7 +130,11 @@ def test_strides_and_places():
             v.copy_(t)
         f, g = qsr.rmsnorm(x, w, residual=res), qsr.rmsnorm(wide[0], w, residual=wide[1])
         assert torch.equal(f.y, g.y) and torch.equal(f.sum, g.sum) and torch.equal(f.rstd, g.rstd)
-        a, b = qsr.rmsnorm_backward(dy, f.sum, w, f.rstd, dres), qsr.rmsnorm_backward(wide[2], f.sum, w, f.rstd, wide[3])
+        apart = torch.full((K, d + 9), float('nan'), device='cuda')[:, 2:2 + d]
+        apart.copy_(w)
+        g = qsr.rmsnorm(x, apart, residual=res)
+        assert torch.equal(f.y, g.y)
+        a, b = qsr.rmsnorm_backward(dy, f.sum, w, f.rstd, dres), qsr.rmsnorm_backward(wide[2], f.sum, apart, f.rstd, wide[3])
         assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
         for out in (res.clone(), x.clone()):
             other = res if torch.equal(out, x) else x

@@ -56,18 +56,18 @@ def test_adamw_null_arguments():
 
 def _norm(**over):
     a = dict(K=2, type=0, y_type=0, rows=3, d=100, x=P, residual=P, weight=P, sum=P, y=P, scale=P, rstd=P, x_stride=100,
-             residual_stride=100, sum_stride=100, y_stride=100, eps=1e-6)
+             residual_stride=100, sum_stride=100, y_stride=100, weight_stride=100, eps=1e-6)
     a.update(over)
     return ops.RMSNormArgs(**a)
 
 
 @pytest.mark.parametrize("over,code", [
-    (dict(K=0), -1), (dict(rows=-1), -1), (dict(d=0), -1), (dict(d=16385, x_stride=20000, residual_stride=20000, sum_stride=20000,
+    (dict(K=0), -1), (dict(rows=-1), -1), (dict(d=0), -1), (dict(d=16385, x_stride=20000, residual_stride=20000, sum_stride=20000, weight_stride=20000,
                                                                y_stride=20000), -7),
     (dict(type=2), -1), (dict(y_type=1), -1), (dict(y_type=3), -1), (dict(y_type=2, scale=None), -1), (dict(x=None), -1),
     (dict(x=P + 2), -1), (dict(residual=P + 1), -1), (dict(weight=None), -1), (dict(sum=P + 2), -1), (dict(y=None), -1),
     (dict(y=P + 2), -1), (dict(rstd=P + 2), -1), (dict(x_stride=99), -1), (dict(residual_stride=99), -1), (dict(sum_stride=0), -1),
-    (dict(y_stride=99), -1), (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(rows=0, x=None, y=None), 0),
+    (dict(y_stride=99), -1), (dict(weight_stride=99), -1), (dict(eps=-1.0), -1), (dict(eps=float("nan")), -1), (dict(rows=0, x=None, y=None), 0),
 ])
 def test_rmsnorm_arguments(over, code):
     a = _norm(**over)
@@ -79,11 +79,11 @@ def test_rmsnorm_arguments(over, code):
     (dict(weight=None), 1 << 30, -1), (dict(rstd=None), 1 << 30, -1), (dict(residual_grad=P + 1), 1 << 30, -1),
     (dict(x_grad=None), 1 << 30, -1), (dict(weight_grad=None), 1 << 30, -1), (dict(x_grad_stride=99), 1 << 30, -1),
     (dict(y_grad_stride=99), 1 << 30, -1), (dict(sum_stride=99), 1 << 30, -1), (dict(residual_grad_stride=99), 1 << 30, -1),
-    (dict(d=16385), 1 << 30, -1),
+    (dict(d=16385), 1 << 30, -1), (dict(weight_stride=99), 1 << 30, -1),
 ])
 def test_rmsnorm_backward_arguments(over, ws, code):
     a = dict(K=2, type=0, rows=3, d=100, y_grad=P, sum=P, weight=P, rstd=P, residual_grad=P, x_grad=P, weight_grad=P, y_grad_stride=100,
-             sum_stride=100, residual_grad_stride=100, x_grad_stride=100)
+             sum_stride=100, residual_grad_stride=100, x_grad_stride=100, weight_stride=100)
     a.update(over)
     a = ops.RMSNormBackwardArgs(**a)
     rc = qsr.lib().qsr_rmsnorm_backward(C.byref(a), C.c_void_p(0 if ws is None else P), C.c_size_t(ws or 0), None)
