@@ -321,7 +321,8 @@ typedef struct qsr_adamw qsr_adamw; /* opaque, library-owned */
 
 /* Checks a configuration on the host; *why, if given, names the offending field. */
 int qsr_adamw_validate(const qsr_adamw_config *cfg, const char **why);
-/* Keeps the list (addresses, not contents) and tables for it in device memory.  Synchronises.  On failure *out is NULL. */
+/* Keeps the list (addresses, not contents) and tables for it in the current device's memory, which has to be current in the calls
+ * below too.  Synchronises.  On failure *out is NULL. */
 int qsr_adamw_init(const qsr_adamw_config *cfg, qsr_adamw **out);
 /* One step of all workers with learning rate eta; t: steps taken before (0, 1, ...), which sets the bias corrections.  The scalars
  * are passed by value: a recorded step repeats the same t and eta. */
@@ -330,7 +331,7 @@ int qsr_adamw_step(qsr_adamw *a, int64_t t, double eta, void *stream);
 int qsr_adamw_set_grads(qsr_adamw *a, const void *const *grads, int32_t n, void *stream);
 /* The K factors and norms of the last step's clipping: DEVICE arrays of the library's.  QSR_ESTATE without clip_norm. */
 int qsr_adamw_clip(qsr_adamw *a, const float **coef, const float **norm);
-/* Waits for the device. */
+/* Waits for its device. */
 int qsr_adamw_destroy(qsr_adamw *a);
 
 /* Root-mean-square norm of rows of d elements with the residual's addition; worker k owns rows k * rows .. (k + 1) * rows - 1:

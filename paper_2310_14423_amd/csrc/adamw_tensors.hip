@@ -8,7 +8,8 @@
 // with the arithmetic of the [K][P] update (opt_elem.h) where the moments are fp32: the same bits.  Where they are held in 8 bits
 // every operation that leads to a code is rounded by itself, in the order of the formulas and with no fused ones: a last bit decides
 // now and then which of two codes a moment becomes, and so the codes are those of any fp32 implementation of this comment.
-// Parameters are fp32: steps are smaller than half a unit of a bf16 parameter.  A copy of the new parameters in bf16, rounded to nearest, is written on request.
+// Parameters are fp32: steps are smaller than half a unit of a bf16 parameter.  A copy of the new parameters in bf16, rounded to
+// nearest, is written on request.
 //
 // Moments in 8 bits: each 256 consecutive elements of a worker's tensor are a block with one fp32 scale, a lane of a wavefront holds
 // four of them.  m and r (the root: half of v's range of exponents) are e4m3 codes of value * (1 / top * 448), top = max|value| over
@@ -374,7 +375,7 @@ extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
     else if (c->grad_type != QSR_TYPE_F32 && c->grad_type != QSR_TYPE_BF16) w = "grad_type";
     else if (c->state_type != QSR_TYPE_F32 && c->state_type != QSR_TYPE_E4M3) w = "state_type";
     else if (!(finite_ge0(c->beta1) && c->beta1 < 1.0 && finite_ge0(c->beta2) && c->beta2 < 1.0)) w = "beta1/beta2";
-    else if (!(std::isfinite(c->eps) && c->eps > 0.0)) w = "eps";
+    else if (!(std::isfinite(c->eps) && c->eps >= 1.2e-38)) w = "eps";          // a normal float: its reciprocal is finite
     else if (!finite_ge0(c->clip_norm) || c->clip_norm > 1e38 || (c->clip_norm > 0.0 && c->clip_norm < 1e-37)) w = "clip_norm";
     const bool fp8 = !w && c->state_type == QSR_TYPE_E4M3;
     const uintptr_t ga = !w && c->grad_type == QSR_TYPE_BF16 ? 2 : 4;
@@ -538,7 +539,11 @@ extern "C" int qsr_adamw_clip(qsr_adamw *a, const float **coef, const float **no
 extern "C" int qsr_adamw_destroy(qsr_adamw *a)
 {
     if (!a) return QSR_EINVAL;
+    int now = a->device;
+    (void)hipGetDevice(&now);
+    (void)hipSetDevice(a->device);
     (void)hipDeviceSynchronize();
     free_adamw(a);
+    (void)hipSetDevice(now);
     return QSR_OK;
 }

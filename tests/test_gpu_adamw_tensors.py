@@ -241,6 +241,34 @@ def test_rows_apart_other_gradients_and_streams():
         assert torch.equal(buf["p"][:, mask.cuda()], outside[:, mask.cuda()])
 
 
+def test_other_gradients_for_many_tensors():
+    """More tensors than one launch of addresses holds."""
+    p, g = _tensors([3 + i % 5 for i in range(700)], 2, torch.bfloat16, 8)
+    q, h = [x.clone() for x in p], [x.flip(1).contiguous() for x in g]
+    a, b = qsr.AdamW(p, g), qsr.AdamW(q, h)
+    a.set_grads(h)
+    a.step(1e-2, 0)
+    b.step(1e-2, 0)
+    assert all(torch.equal(x, y) for x, y in zip(p, q))
+
+
+def test_recorded_and_replayed():
+    p, g = _tensors([5000, 70000, 3], 2, torch.float32, 9)
+    q, h = [x.clone() for x in p], [x.clone() for x in g]
+    a, b = (qsr.AdamW(x, y, states="fp8", clip_norm=0.5) for x, y in ((p, g), (q, h)))
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        a.step(1e-2, 4)
+    for _ in range(3):
+        graph.replay()
+        b.step(1e-2, 4)
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(p, q))
+        assert all(torch.equal(a.m[i].view(torch.uint8), b.m[i].view(torch.uint8)) for i in range(3))
+        torch.randn(1000, device="cuda").sum().item()
+
+
 def test_workers_alone_and_together():
     """A worker's fp32 step does not depend on the others."""
     p, g = _tensors([700, 5], 4, torch.float32, 6)

@@ -27,7 +27,7 @@ def _adamw(K=2, n=1000, **over):
     (dict(K=1, param_stride=0, grad_stride=0, state_stride=0, scale_stride=0, copy_stride=0, state_type=2), None),
     (dict(K=0), "K"), (dict(K=65536), "K"), (dict(n_tensors=0), "tensors"), (dict(grad_type=2), "grad_type"),
     (dict(state_type=1), "state_type"), (dict(beta1=1.0), "beta1/beta2"), (dict(beta2=-0.1), "beta1/beta2"),
-    (dict(beta2=float("nan")), "beta1/beta2"), (dict(eps=0.0), "eps"), (dict(clip_norm=float("inf")), "clip_norm"),
+    (dict(beta2=float("nan")), "beta1/beta2"), (dict(eps=0.0), "eps"), (dict(eps=1e-39), "eps"), (dict(clip_norm=float("inf")), "clip_norm"),
     (dict(clip_norm=1e-60), "clip_norm"), (dict(n=0), "n"), (dict(n=1 << 36), "n"), (dict(param=None), "param"),
     (dict(param=P + 2), "param"), (dict(grad=P + 2), "grad"), (dict(grad_type=1, grad=P + 1), "grad"), (dict(m=None), "m/v"),
     (dict(v=P + 1), "m/v"), (dict(state_type=2, m_scale=None), "m_scale"), (dict(copy=P + 1), "copy"),
