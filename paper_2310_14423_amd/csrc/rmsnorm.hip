@@ -319,26 +319,32 @@ __global__ __launch_bounds__(rms_threads<W>(), 4) void rmsnorm_back_kernel(RmsBa
     store_words<T, L, W, NV>(a.partial + ((long long)k * gridDim.x + blockIdx.x) * a.d, lane, a.d, dw);
 }
 
-// dw[k][j] = sum over the parts: 32 columns and 32 runs of parts, four of each in flight, to a workgroup; a fixed order
-constexpr int SUM_RUNS = 32;
-__global__ __launch_bounds__(32 * SUM_RUNS) void rmsnorm_weight_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dw)
+// dw[k][j] = sum over the parts, in a fixed order: COLS columns and 1024 / COLS runs of parts, four of each in flight, to a workgroup.
+// Latency is everything: fewer columns, on more workgroups, where there are few of them.
+constexpr int SUM_THREADS = 1024;
+template <int COLS>
+__global__ __launch_bounds__(SUM_THREADS) void rmsnorm_weight_kernel(const float *__restrict__ partial, int parts, int d, float *__restrict__ dw)
 {
-    __shared__ float red[SUM_RUNS][33];
-    const int k = blockIdx.y, col = threadIdx.x & 31, run = threadIdx.x >> 5;
-    const int j = blockIdx.x * 32 + col;
+    constexpr int RUNS = SUM_THREADS / COLS, WAVES = SUM_THREADS / 64;
+    __shared__ float red[WAVES][COLS];
+    const int k = blockIdx.y, col = threadIdx.x % COLS, run = threadIdx.x / COLS;
+    const int j = blockIdx.x * COLS + col;
     const float *p = partial + (long long)k * parts * d + j;
     float s[4] = {0.f, 0.f, 0.f, 0.f};
     if (j < d)
-        for (int i = run; i < parts; i += 4 * SUM_RUNS)
+        for (int i = run; i < parts; i += 4 * RUNS)
 #pragma unroll
             for (int u = 0; u < 4; ++u)
-                if (i + u * SUM_RUNS < parts) s[u] += p[(long long)(i + u * SUM_RUNS) * d];
-    red[run][col] = (s[0] + s[1]) + (s[2] + s[3]);
+                if (i + u * RUNS < parts) s[u] += p[(long long)(i + u * RUNS) * d];
+    float sum = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+    for (int o = COLS; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+    if ((threadIdx.x & 63) < COLS) red[threadIdx.x >> 6][col] = sum;
     __syncthreads();
     if (run != 0 || j >= d) return;
-    float sum = 0.f;
+    sum = 0.f;
 #pragma unroll
-    for (int i = 0; i < SUM_RUNS; ++i) sum += red[i][col];
+    for (int i = 0; i < WAVES; ++i) sum += red[i][col];
     dw[(long long)k * d + j] = sum;
 }
 
@@ -405,7 +411,10 @@ static hipError_t launch_rms_back(RmsBackArgs &a, int K, float *dw, hipStream_t 
 #undef RMS_BACK
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || groups == 1) return e;
-    rmsnorm_weight_kernel<<<dim3((unsigned)((a.d + 31) / 32), (unsigned)K), 32 * SUM_RUNS, 0, s>>>(a.partial, (int)groups, a.d, dw);
+    const long long cols = (long long)K * a.d;
+    const auto sums = cols >= 256 * 32 ? rmsnorm_weight_kernel<32> : cols >= 256 * 16 ? rmsnorm_weight_kernel<16> : rmsnorm_weight_kernel<8>;
+    const int per = cols >= 256 * 32 ? 32 : cols >= 256 * 16 ? 16 : 8;
+    sums<<<dim3((unsigned)((a.d + per - 1) / per), (unsigned)K), SUM_THREADS, 0, s>>>(a.partial, (int)groups, a.d, dw);
     return hipGetLastError();
 }
 

@@ -426,14 +426,15 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_back_kernel(LpBackArgs
 
 // How a row is shared out: workgroups of 64 lanes for short rows, 256 for longer ones and wherever rows are many (8192 bf16 rows of
 // 32768 100 us, 106 with 512), 512 for long rows that one workgroup each just about fills the chip with (512 fp32 rows of 50020 19.0 us,
-// 22.6 with 256); rows too few to fill the chip are split, down to a run for each of 256 lanes.
+// 22.6 with 256); long rows too few to fill the chip are split,
+// down to a run for each of 256 lanes: one of 16000 in bf16 takes 5.1 us either way, and the second launch of a split one is saved below.
 struct LpPlan { int threads, splits, part; };
 static LpPlan lp_plan(long long rows, long long V, int E, int top)
 {
     LpPlan q;
     q.threads = V <= 64 * E * 4 ? 64 : V <= 256 * E * 8 || rows >= 2048 ? 256 : 512;
     q.splits = 1;
-    if (q.threads > 64 && rows < 512) {
+    if (V > 512 * E * 8 && rows < 512) {
         const long long want = (1024 + rows - 1) / rows, most = (V + 256 * E - 1) / (256 * E);
         q.splits = (int)(want < most ? want : most);
         if (q.splits > LP_MAX_SPLITS) q.splits = LP_MAX_SPLITS;
