@@ -267,11 +267,27 @@ __device__ __forceinline__ float at_factor(const AtClip &c, int k)
     return factor;
 }
 
+// Workgroups go to the chip's 8 dies in turn, each with an L2 of its own.  With 8-bit moments 64 trips in a row are one die's, so that
+// their scales' and chunks' cache lines are fetched once and not by every die: 1.80 against 1.87 ms for 8 x 85e6 elements with bf16
+// gradients (runs of 16: 1.93, 32: 1.93, 256: 1.81).  With fp32 moments, which have no scales, it only scatters: 0.885 against 0.878 ms.
+__device__ __forceinline__ unsigned at_trip(unsigned block, unsigned n)
+{
+    constexpr unsigned DIES = 8, RUN = 64;
+    if ((block | (DIES * RUN - 1)) >= n) return block;                         // the last, incomplete group
+    return (block & ~(DIES * RUN - 1)) + (block % DIES) * RUN + block / DIES % RUN;
+}
+
+// Bound by memory.  With 85e6 elements a worker:
+//   fp32 moments and gradients, 2 workers: 28 bytes an element, 0.73-0.74 ms, 6.5 TB/s; clipped, 0.11 ms before it for the norm
+//   8-bit moments, bf16 gradients and copies, 8 workers: 16.03 bytes an element, 1.80 ms, 6.1 TB/s
+// (a large copy reaches 5.4 TB/s, with one byte written for each one read).  The arithmetic of roots, random words and codes hides
+// behind the loads of the other 31 wavefronts of a CU: 49 registers a lane.
+// A wavefront is a workgroup: a block's largest value needs no LDS and no barrier.
 template <typename G, bool FP8>
 __global__ __launch_bounds__(64) void adamw_tensors_kernel(const AtTensor *__restrict__ list, const AtChunk *__restrict__ chunks,
                                                            AtStep st, AtClip clip)
 {
-    const AtChunk ch = chunks[blockIdx.x];
+    const AtChunk ch = chunks[FP8 ? at_trip(blockIdx.x, gridDim.x) : blockIdx.x];
     const AtTensor &t = list[ch.tensor];
     const long long k = blockIdx.y, e0 = (long long)ch.block * AT_BLOCK;
     const float gs = at_factor(clip, blockIdx.y);
