@@ -329,8 +329,8 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
     }
 }
 
-// Rows that were split: a wavefront joins a row's parts.  Alternatives: each lane keeps the largest key not yet taken of its splits,
-// whose lists are sorted and lie in LDS; `top` times the largest of all lanes is taken.
+// Rows that were split: a wavefront joins a row's parts.  Alternatives: each lane holds the largest key not yet taken of each of its
+// splits, whose lists are sorted and lie in LDS; `top` times the largest of all lanes is taken.
 constexpr int LP_MAX_SPLITS = 256;
 template <typename T>
 __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
@@ -341,7 +341,14 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
     const float c = a.inv_t * LOG2E;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
         Stat st = {LOWEST, 0.f, 0.f}, mine[S];
-        for (int i = lane; i < n; i += 64) keys[i] = a.keys[row * n + i];
+        for (int i = lane; i < n; i += 8 * 64) {                   // eight loads in flight
+            uint64_t key[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) key[u] = a.keys[row * n + min(i + u * 64, n - 1)];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                if (i + u * 64 < n) keys[i + u * 64] = key[u];
+        }
         float m = LOWEST;
 #pragma unroll
         for (int i = 0; i < S; ++i) {
@@ -357,21 +364,21 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
         const Done r = lp_done(st);
         if (lane == 0) lp_row<T>(a, row, r);
         __syncthreads();
-        int at[S];                             // the heads of the lane's lists
+        int at[S];
+        uint64_t head[S];
 #pragma unroll
-        for (int i = 0; i < S; ++i) at[i] = (lane + i * 64) * a.top;
+        for (int i = 0; i < S; ++i) {
+            at[i] = (lane + i * 64) * a.top;
+            head[i] = at[i] < n ? keys[at[i]] : 0;
+        }
         for (int t = 0; t < a.top; ++t) {
-            uint64_t most = 0;
+            uint64_t most = head[0];
 #pragma unroll
-            for (int i = 0; i < S; ++i) {
-                const bool some = lane + i * 64 < a.splits && at[i] < (lane + i * 64 + 1) * a.top;
-                const uint64_t head = some ? keys[at[i]] : 0;
-                most = head > most ? head : most;
-            }
+            for (int i = 1; i < S; ++i) most = head[i] > most ? head[i] : most;
             most = wave_max(most);
 #pragma unroll
             for (int i = 0; i < S; ++i)
-                if (lane + i * 64 < a.splits && at[i] < (lane + i * 64 + 1) * a.top && keys[at[i]] == most) ++at[i];
+                if (head[i] == most) head[i] = ++at[i] < (lane + i * 64 + 1) * a.top ? keys[at[i]] : 0;
             if (lane == 0) lp_alternative(a, row, t, most, r);
         }
         __syncthreads();
@@ -412,12 +419,18 @@ __global__ __launch_bounds__(THREADS) void token_logprobs_back_kernel(LpBackArgs
         };
         const Runs r = runs_of(p, count);
         if ((int)threadIdx.x < r.head) d[threadIdx.x] = (T)grad((float)p[threadIdx.x], threadIdx.x);
-        for (int i = threadIdx.x; i < r.n; i += THREADS) {
-            float x[E];
-            load_wide<T, E, true>(p + r.head + (long long)i * E, x);
+        for (int i = threadIdx.x; i < r.n; i += 4 * THREADS) {
+            float x[4][E];
 #pragma unroll
-            for (int u = 0; u < E; ++u) x[u] = grad(x[u], r.head + i * E + u);
-            store_wide<T, E, true>(d + r.head + (long long)i * E, x);
+            for (int v = 0; v < 4; ++v) load_wide<T, E, true>(p + r.head + (long long)min(i + v * THREADS, r.n - 1) * E, x[v]);
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+                const int run = i + v * THREADS;
+                if (run >= r.n) break;
+#pragma unroll
+                for (int u = 0; u < E; ++u) x[v][u] = grad(x[v][u], r.head + run * E + u);
+                store_wide<T, E, true>(d + r.head + (long long)run * E, x[v]);
+            }
         }
         const int t0 = r.head + r.n * E + threadIdx.x;
         if ((int)threadIdx.x < r.tail) d[t0] = (T)grad((float)p[t0], t0);
