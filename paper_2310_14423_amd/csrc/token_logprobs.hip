@@ -280,9 +280,16 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
         if (tid < q.head) { seen((float)part.p[tid]); take((float)part.p[tid]); }
         int i = tid;
         for (; i + (U - 1) * THREADS < q.n; i += U * THREADS) {
+            typedef typename Wide<T, E>::vec V;
+            V raw[U];
+#pragma unroll
+            for (int v = 0; v < U; ++v) raw[v] = *(const V *)(part.body + (long long)(i + v * THREADS) * E);
+            if (!TOP) __builtin_amdgcn_sched_barrier(0);       // or the second load waits for the first: 8192 bf16 rows of 32768 take 100 us then, 98 so
             float x[U][E];
 #pragma unroll
-            for (int v = 0; v < U; ++v) load_wide<T, E, false>(part.body + (long long)(i + v * THREADS) * E, x[v]);
+            for (int v = 0; v < U; ++v)
+#pragma unroll
+                for (int u = 0; u < E; ++u) x[v][u] = (float)raw[v][u];
             float top = x[0][0];
 #pragma unroll
             for (int v = 0; v < U; ++v)
