@@ -307,3 +307,32 @@ def test_refusals():
         with pytest.raises(qsr.QSRError) as e:
             opt.step(eta, t)
         assert e.value.code == -1
+
+
+def test_step_numbers_have_an_end():
+    p, g = _tensors([10], 1, torch.float32, 10)
+    opt = qsr.AdamW(p, g)
+    with pytest.raises(qsr.QSRError) as e:
+        opt.step(1e-3, 2 ** 63 - 1)
+    assert e.value.code == -1
+    opt.step(1e-3, 2 ** 63 - 2)
+    assert p[0].isfinite().all()
+
+
+@pytest.mark.parametrize("blocks", [1023, 1024, 1025, 2048, 2600])
+def test_every_block_is_taken_once(blocks):
+    """Lists around whole groups of trips, with 8-bit moments: after two steps of a gradient that is the same everywhere, from the same
+    parameters, every element is where the others are but for the second step's rounded moments (a code is off by 2^-3 at most), and
+    every block has its scale."""
+    n = blocks * 256 - 100
+    p, g = [torch.ones(2, n, device="cuda"), torch.ones(2, 300, device="cuda")], [torch.full((2, n), 1e-2, device="cuda"),
+                                                                                 torch.full((2, 300), 1e-2, device="cuda")]
+    opt = qsr.AdamW(p, g, states="fp8", beta1=B1, beta2=B2, eps=EPS)
+    opt.step(1e-3, 0)
+    for x in p:         # m and r are still exact where they are used: a step of eta
+        assert (x.double() - (1 - 1e-3)).abs().max() <= 2 ** -24 * 2
+    opt.step(1e-3, 1)
+    for i, x in enumerate(p):
+        assert (x.double() - (1 - 2e-3)).abs().max() <= 1e-3 * 2 ** -2
+        for s, want in ((opt.m_scale[i], 1.9e-3), (opt.v_scale[i], 1e-2 * (1 - B2 ** 2) ** 0.5)):
+            assert ((s.double() * 448 - want).abs() <= want * 2 ** -3).all()
