@@ -312,7 +312,8 @@ typedef struct {
 typedef struct {
     int32_t K, n_tensors, grad_type, state_type;
     double beta1, beta2, eps;
-    double clip_norm;         /* > 0: gradient clipping by global norm over all tensors of a worker, as in qsr_config; 0 = off */
+    double clip_norm;         /* > 0: gradient clipping by global norm over all tensors of a worker, as in qsr_config; 0 = off.
+                                 Any finite gradients have a finite norm; an infinite one makes the factor 0, a NaN leaves it 1 */
     uint64_t seed;
     const qsr_tensor *tensors; /* (host) read during qsr_adamw_init only */
 } qsr_adamw_config;

@@ -252,7 +252,8 @@ __device__ __forceinline__ void at_trip_fp8(const AtTensor &t, const AtStep &st,
 }
 
 // How a worker's factor comes to the update: from `coef`, or, where its partial sums of squares are at most one to a lane (nb > 0),
-// from these, added up by every wavefront in the same order; the first one leaves factor and norm in coef for those who ask.
+// from these, added up by every wavefront in the same order; the first one leaves factor and norm in coef for those who ask.  A norm
+// that is infinite makes the factor 0; one that is no number clips nothing (factor 1), as in clip_coef_kernel.
 struct AtClip { float *coef; const double *partial; int nb, K; float max_norm; };
 __device__ __forceinline__ float at_factor(const AtClip &c, int k)
 {
@@ -301,9 +302,9 @@ __global__ __launch_bounds__(64) void adamw_tensors_kernel(const AtTensor *__res
     }
 }
 
-// Sum of squares of a span of blocks of a tensor, for each worker: partial[k][span].  Lanes add at most a few hundred squares in fp32,
-// with the rounding errors (opt_elem.h), the rest is double, all in a fixed order.  Bound by memory, four loads of a lane in flight: 110 us
-// for 2 x 85e6 fp32, 6.2 TB/s.
+// Sum of squares of a span of blocks of a tensor, for each worker: partial[k][span].  Squares and sums are double, in a fixed order: a
+// gradient's square may leave the range of floats (from 1.8e19 on), and a norm that is lost there is one that nothing is clipped by.
+// Bound by memory, four loads of a lane in flight, double or not: 109 us for 2 x 85e6 fp32, 6.2 TB/s.
 constexpr int AT_NORM_THREADS = 256;
 struct AtSpan { int tensor, block, blocks; };
 template <typename G>
@@ -316,7 +317,7 @@ __global__ __launch_bounds__(AT_NORM_THREADS) void tensors_sqnorm_kernel(const A
     const int k = blockIdx.y;
     const G *const g = global((const G *)t.grad) + k * t.s_grad;
     const long long e0 = (long long)sp.block * AT_BLOCK, e1 = min(t.n, e0 + (long long)sp.blocks * AT_BLOCK);
-    float s[4] = {0.f, 0.f, 0.f, 0.f}, c[4] = {0.f, 0.f, 0.f, 0.f};
+    double s[4] = {0.0, 0.0, 0.0, 0.0};
     constexpr int U = 4, STEP = AT_NORM_THREADS * 4;
     long long e = e0 + threadIdx.x * 4;
     for (; e + (U - 1) * STEP + 4 <= e1; e += U * STEP) {
@@ -326,18 +327,16 @@ __global__ __launch_bounds__(AT_NORM_THREADS) void tensors_sqnorm_kernel(const A
 #pragma unroll
         for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) add_comp(s[i], c[i], x[u][i] * x[u][i]);
+            for (int i = 0; i < 4; ++i) s[i] = fma((double)x[u][i], (double)x[u][i], s[i]);
     }
     for (; e < e1; e += STEP) {
         float x[4];
         if (e1 - e >= 4) load_wide<G, 4, false>(g + e, x);
         else load_some(g + e, (int)(e1 - e), x);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) add_comp(s[i], c[i], x[i] * x[i]);
+        for (int i = 0; i < 4; ++i) s[i] = fma((double)x[i], (double)x[i], s[i]);
     }
-    double acc = 0.0;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) acc += (double)s[i] + (double)c[i];
+    double acc = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) acc += __shfl_xor(acc, o, 64);
     if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = acc;
