@@ -126,7 +126,8 @@ typedef struct {
     double data_sigma;    /* LINREG: observation noise; MLP2: input noise                  */
     double clip_norm;     /* > 0: gradient clipping by global norm, per worker, before OPT (App. C):
                              g_k <- g_k * min(1, clip_norm / (||g_k||_2 + 1e-6)); with parallel = 1
-                             it acts on the averaged gradient.  0 = off                     */
+                             it acts on the averaged gradient.  0 = off.  Any finite gradient has a
+                             finite norm; an infinite one makes the factor 0, a NaN leaves it 1 */
     uint64_t seed;        /* Philox4x32-10 key of all per-iteration draws                  */
     const int64_t *milestones; /* (host) ascending iteration indices, QSR_LR_STEP          */
     const double *eta_table;   /* (host) T entries, QSR_LR_TABLE                           */
@@ -259,7 +260,8 @@ int qsr_average_rows(float *buf, int32_t K, int64_t P, void *stream);
  * arrays of K floats; the caller multiplies row k by coef[k] (the update kernels of a context with
  * clip_norm do so as they read the gradient).  workspace: DEVICE memory for the partial sums of
  * squares, qsr_clip_workspace_bytes(K, P) bytes, 8-byte aligned, contents irrelevant before and
- * after.  The sums are deterministic (fixed order).  Asynchronous on `stream`.  QSR_EINVAL on bad
+ * after.  The sums are deterministic (fixed order).  Any finite row has a finite norm; an infinite
+ * element makes its row's factor 0, a NaN leaves it 1.  Asynchronous on `stream`.  QSR_EINVAL on bad
  * arguments (K outside 1..65535, P < 1, max_norm not positive and finite), QSR_ENOMEM if the
  * workspace is too small. */
 int qsr_clip_workspace_bytes(int32_t K, int64_t P, size_t *bytes);
@@ -312,8 +314,7 @@ typedef struct {
 typedef struct {
     int32_t K, n_tensors, grad_type, state_type;
     double beta1, beta2, eps;
-    double clip_norm;         /* > 0: gradient clipping by global norm over all tensors of a worker, as in qsr_config; 0 = off.
-                                 Any finite gradients have a finite norm; an infinite one makes the factor 0, a NaN leaves it 1 */
+    double clip_norm;         /* > 0: gradient clipping by global norm over all tensors of a worker, as in qsr_config; 0 = off */
     uint64_t seed;
     const qsr_tensor *tensors; /* (host) read during qsr_adamw_init only */
 } qsr_adamw_config;

@@ -56,6 +56,18 @@ __global__ __launch_bounds__(CLIP_THREADS) void sqnorm_partial_kernel(
     double acc = 0.0;
 #pragma unroll
     for (int u = 0; u < U; ++u) acc += (double)s[u] + (double)c[u];
+    // A square may leave the range of floats (from 1.8e19 on), and its rounding error then is NaN: the lane's elements once more,
+    // in double, where only an element that is not finite itself has such a square.
+    if (!(fabs(acc) < INFINITY)) {
+        acc = 0.0;
+        auto add = [&](float x) { acc = fma((double)x, (double)x, acc); };
+        const long long head = min(i1 - i0, (long long)((16 - ((uintptr_t)(row + i0) & 15)) & 15) / 4);
+        const long long v0 = i0 + head, n4 = (i1 - v0) / 4, t = v0 + n4 * 4 + threadIdx.x;
+        for (long long i = threadIdx.x; i < n4; i += CLIP_THREADS)
+            for (int j = 0; j < 4; ++j) add(row[v0 + 4 * i + j]);
+        if ((long long)threadIdx.x < head) add(row[i0 + threadIdx.x]);
+        if (t < i1) add(row[t]);
+    }
     red[threadIdx.x] = acc;
     __syncthreads();
     for (int w = CLIP_THREADS / 2; w > 0; w >>= 1) {
@@ -67,7 +79,7 @@ __global__ __launch_bounds__(CLIP_THREADS) void sqnorm_partial_kernel(
 
 // coef[k] = min(1, max_norm / (sqrt(sum_b partial[k][b]) + 1e-6)); norm[k] = that square root.  One workgroup per
 // row (nb <= 1024 for a flat row: at most four partial sums per lane, then a fixed tree; one lane adding them all took 12-15 us);
-// same_rows: row 0's sum serves all rows.
+// same_rows: row 0's sum serves all rows.  A norm that is infinite makes the factor 0; one that is no number clips nothing.
 __global__ __launch_bounds__(CLIP_THREADS) void clip_coef_kernel(const double *__restrict__ partial, int nb, float max_norm,
                                                                  int same_rows, float *__restrict__ coef, float *__restrict__ norm)
 {

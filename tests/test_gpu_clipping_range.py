@@ -129,3 +129,35 @@ def test_codes_of_a_long_clipped_list():
         x = torch.nn.functional.pad(g[i].double(), (0, 212)).view(2, 2, 256).abs().amax(-1) * want[:, None].cuda()
         for scale, top in ((opt.m_scale[i], (1 - B1) * x), (opt.v_scale[i], (1 - B2) ** 0.5 * x)):
             assert (scale.double() * 448 - top).abs().le(12 * U * top).all()
+
+
+@pytest.mark.parametrize("at", [0, 2, 500, -1])
+@pytest.mark.parametrize("K,P", [(3, 5), (2, 1027), (3, 20001), (2, 300003)])
+def test_flat_rows_outside_fp32(K, P, at):
+    """Flat rows: one element of row 1 whose square is no float, infinite or no number, wherever it lies in the row.  Ordinary rows'
+    norms are off by the roundings of the squares, U at most; a factor may be subnormal."""
+    at = min(at, P - 1)
+    g = torch.randn(K, P, generator=torch.Generator().manual_seed(5)).cuda()
+    plain = qsr.clip_factors(g, 1.5)
+    for size, infinite in ((2e19, False), (-3e38, False), (float("inf"), True), (float("nan"), None)):
+        g[1, at] = size
+        norm = g.double().pow(2).sum(1).sqrt().cpu()
+        for coef, got in (qsr.clip_factors(g, 1.5), _static_factors(g, 1.5)):
+            coef, got = coef.cpu(), got.cpu()
+            for k in range(K):
+                if k != 1:
+                    assert coef[k] == plain[0][k] and got[k] == plain[1][k]
+                    assert abs(float(got[k]) - float(norm[k])) <= 4 * U * float(norm[k])
+                elif infinite is None:
+                    assert coef[1] == 1 and got[1].isnan()
+                elif infinite:
+                    assert coef[1] == 0 and got[1] == float("inf")
+                else:
+                    want = 1.5 / (float(norm[1]) + 1e-6)
+                    assert abs(float(got[1]) - float(norm[1])) <= 4 * U * float(norm[1]) and abs(float(coef[1]) - want) <= 4 * U * want + 1e-45
+
+
+def _static_factors(g, clip):
+    out = torch.empty(2, g.shape[0], device="cuda")
+    qsr.clip_factors_static(g, clip, out[0], out[1])
+    return out[0], out[1]
