@@ -191,7 +191,7 @@ __device__ __forceinline__ void find_top(const Part<T> &a, float mine, int top, 
         const float b = top_bound(se.group, top);
         if (tid == 0) se.bound = b;
     }
-    if (THREADS > 64) __syncthreads();
+    __syncthreads();
     const float bound = se.bound;
     if (mine >= bound && mine > -INFINITY) se.owner[atomicAdd(&se.owners, 1)] = (unsigned short)tid;
     __syncthreads();
