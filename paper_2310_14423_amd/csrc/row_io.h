@@ -76,6 +76,20 @@ __device__ __forceinline__ float wave_sum(float v)
     v += row_step<0>(v); v += row_step<1>(v); v += row_step<2>(v); v += row_step<3>(v);
     return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
 }
+// the same in double, whose halves go by the same exchanges
+template <int STEP> __device__ __forceinline__ double row_step(double v)
+{
+    return __hiloint2double(row_step<STEP>(__double2hiint(v)), row_step<STEP>(__double2loint(v)));
+}
+__device__ __forceinline__ double lane_of(double v, int lane)
+{
+    return __hiloint2double(__builtin_amdgcn_readlane(__double2hiint(v), lane), __builtin_amdgcn_readlane(__double2loint(v), lane));
+}
+__device__ __forceinline__ double wave_sum(double v)
+{
+    v += row_step<0>(v); v += row_step<1>(v); v += row_step<2>(v); v += row_step<3>(v);
+    return (lane_of(v, 0) + lane_of(v, 16)) + (lane_of(v, 32) + lane_of(v, 48));
+}
 __device__ __forceinline__ float wave_max(float v)
 {
     v = fmaxf(v, row_step<0>(v)); v = fmaxf(v, row_step<1>(v)); v = fmaxf(v, row_step<2>(v)); v = fmaxf(v, row_step<3>(v));

@@ -8,7 +8,8 @@
 // logp = 0 and no gradient from it.
 //
 // One pass over the logits: every lane keeps the largest logit m it has seen, s = sum 2^t and w = sum t 2^t with t = (x - m) c,
-// c = log2 e / T, rescaled where m grows; H = ln 2 (log2 s - w / s).  m starts at the lowest float, not at -inf, so that masked entries
+// c = log2 e / T, rescaled where m grows; H = log s - ln 2 w / s.  s and w are double, a trip of logits a term (take): 1 - p of a token
+// that is nearly certain is what is left of s beside one.  m starts at the lowest float, not at -inf, so that masked entries
 // (t = -inf) are zeros and never NaN.  x - m is taken before the scaling: c x - c m in one product-sum would shift the row by the
 // rounding of c m, and a token that is certain would not have logp = H = 0.  The wide loads of a trip are in flight together and
 // share one comparison with m.
@@ -16,8 +17,8 @@
 // their logits looked at again, from the caches (find_top).
 //
 // What bounds it: many rows, the memory, and close behind it the arithmetic (an exponential, at a quarter of the rate, and eight other
-// instructions a logit).  8192 bf16 rows of 32768: 98 us, 5.5 TB/s; 1001 fp32 rows of 50021 with 5 alternatives 39 us, 5.1 TB/s.  Few
-// rows: chains of latencies, 4 bf16 rows of 131072 with 8 alternatives 6.5 us and 5.3 for the join.
+// instructions a logit).  8192 bf16 rows of 32768: 100 us, 5.4 TB/s (98 with float sums); 1001 fp32 rows of 50021 with 5 alternatives
+// 41 us, 4.9 TB/s (39.5).  Few rows: chains of latencies, 4 bf16 rows of 131072 with 8 alternatives 6.8 us and 5.3 for the join.
 #include <cmath>
 
 #include "qsr_internal.h"
@@ -42,16 +43,33 @@ __device__ __forceinline__ float key_value(uint64_t key)
     return __uint_as_float(b ^ ((b >> 31) ? 0x80000000u : 0xFFFFFFFFu));
 }
 __device__ __forceinline__ uint32_t key_index(uint64_t key) { return ~(uint32_t)key; }
-// w + t 2^t, where 2^t is e; of masked entries 0 and not 0 * -inf (2^-1000 is 0 already)
-__device__ __forceinline__ float add_part(float w, float t, float e) { return fmaf(e, fmaxf(t, -1000.f), w); }
 // m: the largest logit (the lowest float at least); s, w: see above
-struct Stat { float m, s, w; };
+struct Stat { float m; double s, w; };
 __device__ __forceinline__ void rescale(Stat &a, float m, float c)
 {
     const float d = fmaxf((a.m - m) * c, -1000.f), f = __builtin_amdgcn_exp2f(d);
-    a.w = f * fmaf(d, a.s, a.w);
-    a.s *= f;
+    a.w = (double)f * fma((double)d, a.s, a.w);
+    a.s *= (double)f;
     a.m = m;
+}
+// A trip's logits, whose sums are one term of the lane's sums in double: beside a token that is nearly certain every other term is less
+// than half a unit of s as a float, and one after the other they would all be lost.  s in chains of at most four, so that a trip loses
+// little either.  A masked entry's 2^t is 0, and its t 2^t is 0 too and not 0 * -inf (2^-1000 is 0 already).
+template <int N>
+__device__ __forceinline__ void take(Stat &a, const float *x, float c)
+{
+    constexpr int CHAINS = N < 4 ? N : 4;
+    static_assert(CHAINS == 1 || CHAINS == 4, "");
+    float s[CHAINS], w;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+        const float t = (x[i] - a.m) * c, e = __builtin_amdgcn_exp2f(t), u = fmaxf(t, -1000.f);
+        s[i % CHAINS] = i < CHAINS ? e : s[i % CHAINS] + e;
+        w = i == 0 ? e * u : fmaf(e, u, w);
+    }
+    if constexpr (CHAINS == 4) s[0] = (s[0] + s[1]) + (s[2] + s[3]);
+    a.s += (double)s[0];
+    a.w += (double)w;
 }
 __device__ __forceinline__ Stat wave_merge(Stat a, float c)
 {
@@ -60,17 +78,14 @@ __device__ __forceinline__ Stat wave_merge(Stat a, float c)
     a.w = wave_sum(a.w);
     return a;
 }
+// The wavefronts' sums, one to a lane
 template <int W>
 __device__ __forceinline__ Stat merge_all(const Stat *p, float c)
 {
-    Stat a[W], r;
-    float m = p[0].m;
-#pragma unroll
-    for (int i = 0; i < W; ++i) { a[i] = p[i]; m = fmaxf(m, a[i].m); }
-    r = {m, 0.f, 0.f};
-#pragma unroll
-    for (int i = 0; i < W; ++i) { rescale(a[i], m, c); r.s += a[i].s; r.w += a[i].w; }
-    return r;
+    const int lane = threadIdx.x & 63;
+    Stat a = {LOWEST, 0.0, 0.0};
+    if (lane < W) a = p[lane];
+    return wave_merge(a, c);
 }
 
 struct LpArgs {
@@ -91,12 +106,12 @@ struct LpArgs {
 struct Done { float m, ls, entropy; bool empty; };
 __device__ __forceinline__ Done lp_done(const Stat &st)
 {
-    const float l2 = __log2f(st.s);
+    const float s = (float)st.s, rest = (float)(st.s - (double)s);             // (rest: where one token is certain, much of log s)
     Done r;
     r.m = st.m;
-    r.empty = st.s == 0.f;
-    r.ls = r.empty ? -INFINITY : LN2 * l2;
-    r.entropy = r.empty ? 0.f : LN2 * (l2 - st.w / st.s);
+    r.empty = st.s == 0.0;
+    r.ls = r.empty ? -INFINITY : logf(s) + rest / s;
+    r.entropy = r.empty ? 0.f : r.ls - LN2 * ((float)st.w / s);
     return r;
 }
 __device__ __forceinline__ float lp_of(const LpArgs &a, const Done &r, float x)
@@ -272,16 +287,15 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
         const Runs q = part.q = runs_of(part.p, part.count);
         part.body = part.p + q.head;
         part.rest = part.body + q.n * E;
-        Stat st = {LOWEST, 0.f, 0.f};
+        Stat st = {LOWEST, 0.0, 0.0};
         auto seen = [&](float top) {
             if (top > st.m) rescale(st, top, c);
         };
-        auto take = [&](float x) {
-            const float t = (x - st.m) * c, e = __builtin_amdgcn_exp2f(t);
-            st.s += e;
-            st.w = add_part(st.w, t, e);
+        auto one = [&](float x) {
+            seen(x);
+            take<1>(st, &x, c);
         };
-        if (tid < q.head) { seen((float)part.p[tid]); take((float)part.p[tid]); }
+        if (tid < q.head) one((float)part.p[tid]);
         int i = tid;
         for (; i + (U - 1) * THREADS < q.n; i += U * THREADS) {
             typedef typename Wide<T, E>::vec V;
@@ -289,21 +303,16 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
 #pragma unroll
             for (int v = 0; v < U; ++v) raw[v] = *(const V *)(part.body + (long long)(i + v * THREADS) * E);
             if (!TOP) __builtin_amdgcn_sched_barrier(0);       // or the second load waits for the first: 8192 bf16 rows of 32768 take 100 us then, 98 so
-            float x[U][E];
+            float x[U * E];
 #pragma unroll
             for (int v = 0; v < U; ++v)
 #pragma unroll
-                for (int u = 0; u < E; ++u) x[v][u] = (float)raw[v][u];
-            float top = x[0][0];
+                for (int u = 0; u < E; ++u) x[v * E + u] = (float)raw[v][u];
+            float top = x[0];
 #pragma unroll
-            for (int v = 0; v < U; ++v)
-#pragma unroll
-                for (int u = 0; u < E; ++u) top = fmaxf(top, x[v][u]);
+            for (int u = 1; u < U * E; ++u) top = fmaxf(top, x[u]);
             seen(top);
-#pragma unroll
-            for (int v = 0; v < U; ++v)
-#pragma unroll
-                for (int u = 0; u < E; ++u) take(x[v][u]);
+            take<U * E>(st, x, c);
         }
         for (; i < q.n; i += THREADS) {
             float x[E];
@@ -312,11 +321,10 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
 #pragma unroll
             for (int u = 1; u < E; ++u) top = fmaxf(top, x[u]);
             seen(top);
-#pragma unroll
-            for (int u = 0; u < E; ++u) take(x[u]);
+            take<E>(st, x, c);
         }
-        if (tid < q.tail) { seen((float)part.rest[tid]); take((float)part.rest[tid]); }
-        const float mine = st.s == 0.f ? -INFINITY : st.m;                     // (its own largest has 2^0 in s)
+        if (tid < q.tail) one((float)part.rest[tid]);
+        const float mine = st.s == 0.0 ? -INFINITY : st.m;                     // (its own largest has 2^0 in s)
         st = wave_merge(st, c);
         if (W > 1) {
             if ((tid & 63) == 0) red[tid >> 6] = st;
@@ -351,7 +359,7 @@ __global__ __launch_bounds__(64) void token_logprobs_join_kernel(LpArgs a)
     const int lane = threadIdx.x, n = a.splits * a.top;
     const float c = a.inv_t * LOG2E;
     for (long long row = blockIdx.x; row < a.rows; row += gridDim.x) {
-        Stat st = {LOWEST, 0.f, 0.f}, mine[S];
+        Stat st = {LOWEST, 0.0, 0.0}, mine[S];
         for (int i = lane; i < n; i += 8 * 64) {                   // eight loads in flight
             uint64_t key[8];
 #pragma unroll
