@@ -340,6 +340,8 @@ int qsr_adamw_destroy(qsr_adamw *a);
  *   s = x + residual (or x);  rstd = 1 / sqrt(mean(s^2) + eps);  y = s * rstd * weight_k
  * sum: s in the rows' type (may be x or residual itself), or NULL; rstd: [K * rows] floats, or NULL; y_type: the rows' type, or
  * QSR_TYPE_E4M3 with scale [K * rows], scale = max|y| / 448 of the row's finite entries, y = code * scale (a row of zeros has scale 0).
+ * Squares are floats: where mean(s^2) + eps is 0 as a float (a row of zeros, or of less than 1e-23, with eps = 0) rstd is 0, and so are y
+ * and the row's gradients; where it is infinite rstd is 0 too.
  * QSR_ELIMIT above d = 16384. */
 typedef struct {
     int32_t K, type, y_type;

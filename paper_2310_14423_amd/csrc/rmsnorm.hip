@@ -5,7 +5,8 @@
 //   row, scale = max|y| / 448 over the row's finite entries (for a product with scales by rows)
 // and backward, from h as it is kept, with u = dy w and dres what comes down the residual stream:
 //   dx = rstd (u - h rstd^2 mean(u h)) + dres  (the gradient of x and of res);  dw_k = sum over the worker's rows of dy h rstd
-// All arithmetic is fp32; y is taken from s before its rounding, which is in the registers anyway.
+// All arithmetic is fp32; y is taken from s before its rounding, which is in the registers anyway.  rstd is 0 where mean(s^2) + eps is 0
+// as a float.
 // Bound by memory: every row is read once and lies in the registers of its lanes until both passes over it are done.  bf16, with
 // residual: 8 x 12608 rows of 768 93 us, 6.7 TB/s, their gradients 108 us, 5.8 TB/s, and 5 us for the sums of the weights'; 16384 rows of
 // 4096 to e4m3 75 us, 6.3 TB/s.  fp32: 3 x 1001 rows of 1003 10.5 us, 4.6 TB/s, gradients 11.2 and 3.8.  Four rows: 2.6 us, latency.
@@ -190,7 +191,8 @@ __device__ __forceinline__ void rmsnorm_row(const RmsArgs &a, int k, long long r
     }
     q += lane < rest ? s.t * s.t : 0.f;
     if (a.sum != nullptr) store_row<T, L, W, NV, false>((T *)a.sum + row * a.s_sum, lane, a.d, s);
-    const float rstd = 1.f / sqrtf(group_sum<L, W>(q, red, 0) / (float)a.d + a.eps);
+    const float mean = group_sum<L, W>(q, red, 0) / (float)a.d + a.eps;
+    const float rstd = mean == 0.f ? 0.f : 1.f / sqrtf(mean);              // a row of zeros without eps: zeros, and no gradient
     if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
     float top = 0.f;
     each<T, NV>([&](float &y, float &f) {
