@@ -5,6 +5,7 @@
 // Arguments are those of the functions in operators.py, with the stream's address behind.  ValueError for what is checked here; a
 // code of the library's other than QSR_OK goes to the function that setup() was given, which raises.
 #include <ATen/core/Tensor.h>
+#include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -27,6 +28,15 @@ const at::Tensor &tensor(PyObject *o, const char *what)
     return THPVariable_Unpack(o);
 }
 const at::Tensor *maybe(PyObject *o, const char *what) { return o == Py_None ? nullptr : &tensor(o, what); }
+
+// No graph is recorded here: a tensor that asks for a gradient is not taken as one that does not
+void unrecorded(std::initializer_list<const at::Tensor *> ts)
+{
+    if (!at::GradMode::is_enabled()) return;
+    for (const at::Tensor *t : ts)
+        need(t == nullptr || !t->requires_grad(),
+             "a tensor requires a gradient, and no graph is recorded here: call with detached tensors or under torch.no_grad(), and the backward function by hand");
+}
 
 int type_of(const at::Tensor &t, const char *what)
 {
@@ -135,6 +145,7 @@ PyObject *rmsnorm(PyObject *, PyObject *const *o, Py_ssize_t n)
         const at::Tensor &x = tensor(o[0], "x"), &w = tensor(o[1], "weight");
         const at::Tensor *res = maybe(o[2], "residual"), *out = maybe(o[5], "sum_out");
         const bool fp8 = o[4] == Py_True;
+        unrecorded({&x, &w, res, out});
         qsr_rmsnorm_args a{};
         a.type = type_of(x, "x: float32 or bfloat16");
         a.y_type = fp8 ? QSR_TYPE_E4M3 : a.type;
@@ -166,6 +177,7 @@ PyObject *rmsnorm_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
     return guarded(n, 6, [&] {
         const at::Tensor &dy = tensor(o[0], "y_grad"), &h = tensor(o[1], "sum"), &w = tensor(o[2], "weight"), &rstd = tensor(o[3], "rstd");
         const at::Tensor *res = maybe(o[4], "residual_grad");
+        unrecorded({&dy, &h, &w, &rstd, res});
         qsr_rmsnorm_backward_args a{};
         a.type = type_of(h, "sum: float32 or bfloat16");
         workers(h, w, a.K, a.rows, a.weight_stride);
@@ -201,6 +213,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *o, Py_ssize_t n)
 {
     return guarded(n, 5, [&] {
         const at::Tensor &x = tensor(o[0], "logits"), &tok = tensor(o[1], "tokens");
+        unrecorded({&x});
         qsr_token_logprobs_args a{};
         a.type = type_of(x, "logits: float32 or bfloat16");
         tokens_ok(x, tok);
@@ -241,6 +254,8 @@ PyObject *token_logprobs_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
     return guarded(n, 9, [&] {
         const at::Tensor &x = tensor(o[0], "logits"), &tok = tensor(o[1], "tokens");
         const at::Tensor *ga = maybe(o[4], "logp_grad"), *gb = maybe(o[5], "entropy_grad"), *out = maybe(o[7], "out");
+        const at::Tensor &stats = tensor(o[2], "stats"), &entropy = tensor(o[3], "entropy");
+        unrecorded({&x, &stats, &entropy, ga, gb, out});
         qsr_token_logprobs_backward_args a{};
         a.type = type_of(x, "logits: float32 or bfloat16");
         tokens_ok(x, tok);
@@ -251,8 +266,8 @@ PyObject *token_logprobs_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
         a.stride = row_stride(x, "logits: rows with one stride, their elements side by side");
         a.logits = x.const_data_ptr();
         a.tokens = (const int64_t *)tok.const_data_ptr();
-        a.stats = numbers(tensor(o[2], "stats"), x, 2, "stats: contiguous float32 [..., 2]");
-        a.entropy = numbers(tensor(o[3], "entropy"), x, 0, "entropy: contiguous float32, one for each row");
+        a.stats = numbers(stats, x, 2, "stats: contiguous float32 [..., 2]");
+        a.entropy = numbers(entropy, x, 0, "entropy: contiguous float32, one for each row");
         if (ga) a.logp_grad = numbers(*ga, x, 0, "logp_grad: contiguous float32, one for each row");
         if (gb) a.entropy_grad = numbers(*gb, x, 0, "entropy_grad: contiguous float32, one for each row");
         at::Tensor grad = out ? *out : new_like(x, x.scalar_type());

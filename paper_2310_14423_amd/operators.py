@@ -5,6 +5,8 @@ As in the binding, this is marshalling and the allocation of results and workspa
 model makes in every step go through a small extension (csrc/torch_calls.cpp), the others through ctypes.  All of them work on the
 current stream of the tensors' device, or on `stream` (a stream's address), which then also owns what they allocate.
 Shapes and types are checked here (ValueError), everything else in the library (QSRError).
+None of them records a graph for automatic differentiation: the backward functions are called by hand, and where gradients are being
+recorded a tensor that requires one is refused (ValueError) instead of being taken without it.
 """
 import ctypes as C
 from collections import namedtuple
