@@ -38,6 +38,12 @@ void unrecorded(std::initializer_list<const at::Tensor *> ts)
              "a tensor requires a gradient, and no graph is recorded here: call with detached tensors or under torch.no_grad(), and the backward function by hand");
 }
 
+// A tensor that was written in place has a new version (tensors of inference mode have none), by which graphs that kept it find out
+void written(const at::Tensor &t)
+{
+    if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+}
+
 int type_of(const at::Tensor &t, const char *what)
 {
     const at::ScalarType s = t.scalar_type();
@@ -164,6 +170,7 @@ PyObject *rmsnorm(PyObject *, PyObject *const *o, Py_ssize_t n)
         a.y = y.mutable_data_ptr();
         a.rstd = (float *)rstd.mutable_data_ptr();
         check(qsr_rmsnorm(&a, stream_of(o[6])), "qsr_rmsnorm");
+        if (out) written(*out);
         PyObject *s;
         if (sum.defined() && !out) s = wrap(std::move(sum));
         else { s = out ? o[5] : o[0]; Py_INCREF(s); }
@@ -274,20 +281,22 @@ PyObject *token_logprobs_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
         a.grad = grad.mutable_data_ptr();
         a.grad_stride = like(grad, x, "out: as logits");
         check(qsr_token_logprobs_backward(&a, stream_of(o[8])), "qsr_token_logprobs_backward");
-        if (out) { Py_INCREF(o[7]); return o[7]; }
+        if (out) { written(*out); Py_INCREF(o[7]); return o[7]; }
         return wrap(std::move(grad));
     });
 }
 
-// handle, t, eta, stream
+// handle, t, eta, stream, a tuple of the tensors that it writes
 PyObject *adamw_step(PyObject *, PyObject *const *o, Py_ssize_t n)
 {
-    return guarded(n, 4, [&] {
+    return guarded(n, 5, [&] {
+        need(PyTuple_Check(o[4]), "a tuple of tensors");
         qsr_adamw *const a = (qsr_adamw *)PyLong_AsVoidPtr(o[0]);
         const long long t = PyLong_AsLongLong(o[1]);
         const double eta = PyFloat_AsDouble(o[2]);
         if (PyErr_Occurred()) throw Failed{};
         check(qsr_adamw_step(a, t, eta, stream_of(o[3])), "qsr_adamw_step");
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(o[4]); ++i) written(tensor(PyTuple_GET_ITEM(o[4], i), "a tuple of tensors"));
         return none();
     });
 }

@@ -198,6 +198,9 @@ class AdamW:
                       "moments[%r]: %s [K][size], rows dense" % (name, dt))
             setattr(self, name, got)
         self.params, self.grads, self.copies = params, grads, copies
+        # what a step writes: one tensor for each buffer, since views have their buffer's version
+        wrote = params + (copies or []) + self.m + self.v + (self.m_scale or []) + (self.v_scale or [])
+        self._written = tuple({id(t): t for t in (t._base if t._is_view() else t for t in wrote)}.values())
         stride = lambda t: t.stride(0)  # noqa: E731
         pairs = [(self.m, self.v)] + ([(self.m_scale, self.v_scale)] if states == "fp8" else [])
         _need(all(a.stride(0) == b.stride(0) for m, v in pairs for a, b in zip(m, v)), "moments: m and v with the same strides")
@@ -225,7 +228,7 @@ class AdamW:
         """One step of all workers with learning rate eta; t = steps taken before."""
         s, place = _place(self.params[0], stream)
         with place or _nothing:
-            _calls.adamw_step(self._handle.value, t, eta, s)
+            _calls.adamw_step(self._handle.value, t, eta, s, self._written)
 
     def set_grads(self, grads, stream=None):
         """Other tensors for the gradients, of the same type and strides, from the next step on."""

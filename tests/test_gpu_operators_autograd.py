@@ -48,3 +48,52 @@ def test_parameters_that_want_gradients_are_updated():
     for params in (p, q):
         qsr.AdamW(params, g).step(1e-2, 0)
     assert all(torch.equal(a, b) and a.requires_grad for a, b in zip(p, q)) and float(q[0][0, 0].detach()) < 1
+
+
+def test_results_in_place_are_new_versions():
+    """What is written in place counts as written: a graph that has kept the tensor finds out in its backward pass."""
+    g = torch.Generator().manual_seed(2)
+    x, w, tok = torch.randn(4, 32, generator=g).cuda(), torch.ones(32, device="cuda"), torch.zeros(4, dtype=torch.int64, device="cuda")
+    t = qsr.token_logprobs(x, tok)
+
+    def norm(out):
+        qsr.rmsnorm(x, w, residual=x, sum_out=out)
+
+    def logits(out):
+        qsr.token_logprobs_backward(x, tok, t.stats, t.entropy, t.logp, out=out)
+    for write in (norm, logits):
+        for out in (torch.randn(4, 32, device="cuda"), torch.randn(4, 40, device="cuda")[:, 3:35]):
+            a = torch.ones(4, 32, device="cuda", requires_grad=True)
+            kept, before = (a * out).sum(), out._version
+            write(out)
+            assert out._version > before
+            with pytest.raises(RuntimeError, match="inplace"):
+                kept.backward()
+
+
+@pytest.mark.parametrize("states", ["f32", "fp8"])
+def test_steps_are_new_versions(states):
+    """Parameters, copies and moments of a step, as tensors of their own or as views of one buffer; gradients are only read."""
+    flat = torch.zeros(2, 60, device="cuda")
+    for p in ([torch.zeros(2, 40, device="cuda"), torch.zeros(2, 3, device="cuda")], [flat[:, :40], flat[:, 44:47]]):
+        grads, copies = [torch.ones_like(x) for x in p], [x.to(torch.bfloat16) for x in p]
+        opt = qsr.AdamW(p, grads, states=states, copies=copies)
+        written = p + copies + opt.m + opt.v + (opt.m_scale + opt.v_scale if states == "fp8" else [])
+        for t in range(2):
+            before, read = [x._version for x in written], [x._version for x in grads]
+            a = torch.ones_like(p[1], requires_grad=True)
+            kept = (a * p[1]).sum()
+            opt.step(1e-2, t)
+            assert all(x._version > v for x, v in zip(written, before)) and [x._version for x in grads] == read
+            with pytest.raises(RuntimeError, match="inplace"):
+                kept.backward()
+
+
+def test_tensors_of_inference_have_no_versions():
+    with torch.inference_mode():
+        x, w, p = torch.randn(4, 32, device="cuda"), torch.ones(32, device="cuda"), torch.zeros(1, 5, device="cuda")
+        f = qsr.rmsnorm(x, w, residual=x, sum_out=x)
+        opt = qsr.AdamW([p], [torch.ones_like(p)])
+        opt.step(1e-2, 0)
+    opt.step(1e-2, 1)
+    assert f.sum is x and bool(p.lt(0).all())
