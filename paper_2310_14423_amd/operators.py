@@ -59,7 +59,9 @@ def _place(t, stream):
     if not here:
         stack.enter_context(torch.cuda.device(index))
     if stream is not None and stream != now:
-        stack.enter_context(torch.cuda.stream(torch.cuda.ExternalStream(stream, device=t.device)))
+        # (an ExternalStream at address 0 would be some other stream, and own what the default stream writes)
+        side = torch.cuda.ExternalStream(stream, device=t.device) if stream else torch.cuda.default_stream(t.device)
+        stack.enter_context(torch.cuda.stream(side))
     return (now if stream is None else stream), stack
 
 
