@@ -40,7 +40,10 @@ def _setup():
     global _torch, _calls
     import torch
     lib()               # fails loudly if nothing is built
-    from . import _calls as calls
+    try:
+        from . import _calls as calls
+    except ImportError as e:
+        raise RuntimeError("the operators' extension cannot be loaded: run `python -m paper_2310_14423_amd.build` (%s)" % e) from e
     calls.setup(_check, RMSNorm, TokenLogprobs)
     _torch, _calls = torch, calls
 
