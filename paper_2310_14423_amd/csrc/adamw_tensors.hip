@@ -20,6 +20,7 @@
 // A root above zero does not become zero (the smallest code instead): m / r of the next step stays bounded.
 // The random words: a 32-bit multiply-xorshift mix (constants from C. Wellons' search for mixes of low bias) of the element's index,
 // counted over the padded blocks of all tensors (modulo 2^32), and the step's key; 16 bits for each of the two moments.
+#include <algorithm>
 #include <cmath>
 #include <cstring>
 #include <new>
@@ -381,6 +382,17 @@ struct qsr_adamw {
 
 static bool unaligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
+// One address in two tensors of the list: two wavefronts would update the same elements at once
+static bool given_twice(const qsr_adamw_config *c, const void *(*address)(const qsr_tensor &))
+{
+    std::vector<uintptr_t> at;
+    at.reserve((size_t)c->n_tensors);
+    for (int i = 0; i < c->n_tensors; ++i)
+        if (address(c->tensors[i])) at.push_back((uintptr_t)address(c->tensors[i]));
+    std::sort(at.begin(), at.end());
+    return std::adjacent_find(at.begin(), at.end()) != at.end();
+}
+
 extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
 {
     const char *w = nullptr;
@@ -412,6 +424,18 @@ extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
         else if (!finite_ge0(t.weight_decay)) w = "a tensor's weight_decay";
     }
     if (!w && blocks > ((long long)1 << 26)) w = "tensors (above 2^34 elements together)";     // the grid's limit of 2^32 threads
+    if (!w) {
+        try {
+            if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.param; })) w = "a tensor's param (given twice)";
+            else if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.m; })) w = "a tensor's m (given twice)";
+            else if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.v; })) w = "a tensor's v (given twice)";
+            else if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.copy; })) w = "a tensor's copy (given twice)";
+            else if (fp8 && given_twice(c, [](const qsr_tensor &t) -> const void * { return t.m_scale; })) w = "a tensor's m_scale (given twice)";
+            else if (fp8 && given_twice(c, [](const qsr_tensor &t) -> const void * { return t.v_scale; })) w = "a tensor's v_scale (given twice)";
+        } catch (...) {
+            w = "tensors (the host's memory does not hold their addresses)";
+        }
+    }
     if (why) *why = w ? w : "ok";
     return w ? QSR_EINVAL : QSR_OK;
 }

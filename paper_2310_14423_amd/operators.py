@@ -155,6 +155,7 @@ class AdamW:
 
     grads: the gradients' tensors, float32 or bfloat16, read by every step (set_grads: other ones from then on).
     states: "f32" or "fp8" (moments in 8 bits: e4m3 codes in blocks of 256 elements with a scale, of m and of the root of v).
+    params: each of them once, also where a model uses one in two places.
     copies: bfloat16 tensors that get a copy of the new parameters, or None.
     weight_decay: one number, or one for each tensor.  clip_norm > 0: clipping by global norm over all tensors of a worker.
     moments: {"m": [...], "v": [...]} and with "fp8" also "m_scale", "v_scale" to go on with; zeros otherwise.  "f32": float32

@@ -1,9 +1,11 @@
-"""The Python side of the operators without a GPU: the streams that it works on."""
+"""The operators' calls without a GPU: the streams that the Python side works on, and lists that name a tensor twice."""
 import contextlib
+import ctypes as C
 import types
 
 import pytest
 
+import paper_2310_14423_amd as qsr
 import paper_2310_14423_amd.operators as ops
 
 
@@ -40,3 +42,29 @@ def test_streams(stream, want, device, monkeypatch):
         pass
     assert [x for x in log if x[0] != "device"] == ([want] if want else []) and [x for x in log if x[0] == "device"] == ([("device", 1)] if device == 0 else [])
     assert (place is None) == (not log)
+
+
+def _list(n, state_type, **same):
+    """n tensors of 300 elements for two workers at addresses of their own, but for those that are said to be the first one's."""
+    arr = (ops.Tensor * n)()
+    for i in range(n):
+        t = arr[i]
+        for j, name in enumerate(("param", "grad", "m", "v", "m_scale", "v_scale", "copy")):
+            setattr(t, name, ((j + 1) << 32) + 8192 * (0 if same.get(name) == i else i))
+        t.n, t.param_stride, t.grad_stride, t.state_stride, t.scale_stride, t.copy_stride = 300, 300, 300, 512, 2, 300
+    return ops.AdamWConfig(K=2, n_tensors=n, grad_type=0, state_type=state_type, beta1=0.9, beta2=0.999, eps=1e-8, clip_norm=0.0, seed=0,
+                           tensors=arr), arr
+
+
+@pytest.mark.parametrize("state_type", [0, 2])
+@pytest.mark.parametrize("name,refused", [("param", True), ("m", True), ("v", True), ("copy", True), ("m_scale", None), ("v_scale", None), ("grad", False)])
+def test_tensors_named_twice(name, refused, state_type):
+    """What a step writes is refused (scales only where there are any); gradients are only read."""
+    refused = state_type == 2 if refused is None else refused
+    for n, again in ((2, 1), (5, 3), (300, 299)):
+        cfg, keep = _list(n, state_type, **{name: again})
+        why = C.c_char_p()
+        rc = qsr.lib().qsr_adamw_validate(C.byref(cfg), C.byref(why))
+        assert rc == (-1 if refused else 0) and (not refused or (name + " (given twice)") in why.value.decode())
+        cfg, keep = _list(n, state_type)
+        assert qsr.lib().qsr_adamw_validate(C.byref(cfg), None) == 0
