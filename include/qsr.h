@@ -385,7 +385,7 @@ typedef struct {
     int32_t type, top;
     const void *logits;
     const int64_t *tokens;    /* [rows] */
-    double temperature;       /* > 0 */
+    double temperature;       /* > 0, with log2(e) / temperature in the range of floats */
     float *logp, *entropy, *lse, *stats;
     float *top_logp;          /* [rows][top] */
     int32_t *top_id;          /* [rows][top] */

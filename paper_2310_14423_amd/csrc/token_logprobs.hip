@@ -523,6 +523,14 @@ static bool type_ok(int type) { return type == QSR_TYPE_F32 || type == QSR_TYPE_
 static uintptr_t size_of(int type) { return type == QSR_TYPE_F32 ? 4 : 2; }
 static bool sizes_ok(int64_t rows, int64_t V) { return rows >= 0 && rows <= ((long long)1 << 31) && V >= 1 && V <= (1 << 30); }
 
+// 1 / T as a float; of use where log2(e) / T is one as well
+static bool inverse(double temperature, float &inv_t)
+{
+    if (!(std::isfinite(temperature) && temperature > 0.0)) return false;
+    inv_t = (float)(1.0 / temperature);
+    return inv_t > 0.f && inv_t * LOG2E < INFINITY;
+}
+
 extern "C" int qsr_token_logprobs_workspace_bytes(int64_t rows, int64_t vocab, int32_t type, int32_t top, size_t *bytes)
 {
     if (!bytes) return QSR_EINVAL;
@@ -541,9 +549,8 @@ extern "C" int qsr_token_logprobs(const qsr_token_logprobs_args *q, void *worksp
     size_t need = 0;
     const int rc = qsr_token_logprobs_workspace_bytes(q->rows, q->vocab, q->type, q->top, &need);
     if (rc != QSR_OK) return rc;
-    if (!(std::isfinite(q->temperature) && q->temperature > 0.0)) return QSR_EINVAL;
-    const float inv_t = (float)(1.0 / q->temperature);
-    if (!(inv_t > 0.f && inv_t < INFINITY) || q->stride < q->vocab) return QSR_EINVAL;
+    float inv_t;
+    if (!inverse(q->temperature, inv_t) || q->stride < q->vocab) return QSR_EINVAL;
     if (q->rows == 0) return QSR_OK;
     if (!q->logits || off(q->logits, size_of(q->type)) || off(q->tokens, 8) || off(q->logp, 4) || off(q->entropy, 4) || off(q->lse, 4) || off(q->stats, 4))
         return QSR_EINVAL;
@@ -562,9 +569,8 @@ extern "C" int qsr_token_logprobs(const qsr_token_logprobs_args *q, void *worksp
 extern "C" int qsr_token_logprobs_backward(const qsr_token_logprobs_backward_args *q, void *stream)
 {
     if (!q || !sizes_ok(q->rows, q->vocab) || !type_ok(q->type)) return QSR_EINVAL;
-    if (!(std::isfinite(q->temperature) && q->temperature > 0.0)) return QSR_EINVAL;
-    const float inv_t = (float)(1.0 / q->temperature);
-    if (!(inv_t > 0.f && inv_t < INFINITY) || q->stride < q->vocab || q->grad_stride < q->vocab) return QSR_EINVAL;
+    float inv_t;
+    if (!inverse(q->temperature, inv_t) || q->stride < q->vocab || q->grad_stride < q->vocab) return QSR_EINVAL;
     if (q->rows == 0) return QSR_OK;
     const uintptr_t es = size_of(q->type);
     if (!q->logits || off(q->logits, es) || !q->grad || off(q->grad, es) || off(q->tokens, 8) || !q->stats || off(q->stats, 4) ||

@@ -68,3 +68,16 @@ def test_tensors_named_twice(name, refused, state_type):
         assert rc == (-1 if refused else 0) and (not refused or (name + " (given twice)") in why.value.decode())
         cfg, keep = _list(n, state_type)
         assert qsr.lib().qsr_adamw_validate(C.byref(cfg), None) == 0
+
+
+@pytest.mark.parametrize("T,code", [(1e-30, 0), (4.3e-39, 0), (4.2e-39, -1), (3e-39, -1), (1e38, 0)])
+def test_temperatures(T, code):
+    """Exponents are to the base 2: log2(e) / T has to be a float, not only 1 / T, or the largest logit's 0 * inf is NaN.  (No rows:
+    nothing is launched on what is accepted.)"""
+    from operators_abi import TokenLogprobsArgs, TokenLogprobsBackwardArgs
+    P = 1 << 20
+    a = dict(rows=0, vocab=100, stride=100, type=0, logits=P, tokens=P, temperature=T, entropy=P, stats=P)
+    f = TokenLogprobsArgs(top=0, logp=P, lse=P, **a)
+    assert qsr.lib().qsr_token_logprobs(C.byref(f), None, C.c_size_t(0), None) == code
+    b = TokenLogprobsBackwardArgs(grad=P, grad_stride=100, logp_grad=P, entropy_grad=P, **a)
+    assert qsr.lib().qsr_token_logprobs_backward(C.byref(b), None) == code
