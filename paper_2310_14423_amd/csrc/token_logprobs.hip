@@ -191,7 +191,9 @@ __device__ __forceinline__ float top_bound(const float *group, int top)
 // The `top` largest keys of a part to se.best, 0 where it has fewer elements.  mine: the lane's largest logit, -inf if all are masked.
 // The `top`-th largest of 64 groups' maxima is a bound: that many logits reach it, and only lanes whose own maximum does have any that
 // do.  Their logits alone are looked at again, shared out among all lanes, and those from the bound on are put in order.  Entries of
-// -inf are left out of this; where too few others are there, the first of them follow.
+// -inf are left out of this; where too few others are there, the first of them follow.  More than the list holds (many equal logits, or
+// few tokens left by masks of the lowest value, which then are the bound) are found by `top` passes over the part: 1001 fp32 rows of
+// 50021 with 5 alternatives 277 us, 36 with masks of -inf or few masks.
 template <typename T, int THREADS>
 __device__ __forceinline__ void find_top(const Part<T> &a, float mine, int top, Search<THREADS> &se)
 {
@@ -302,7 +304,7 @@ __global__ __launch_bounds__(THREADS, 8) void token_logprobs_kernel(LpArgs a)
             V raw[U];
 #pragma unroll
             for (int v = 0; v < U; ++v) raw[v] = *(const V *)(part.body + (long long)(i + v * THREADS) * E);
-            if (!TOP) __builtin_amdgcn_sched_barrier(0);       // or the second load waits for the first: 8192 bf16 rows of 32768 take 100 us then, 98 so
+            if (!TOP) __builtin_amdgcn_sched_barrier(0);       // or the second load waits for the first: 8192 bf16 rows of 32768 take 2 to 4 us more of 100 then
             float x[U * E];
 #pragma unroll
             for (int v = 0; v < U; ++v)
