@@ -300,7 +300,7 @@ enum {
  *          (state_stride a multiple of 4, rows 4-byte aligned), and as many scales as blocks.  Rounding is stochastic, from `seed`,
  *          the number of the step and the element's place in the list, the same on every run.  What is not finite is stored as NaN.
  * The caller zeroes the moments (and scales) for a new run or restores them.  What a step writes belongs to one tensor of the list alone:
- * parameters that a model uses twice are given once, and the same address twice is refused. */
+ * parameters that a model uses twice are given once, and memory that two tensors share is refused. */
 typedef struct {
     float *param;
     const void *grad;

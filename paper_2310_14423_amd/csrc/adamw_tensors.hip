@@ -382,15 +382,21 @@ struct qsr_adamw {
 
 static bool unaligned(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
 
-// One address in two tensors of the list: two wavefronts would update the same elements at once
-static bool given_twice(const qsr_adamw_config *c, const void *(*address)(const qsr_tensor &))
+// Two tensors of the list that share memory of one kind (in the first worker's rows): two wavefronts would update the same elements at
+// once.  of: where a tensor's memory begins and how many bytes a row of it has.
+struct AtRange { uintptr_t at, bytes; };
+template <typename F> static bool shared(const qsr_adamw_config *c, F of)
 {
-    std::vector<uintptr_t> at;
-    at.reserve((size_t)c->n_tensors);
-    for (int i = 0; i < c->n_tensors; ++i)
-        if (address(c->tensors[i])) at.push_back((uintptr_t)address(c->tensors[i]));
-    std::sort(at.begin(), at.end());
-    return std::adjacent_find(at.begin(), at.end()) != at.end();
+    std::vector<AtRange> ranges;
+    ranges.reserve((size_t)c->n_tensors);
+    for (int i = 0; i < c->n_tensors; ++i) {
+        const AtRange r = of(c->tensors[i]);
+        if (r.at) ranges.push_back(r);
+    }
+    std::sort(ranges.begin(), ranges.end(), [](const AtRange &x, const AtRange &y) { return x.at < y.at; });
+    for (size_t i = 1; i < ranges.size(); ++i)
+        if (ranges[i].at - ranges[i - 1].at < ranges[i - 1].bytes) return true;
+    return false;
 }
 
 extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
@@ -426,12 +432,16 @@ extern "C" int qsr_adamw_validate(const qsr_adamw_config *c, const char **why)
     if (!w && blocks > ((long long)1 << 26)) w = "tensors (above 2^34 elements together)";     // the grid's limit of 2^32 threads
     if (!w) {
         try {
-            if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.param; })) w = "a tensor's param (given twice)";
-            else if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.m; })) w = "a tensor's m (given twice)";
-            else if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.v; })) w = "a tensor's v (given twice)";
-            else if (given_twice(c, [](const qsr_tensor &t) -> const void * { return t.copy; })) w = "a tensor's copy (given twice)";
-            else if (fp8 && given_twice(c, [](const qsr_tensor &t) -> const void * { return t.m_scale; })) w = "a tensor's m_scale (given twice)";
-            else if (fp8 && given_twice(c, [](const qsr_tensor &t) -> const void * { return t.v_scale; })) w = "a tensor's v_scale (given twice)";
+            auto numbers = [](const void *p, long long n, int size) { return AtRange{(uintptr_t)p, (uintptr_t)n * (uintptr_t)size}; };
+            auto padded = [](long long n) { return (n + AT_BLOCK - 1) / AT_BLOCK * AT_BLOCK; };
+            auto state = [&](const void *p, long long n) { return fp8 ? numbers(p, padded(n), 1) : numbers(p, n, 4); };
+            auto scales = [&](const void *p, long long n) { return fp8 ? numbers(p, padded(n) / AT_BLOCK, 4) : AtRange{0, 0}; };
+            if (shared(c, [&](const qsr_tensor &t) { return numbers(t.param, t.n, 4); })) w = "a tensor's param (given twice)";
+            else if (shared(c, [&](const qsr_tensor &t) { return state(t.m, t.n); })) w = "a tensor's m (given twice)";
+            else if (shared(c, [&](const qsr_tensor &t) { return state(t.v, t.n); })) w = "a tensor's v (given twice)";
+            else if (shared(c, [&](const qsr_tensor &t) { return numbers(t.copy, t.n, 2); })) w = "a tensor's copy (given twice)";
+            else if (shared(c, [&](const qsr_tensor &t) { return scales(t.m_scale, t.n); })) w = "a tensor's m_scale (given twice)";
+            else if (shared(c, [&](const qsr_tensor &t) { return scales(t.v_scale, t.n); })) w = "a tensor's v_scale (given twice)";
         } catch (...) {
             w = "tensors (the host's memory does not hold their addresses)";
         }

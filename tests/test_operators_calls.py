@@ -81,3 +81,14 @@ def test_temperatures(T, code):
     assert qsr.lib().qsr_token_logprobs(C.byref(f), None, C.c_size_t(0), None) == code
     b = TokenLogprobsBackwardArgs(grad=P, grad_stride=100, logp_grad=P, entropy_grad=P, **a)
     assert qsr.lib().qsr_token_logprobs_backward(C.byref(b), None) == code
+
+
+@pytest.mark.parametrize("state_type", [0, 2])
+def test_tensors_that_overlap(state_type):
+    """Tensors side by side are taken, ones that share an element are not: for every kind at its own size of a row."""
+    for name, row in (("param", 1200), ("m", 512 if state_type == 2 else 1200), ("v", 512 if state_type == 2 else 1200), ("copy", 600)) + \
+            ((("m_scale", 8), ("v_scale", 8)) if state_type == 2 else ()):
+        for off, want in ((row, 0), (row - (2 if name == "copy" else 4), -1), (4, -1)):
+            cfg, arr = _list(3, state_type)
+            setattr(arr[2], name, getattr(arr[0], name) + off)
+            assert qsr.lib().qsr_adamw_validate(C.byref(cfg), None) == want, (name, off)
