@@ -4,6 +4,7 @@ the residual's addition, and the log probabilities of given tokens, each with it
 As in the binding, this is marshalling and the allocation of results and workspaces; nothing is computed in torch.  The calls that a
 model makes in every step go through a small extension (csrc/torch_calls.cpp), the others through ctypes.  All of them work on the
 current stream of the tensors' device, or on `stream` (a stream's address), which then also owns what they allocate.
+Arguments that another stream owns have to be ready, and to be kept until the work is done, as for any of torch's own calls.
 Shapes and types are checked here (ValueError), everything else in the library (QSRError).
 None of them records a graph for automatic differentiation: the backward functions are called by hand, and where gradients are being
 recorded a tensor that requires one is refused (ValueError) instead of being taken without it.
