@@ -372,6 +372,112 @@ typedef struct {
 int qsr_rmsnorm_workspace_bytes(int32_t K, int64_t rows, int64_t d, int32_t type, size_t *bytes);
 int qsr_rmsnorm_backward(const qsr_rmsnorm_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);
 
+/* Layer norm of rows of d elements with the residual's addition; worker k owns rows k * rows .. (k + 1) * rows - 1:
+ *   s = x + residual (or x);  rstd = 1 / sqrt(mean((s - mean(s))^2) + eps);  y = (s - mean) * rstd * weight_k + bias_k
+ * bias, sum, mean, rstd and y_type as in qsr_rmsnorm: bias may be NULL (none), sum is s in the rows' type (may be x or residual itself)
+ * or NULL, mean and rstd are [K * rows] floats or NULL, y_type is the rows' type, or QSR_TYPE_E4M3 with scale [K * rows], scale = max|y| / 448 of
+ * the row's finite entries.  Where mean((s - mean)^2) + eps is 0 as a float (a row of equal numbers, with eps = 0) rstd is 0, y is
+ * the bias and the row has no gradient; where it is infinite rstd is 0 too.  A row with a NaN or an infinity has NaN for all of y.
+ * QSR_ELIMIT above d = 16384. */
+typedef struct {
+    int32_t K, type, y_type;
+    int64_t rows, d;          /* rows of a worker, >= 0 */
+    const void *x, *residual; /* residual may be NULL */
+    const float *weight, *bias; /* [K][d], rows weight_stride and bias_stride apart */
+    void *sum, *y;
+    float *scale, *mean, *rstd;
+    int64_t x_stride, residual_stride, sum_stride, y_stride; /* from row to row, >= d */
+    int64_t weight_stride, bias_stride; /* from worker to worker, >= d; read only where K > 1 */
+    double eps;
+} qsr_layernorm_args;
+int qsr_layernorm(const qsr_layernorm_args *args, void *stream);
+
+/* Its gradients, from s as it was kept: x_grad (of x and of residual alike), weight_grad and, unless it is NULL, bias_grad, [K][d] without
+ * gaps (overwritten; sums in a fixed order).  residual_grad: what comes down the residual stream, added to x_grad, or NULL. */
+typedef struct {
+    int32_t K, type;
+    int64_t rows, d;
+    const void *y_grad, *sum;
+    const float *weight, *mean, *rstd;
+    const void *residual_grad;
+    void *x_grad;
+    float *weight_grad, *bias_grad;
+    int64_t y_grad_stride, sum_stride, residual_grad_stride, x_grad_stride, weight_stride;
+} qsr_layernorm_backward_args;
+int qsr_layernorm_workspace_bytes(int32_t K, int64_t rows, int64_t d, int32_t type, size_t *bytes);
+int qsr_layernorm_backward(const qsr_layernorm_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Rows of K workers' tables by tokens: y_i = scale * table_k[token_i], worker k's tokens being k * tokens_each .. (k + 1) * tokens_each - 1.
+ * A token outside 0..vocab-1 stands for none: a row of zeros.  type: the table's, y_type: either of QSR_TYPE_F32 and QSR_TYPE_BF16.
+ * QSR_ELIMIT above 2^27 tokens of a worker. */
+typedef struct {
+    int32_t K, type, y_type, reserved;
+    int64_t tokens_each, vocab, d; /* d at most 2^22 */
+    const void *table;        /* [K][vocab][d], rows table_stride apart, workers worker_stride (read only where K > 1) */
+    const int64_t *tokens;    /* [K][tokens_each] */
+    void *y;
+    int64_t table_stride, worker_stride, y_stride;
+    double scale;
+} qsr_embedding_args;
+int qsr_embedding(const qsr_embedding_args *args, void *stream);
+
+/* Its gradient: grad_k[v] = scale * sum of y_grad_i over the worker's tokens v, all of the table (0 for rows that no token names), or,
+ * with accumulate = 1, added to what grad holds in the rows that tokens name, the others left as they are.  Sums are floats in a fixed
+ * order, rounded once to grad_type.  type: y_grad's.  The workspace is 16-byte aligned. */
+typedef struct {
+    int32_t K, type, grad_type, accumulate;
+    int64_t tokens_each, vocab, d;
+    const void *y_grad;       /* rows y_grad_stride apart */
+    const int64_t *tokens;
+    void *grad;
+    int64_t y_grad_stride, grad_stride, worker_stride; /* worker_stride read only where K > 1; a table for each worker */
+    double scale;
+} qsr_embedding_backward_args;
+int qsr_embedding_workspace_bytes(int32_t K, int64_t tokens_each, int64_t vocab, int64_t d, int32_t type, size_t *bytes);
+int qsr_embedding_backward(const qsr_embedding_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* A gated linear recurrence over `batch` sequences of `steps` steps, for each of d channels by itself, with a_t = sigmoid(gate_t):
+ *   h_t = a_t * h_{t-1} + (1 - a_t) * x_t (QSR_SCAN_COMPLEMENT), or a_t * h_{t-1} + x_t (QSR_SCAN_PLAIN);  h_{-1} = initial
+ * State and arithmetic are float; h is the state in x's type.  initial: [batch][d] floats, or NULL (0).  last: [batch][d], the state behind a
+ * sequence's last step, or NULL; may be initial itself.  A step with a nonzero reset takes no state from before it.  lengths: steps of a sequence that
+ * there are (less than 0 is none, more than `steps` is all); x and gate behind them are not read, h behind them is 0, last is the
+ * state at the end.  states: [batch][ceil(steps / QSR_SCAN_STEPS)][d] floats for the backward pass, the state that every
+ * QSR_SCAN_STEPS-th step begins with, or NULL.  reset, lengths: without gaps.  The rows of h share no element, with each other or with
+ * x and gate.  steps at most 2^30, d at most 2^28 (QSR_ELIMIT). */
+enum { QSR_SCAN_STEPS = 16 };
+enum { QSR_SCAN_COMPLEMENT = 0, QSR_SCAN_PLAIN = 1 };
+typedef struct {
+    int32_t type, input;
+    int64_t batch, steps, d;
+    const void *x, *gate;
+    const float *initial;
+    const uint8_t *reset;     /* [batch][steps], or NULL */
+    const int64_t *lengths;   /* [batch], or NULL */
+    void *h;
+    float *last, *states;
+    int64_t x_batch_stride, x_stride, gate_batch_stride, gate_stride, h_batch_stride, h_stride; /* from sequence to sequence and from step to step, >= d */
+} qsr_gated_scan_args;
+/* for either pass; 8-byte aligned */
+int qsr_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int64_t d, int32_t type, size_t *bytes);
+int qsr_gated_scan(const qsr_gated_scan_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Its gradients, from x, gate, reset and lengths as they were and the states that were kept: x_grad and gate_grad (0 behind a sequence's length)
+ * and initial_grad [batch][d], or NULL, for the gradients h_grad of h and last_grad [batch][d] of last, or NULL (0).  Rows that are
+ * written share no element with any others. */
+typedef struct {
+    int32_t type, input;
+    int64_t batch, steps, d;
+    const void *h_grad, *x, *gate;
+    const float *states, *last_grad;
+    const uint8_t *reset;
+    const int64_t *lengths;
+    void *x_grad, *gate_grad;
+    float *initial_grad;
+    int64_t h_grad_batch_stride, h_grad_stride, x_batch_stride, x_stride, gate_batch_stride, gate_stride, x_grad_batch_stride, x_grad_stride,
+        gate_grad_batch_stride, gate_grad_stride;
+} qsr_gated_scan_backward_args;
+int qsr_gated_scan_backward(const qsr_gated_scan_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Log probabilities of given tokens from rows of logits, z = logits / temperature:
  *   lse = log sum exp z;  logp = z[token] - lse;  entropy = -sum p log p;  the `top` best alternatives (the lower index first where
  *   logits are equal) with their log probabilities.

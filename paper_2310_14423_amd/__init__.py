@@ -7,9 +7,11 @@ symbols can be inspected), any compute call without the built library or a gfx95
 from .binding import (QSRError, Config, Context, average_rows, clip_factors, clip_factors_static,
                       host_schedule, lib, lib_path, validate,
                       workspace_bytes, EXPORTS)
-from .operators import (AdamW, RMSNorm, TokenLogprobs, rmsnorm, rmsnorm_backward, token_logprobs,
+from .operators import (AdamW, GatedScan, LayerNorm, RMSNorm, TokenLogprobs, embedding, embedding_backward, gated_scan,
+                        gated_scan_backward, layernorm, layernorm_backward, rmsnorm, rmsnorm_backward, token_logprobs,
                         token_logprobs_backward)
 
 __all__ = ["QSRError", "Config", "Context", "average_rows", "clip_factors", "clip_factors_static", "host_schedule", "lib", "lib_path", "validate",
            "workspace_bytes", "EXPORTS", "AdamW", "RMSNorm", "TokenLogprobs", "rmsnorm", "rmsnorm_backward", "token_logprobs",
-           "token_logprobs_backward"]
+           "token_logprobs_backward", "LayerNorm", "layernorm", "layernorm_backward", "embedding", "embedding_backward", "GatedScan",
+           "gated_scan", "gated_scan_backward"]

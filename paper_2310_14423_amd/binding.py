@@ -15,7 +15,10 @@ EXPORTS = ["qsr_validate", "qsr_workspace_bytes", "qsr_host_schedule", "qsr_init
            "qsr_last_hip_error",
            "qsr_adamw_validate", "qsr_adamw_init", "qsr_adamw_step", "qsr_adamw_set_grads", "qsr_adamw_clip", "qsr_adamw_destroy",
            "qsr_rmsnorm", "qsr_rmsnorm_workspace_bytes", "qsr_rmsnorm_backward",
-           "qsr_token_logprobs_workspace_bytes", "qsr_token_logprobs", "qsr_token_logprobs_backward"]
+           "qsr_token_logprobs_workspace_bytes", "qsr_token_logprobs", "qsr_token_logprobs_backward",
+           "qsr_layernorm", "qsr_layernorm_workspace_bytes", "qsr_layernorm_backward",
+           "qsr_embedding", "qsr_embedding_workspace_bytes", "qsr_embedding_backward",
+           "qsr_gated_scan", "qsr_gated_scan_workspace_bytes", "qsr_gated_scan_backward"]
 
 OPTS = {"sgdm": 0, "adamw": 1}
 LRS = {"cosine": 0, "step": 1, "table": 2, "linear": 3, "pow2cos": 4}

@@ -1,0 +1,564 @@
+// embedding.hip -- rows of K workers' tables by tokens, scaled, and the gradient of the tables.
+//
+//   y_i = scale E_k[t_i];   dE_k[v] = scale * (sum of dy_i over the worker's tokens with t_i = v)  (+ what was there)
+// A token outside 0..V-1 stands for none: zeros, and no gradient.
+// The gradient's sums are made in a fixed order and without atomics.  The worker's tokens are sorted with their places by a stable radix
+// sort, so that a row's terms lie side by side in the order of their places.  The sorted list is cut into chunks of equal length, however
+// often a token comes: a chunk's sums go to their rows, but for a sum that other chunks have a part in, which is kept aside and joined by a
+// second launch in the chunks' order.  Rows of the table that no token names are found by a search in the list, and cleared by the same
+// launch that writes the others.  All sums are fp32; a row is scaled, and rounded, once.
+#include <cmath>
+
+#include "qsr_internal.h"
+#include "row_io.h"
+
+namespace qsr {
+
+constexpr int EMBED_THREADS = 256;
+
+struct LookupArgs {
+    const void *table;
+    const int64_t *tokens;
+    void *y;
+    long long N, V, s_table, s_worker, s_y;
+    int d, lanes;              // lanes to a row: a power of two up to EMBED_THREADS
+    float scale;
+};
+
+// The elements of a run that starts at column `first` of d, or E from the row's end where it would end behind it: the run's last E - `skip`
+struct Run { int at, skip; };
+__device__ __forceinline__ Run run_of(int first, int d, int E) { const int at = min(first, d - E); return {at, first - at}; }
+
+template <typename T, int E>
+__device__ __forceinline__ void store_run(T *p, const float (&v)[E], int skip)
+{
+    if (skip == 0) store_wide<T, E, true>(p, v);
+    else {
+#pragma unroll
+        for (int u = 0; u < E; ++u)
+            if (u >= skip) p[u] = (T)v[u];
+    }
+}
+
+template <typename TI, typename TO, int E>
+__global__ __launch_bounds__(EMBED_THREADS) void embedding_kernel(LookupArgs a)
+{
+    const int lane = threadIdx.x & (a.lanes - 1), place = threadIdx.x / a.lanes, k = blockIdx.y;
+    const long long row = (long long)blockIdx.x * (EMBED_THREADS / a.lanes) + place;
+    if (row >= a.N) return;
+    const long long tok = a.tokens[k * a.N + row];
+    const bool has = tok >= 0 && tok < a.V;
+    const TI *const from = (const TI *)a.table + k * a.s_worker + (has ? tok : 0) * a.s_table;
+    TO *const to = (TO *)a.y + (k * a.N + row) * a.s_y;
+    for (int first = lane * E; first < a.d; first += a.lanes * E) {
+        const Run r = run_of(first, a.d, E);
+        float v[E];
+        load_wide<TI, E, false>(from + r.at, v);
+#pragma unroll
+        for (int u = 0; u < E; ++u) v[u] = has ? v[u] * a.scale : 0.f;
+        store_run<TO, E>(to + r.at, v, r.skip);
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// tokens in order
+// ---------------------------------------------------------------------------------------------------
+constexpr int DIGITS = 512;                    // at most, of a pass of the sort
+constexpr int SORT_SMALL = 4096;               // tokens of a worker that one workgroup sorts in LDS
+constexpr int SORT_THREADS = 256, SMALL_THREADS = 1024;
+
+struct SortArgs {
+    const int64_t *tokens;                     // first pass: these, and places as they come
+    const uint32_t *keys_in;
+    const int *place_in;
+    uint32_t *keys;                            // [K][N]
+    int *place;
+    int *counts;                               // [K][blocks][DIGITS]
+    long long N, V, per;                       // tokens to a workgroup: a multiple of SORT_THREADS
+    int shift, bits, passes;
+};
+
+// V stands for none and comes last
+__device__ __forceinline__ uint32_t key_of(long long tok, long long V) { return tok >= 0 && tok < V ? (uint32_t)tok : (uint32_t)V; }
+__device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int k, long long i)
+{
+    return a.tokens != nullptr ? key_of(a.tokens[k * a.N + i], a.V) : a.keys_in[k * a.N + i];
+}
+
+// How many lanes of the wavefront that take part and lie before this one have its digit, and how many have it in all
+__device__ __forceinline__ void same_digit(uint32_t digit, bool in, int bits, int &before, int &all)
+{
+    uint64_t mask = __ballot(in);
+    for (int b = 0; b < bits; ++b) {
+        const uint64_t one = __ballot((digit >> b) & 1);
+        mask &= (digit >> b) & 1 ? one : ~one;
+    }
+    before = __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1));
+    all = __popcll(mask);
+}
+
+// counts[digit], digit < DIGITS, to the sums over all digits before (THREADS * 4 >= DIGITS).  Every thread has to be here.
+template <int THREADS>
+__device__ __forceinline__ void sums_before(int *counts, int *waves)
+{
+    constexpr int EACH = (DIGITS + THREADS - 1) / THREADS;
+    const int tid = threadIdx.x, lane = tid & 63;
+    int c[EACH], sum = 0;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) { c[i] = tid * EACH + i < DIGITS ? counts[tid * EACH + i] : 0; sum += c[i]; }
+    int upto = sum;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(upto, o, 64); upto += lane >= o ? v : 0; }
+    if (lane == 63) waves[tid >> 6] = upto;
+    __syncthreads();
+    int base = upto - sum;
+    for (int w = 0; w < (tid >> 6); ++w) base += waves[w];
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (tid * EACH + i < DIGITS) counts[tid * EACH + i] = base;
+        base += c[i];
+    }
+    __syncthreads();
+}
+
+__global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortArgs a)
+{
+    __shared__ int count[DIGITS];
+    const int k = blockIdx.y;
+    for (int i = threadIdx.x; i < DIGITS; i += SORT_THREADS) count[i] = 0;
+    __syncthreads();
+    const long long from = blockIdx.x * a.per, end = min(a.N, from + a.per);
+    for (long long i = from + threadIdx.x; i < end; i += SORT_THREADS)
+        atomicAdd(&count[(sort_key(a, k, i) >> a.shift) & ((1u << a.bits) - 1)], 1);
+    __syncthreads();
+    for (int i = threadIdx.x; i < DIGITS; i += SORT_THREADS) a.counts[((long long)k * gridDim.x + blockIdx.x) * DIGITS + i] = count[i];
+}
+
+// A wavefront moves a run of its workgroup's tokens, 64 at a time, in their order
+__global__ __launch_bounds__(SORT_THREADS) void sort_move_kernel(SortArgs a)
+{
+    constexpr int WAVES = SORT_THREADS / 64;
+    __shared__ int start[DIGITS], mine[DIGITS], to[WAVES][DIGITS], sums[WAVES];
+    const int k = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const uint32_t mask = (1u << a.bits) - 1;
+    for (int i = tid; i < DIGITS; i += SORT_THREADS) {
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) to[w][i] = 0;
+        const int *c = a.counts + (long long)k * gridDim.x * DIGITS + i;
+        int all = 0, before = 0;
+#pragma unroll 8
+        for (unsigned b = 0; b < gridDim.x; ++b) {
+            const int n = c[b * DIGITS];
+            all += n;
+            before += b < blockIdx.x ? n : 0;
+        }
+        start[i] = all;
+        mine[i] = before;
+    }
+    __syncthreads();
+    sums_before<SORT_THREADS>(start, sums);
+    const long long quarter = a.per / WAVES;
+    const long long from = min(a.N, blockIdx.x * a.per + wave * quarter), end = min(a.N, from + quarter);
+    for (long long i = from + lane; i < end; i += 64) atomicAdd(&to[wave][(sort_key(a, k, i) >> a.shift) & mask], 1);
+    __syncthreads();
+    for (int i = tid; i < DIGITS; i += SORT_THREADS) {
+        int at = start[i] + mine[i];
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) { const int n = to[w][i]; to[w][i] = at; at += n; }
+    }
+    __syncthreads();
+    for (long long i = from; i < end; i += 64) {
+        const bool in = i + lane < end;
+        const long long j = in ? i + lane : end - 1;
+        const uint32_t key = sort_key(a, k, j), digit = (key >> a.shift) & mask;
+        int before, all;
+        same_digit(digit, in, a.bits, before, all);
+        const int at = to[wave][digit];
+        if (in) {
+            a.keys[k * a.N + at + before] = key;
+            a.place[k * a.N + at + before] = a.tokens != nullptr ? (int)j : a.place_in[k * a.N + j];
+        }
+        __builtin_amdgcn_wave_barrier();
+        if (in && before == 0) to[wave][digit] = at + all;
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Few tokens: all passes in LDS
+__global__ __launch_bounds__(SMALL_THREADS) void sort_small_kernel(SortArgs a)
+{
+    constexpr int WAVES = SMALL_THREADS / 64;
+    __shared__ uint32_t keys[2][SORT_SMALL];
+    __shared__ uint16_t place[2][SORT_SMALL];
+    __shared__ int start[DIGITS], to[WAVES][DIGITS], sums[WAVES];
+    const int k = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, N = (int)a.N;
+    const uint32_t mask = (1u << a.bits) - 1;
+    for (int i = tid; i < N; i += SMALL_THREADS) { keys[0][i] = key_of(a.tokens[(long long)k * N + i], a.V); place[0][i] = (uint16_t)i; }
+    const int run = (N + SMALL_THREADS - 1) / SMALL_THREADS * 64, from = min(N, wave * run), end = min(N, from + run);
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int src = pass & 1, dst = src ^ 1, shift = pass * a.bits;
+        for (int i = tid; i < WAVES * DIGITS; i += SMALL_THREADS) to[i / DIGITS][i % DIGITS] = 0;
+        __syncthreads();
+        for (int i = from + lane; i < end; i += 64) atomicAdd(&to[wave][(keys[src][i] >> shift) & mask], 1);
+        __syncthreads();
+        if (tid < DIGITS) {
+            int all = 0;
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) all += to[w][tid];
+            start[tid] = all;
+        }
+        __syncthreads();
+        sums_before<SMALL_THREADS>(start, sums);
+        if (tid < DIGITS) {
+            int at = start[tid];
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) { const int n = to[w][tid]; to[w][tid] = at; at += n; }
+        }
+        __syncthreads();
+        for (int i = from; i < end; i += 64) {
+            const bool in = i + lane < end;
+            const int j = in ? i + lane : end - 1;
+            const uint32_t key = keys[src][j], digit = (key >> shift) & mask;
+            int before, all;
+            same_digit(digit, in, a.bits, before, all);
+            const int at = to[wave][digit];
+            if (in) { keys[dst][at + before] = key; place[dst][at + before] = place[src][j]; }
+            __builtin_amdgcn_wave_barrier();
+            if (in && before == 0) to[wave][digit] = at + all;
+            __builtin_amdgcn_wave_barrier();
+        }
+        __syncthreads();
+    }
+    for (int i = tid; i < N; i += SMALL_THREADS) {
+        a.keys[(long long)k * N + i] = keys[a.passes & 1][i];
+        a.place[(long long)k * N + i] = place[a.passes & 1][i];
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------
+// sums of the sorted rows
+// ---------------------------------------------------------------------------------------------------
+struct GradArgs {
+    const void *dy;
+    const uint32_t *keys;
+    const int *place;
+    void *out;
+    float *parts;                              // [K][chunks][2][d]: of a chunk's first sum, which began before it, and of its last, which goes on
+    long long N, V, chunks, s_dy, s_out, s_worker;
+    long long chunk_groups;                    // workgroups with chunks; those behind clear rows
+    int d, lanes, chunk, clear_rows;
+    float scale;
+    bool add;
+};
+
+template <typename TO, int E>
+__device__ __forceinline__ void finish_run(const GradArgs &a, int k, uint32_t v, const Run &r, const float (&sum)[E])
+{
+    TO *const to = (TO *)a.out + k * a.s_worker + (long long)v * a.s_out + r.at;
+    float x[E];
+#pragma unroll
+    for (int u = 0; u < E; ++u) x[u] = a.scale * sum[u];
+    if (a.add) {
+        float old[E];
+        load_wide<TO, E, false>(to, old);
+#pragma unroll
+        for (int u = 0; u < E; ++u) x[u] += old[u];
+    }
+    store_run<TO, E>(to, x, r.skip);
+}
+
+// The first place in the worker's sorted keys that holds v or more
+__device__ __forceinline__ long long first_of(const uint32_t *keys, long long from, long long N, uint32_t v)
+{
+    long long lo = from, hi = N;
+    while (lo < hi) {
+        const long long mid = (lo + hi) >> 1;
+        if (keys[mid] < v) lo = mid + 1;
+        else hi = mid;
+    }
+    return lo;
+}
+
+constexpr int CHUNK_MOST = 32;                 // tokens to a chunk
+template <typename TI, typename TO, int E>
+__global__ __launch_bounds__(EMBED_THREADS) void embedding_sums_kernel(GradArgs a)
+{
+    __shared__ uint32_t skey[EMBED_THREADS / 16 * CHUNK_MOST];
+    __shared__ int splace[EMBED_THREADS / 16 * CHUNK_MOST];
+    const int k = blockIdx.y, lane = threadIdx.x & (a.lanes - 1), place = threadIdx.x / a.lanes, side = EMBED_THREADS / a.lanes;
+    const uint32_t *const keys = a.keys + k * a.N;
+    const int first = ((int)blockIdx.z * a.lanes + lane) * E;
+    const Run run = run_of(min(first, a.d - 1), a.d, E);
+    if ((long long)blockIdx.x >= a.chunk_groups) {
+        const long long v0 = ((long long)blockIdx.x - a.chunk_groups) * a.clear_rows, rows = min((long long)a.clear_rows, a.V - v0);
+        for (int i = threadIdx.x; i < rows; i += EMBED_THREADS) {
+            const long long at = first_of(keys, 0, a.N, (uint32_t)(v0 + i));
+            skey[i] = at < a.N && keys[at] == (uint32_t)(v0 + i);
+        }
+        __syncthreads();
+        if (first >= a.d) return;
+        const float zero[E] = {};
+        for (int i = place; i < rows; i += side)
+            if (!skey[i]) store_run<TO, E>((TO *)a.out + k * a.s_worker + (v0 + i) * a.s_out + run.at, zero, run.skip);
+        return;
+    }
+    const long long c0 = (long long)blockIdx.x * side * a.chunk;
+    for (int i = threadIdx.x; i < side * a.chunk; i += EMBED_THREADS) {
+        const bool in = c0 + i < a.N;
+        skey[i] = in ? keys[c0 + i] : (uint32_t)a.V;
+        splace[i] = in ? a.place[k * a.N + c0 + i] : 0;
+    }
+    __syncthreads();
+    const long long chunk = (long long)blockIdx.x * side + place, from = chunk * a.chunk;
+    if (first >= a.d || from >= a.N) return;
+    const uint32_t *const ck = skey + place * a.chunk;
+    const int *const cp = splace + place * a.chunk;
+    const uint32_t none = (uint32_t)a.V;
+    uint32_t cur = ck[0];
+    if (cur == none) return;
+    bool begun = from > 0 && keys[from - 1] == cur;                        // the first sum began before this chunk
+    float sum[E] = {};
+    const TI *const dy = (const TI *)a.dy + k * a.N * a.s_dy + run.at;
+    float *const parts = a.parts + (k * a.chunks + chunk) * 2 * a.d + run.at;
+    for (int i = 0; i < a.chunk; i += 8) {
+        typename Wide<TI, E>::vec v[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) v[u] = __builtin_nontemporal_load((const typename Wide<TI, E>::vec *)(dy + cp[i + u] * a.s_dy));
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const uint32_t key = ck[i + u];
+            if (key != cur) {
+                if (cur != none) {
+                    if (begun) store_run<float, E>(parts, sum, run.skip);
+                    else finish_run<TO, E>(a, k, cur, run, sum);
+                }
+                begun = false;
+                cur = key;
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] = 0.f;
+            }
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += (float)v[u][e];
+        }
+    }
+    if (cur == none) return;
+    const bool on = from + a.chunk < a.N && keys[from + a.chunk] == cur;
+    if (begun) store_run<float, E>(parts, sum, run.skip);
+    else if (on) store_run<float, E>(parts + a.d, sum, run.skip);
+    else finish_run<TO, E>(a, k, cur, run, sum);
+}
+
+// A sum that goes on behind the chunk in which it begins: its parts, every fourth to a wavefront, in their order.  One workgroup to a chunk,
+// most of which have nothing to do, and 64 E columns.
+template <typename TO, int E>
+__global__ __launch_bounds__(EMBED_THREADS) void embedding_join_kernel(GradArgs a)
+{
+    constexpr int WAVES = EMBED_THREADS / 64;
+    __shared__ float red[WAVES][64][E + 1];
+    const int k = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const uint32_t *const keys = a.keys + k * a.N;
+    const long long chunk = blockIdx.x, from = chunk * a.chunk, end = from + a.chunk;
+    if (end >= a.N) return;
+    const uint32_t v = keys[end - 1];
+    if (v == (uint32_t)a.V || keys[end] != v || (keys[from] == v && from > 0 && keys[from - 1] == v)) return;
+    const long long last = (first_of(keys, end, a.N, v + 1) - 1) / a.chunk;        // chunk + 1 .. last: first sums of theirs
+    const int first = ((int)blockIdx.z * 64 + lane) * E;
+    const Run run = run_of(min(first, a.d - 1), a.d, E);
+    const float *const parts = a.parts + (k * a.chunks + chunk) * 2 * a.d + run.at;
+    float sum[E] = {};
+    for (long long i = wave; i <= last - chunk; i += 8 * WAVES) {
+        float x[8][E];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) {
+            const long long j = min(i + u * WAVES, last - chunk);
+            load_wide<float, E, false>(j == 0 ? parts + a.d : parts + 2 * j * a.d, x[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += i + u * WAVES <= last - chunk ? x[u][e] : 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < E; ++e) red[wave][lane][e] = sum[e];
+    __syncthreads();
+    if (wave != 0 || first >= a.d) return;
+#pragma unroll
+    for (int w = 1; w < WAVES; ++w)
+#pragma unroll
+        for (int e = 0; e < E; ++e) sum[e] += red[w][lane][e];
+    finish_run<TO, E>(a, k, v, run, sum);
+}
+
+// ---------------------------------------------------------------------------------------------------
+// host
+// ---------------------------------------------------------------------------------------------------
+constexpr long long EMBED_MOST = 1ll << 27;    // tokens of a worker
+
+static int lanes_for(long long d, int E)
+{
+    const long long runs = (d + E - 1) / E;
+    int L = 16;
+    while (L < EMBED_THREADS && L < runs) L <<= 1;
+    return L;
+}
+
+// How the tokens of K workers are sorted and summed, and where what lies in the workspace
+struct GradPlan {
+    int passes, bits, chunk, lanes, slices;
+    long long blocks, per, chunks;
+    size_t keys[2], place[2], counts, parts, bytes;
+};
+static GradPlan grad_plan(int K, long long N, long long V, long long d, int E)
+{
+    GradPlan p;
+    int bits = 1;
+    while (bits < 32 && ((uint64_t)V >> bits) != 0) ++bits;                // V itself is a key
+    p.passes = (bits + 8) / 9;
+    p.bits = (bits + p.passes - 1) / p.passes;
+    p.per = 1024;
+    while ((N + p.per - 1) / p.per > 128) p.per *= 2;
+    p.blocks = N <= SORT_SMALL ? 0 : (N + p.per - 1) / p.per;
+    p.lanes = lanes_for(d, E);
+    p.slices = (int)((d + (long long)p.lanes * E - 1) / ((long long)p.lanes * E));
+    const long long waves = (long long)K * ((N + CHUNK_MOST - 1) / CHUNK_MOST) * p.lanes * p.slices / 64;
+    p.chunk = waves < 2048 ? 8 : CHUNK_MOST;
+    p.chunks = (N + p.chunk - 1) / p.chunk;
+    size_t at = 0;
+    auto take = [&](size_t n) { const size_t here = at; at += (n + 255) / 256 * 256; return here; };
+    const size_t list = (size_t)K * (size_t)N * 4;
+    for (int i = 0; i < (p.blocks ? 2 : 1); ++i) { p.keys[i] = take(list); p.place[i] = take(list); }
+    if (!p.blocks) { p.keys[1] = p.keys[0]; p.place[1] = p.place[0]; }
+    p.counts = take((size_t)K * (size_t)p.blocks * DIGITS * 4);
+    p.parts = take((size_t)K * (size_t)p.chunks * 2 * (size_t)d * 4);
+    p.bytes = N > 0 ? at : 0;
+    return p;
+}
+
+template <typename TI, typename TO, int E>
+static hipError_t launch_sums(GradArgs &a, const GradPlan &p, int K, hipStream_t s)
+{
+    const int side = EMBED_THREADS / p.lanes;
+    a.chunk_groups = (p.chunks + side - 1) / side;
+    // some 64 KiB to a workgroup that clears, and a row to each of its threads at most
+    const long long row = (long long)a.d * (long long)sizeof(TO), rows = (65536 + row - 1) / row;
+    a.clear_rows = (int)(rows < EMBED_THREADS ? rows : EMBED_THREADS);
+    const long long clears = a.add ? 0 : (a.V + a.clear_rows - 1) / a.clear_rows;
+    if (a.chunk_groups + clears > 0)
+        embedding_sums_kernel<TI, TO, E><<<dim3((unsigned)(a.chunk_groups + clears), (unsigned)K, (unsigned)p.slices), EMBED_THREADS, 0, s>>>(a);
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || p.chunks < 2) return e;
+    constexpr int J = E < 4 ? 1 : 4;
+    embedding_join_kernel<TO, J><<<dim3((unsigned)(p.chunks - 1), (unsigned)K, (unsigned)((a.d + 64 * J - 1) / (64 * J))), EMBED_THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename TI, typename TO>
+static hipError_t launch_lookup(LookupArgs &a, int K, hipStream_t s)
+{
+    constexpr int E = wide_of<TI>();
+    a.lanes = lanes_for(a.d, a.d < E ? 1 : E);
+    const long long side = EMBED_THREADS / a.lanes;
+    const dim3 grid((unsigned)((a.N + side - 1) / side), (unsigned)K);
+    if (a.d < E) embedding_kernel<TI, TO, 1><<<grid, EMBED_THREADS, 0, s>>>(a);
+    else embedding_kernel<TI, TO, E><<<grid, EMBED_THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+}  // namespace qsr
+
+using namespace qsr;
+
+static int finish(hipError_t e)
+{
+    if (e == hipSuccess) return QSR_OK;
+    set_last_hip_error((int)e);
+    return QSR_EHIP;
+}
+static bool off(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+static bool is_type(int t) { return t == QSR_TYPE_F32 || t == QSR_TYPE_BF16; }
+static uintptr_t size_of(int type) { return type == QSR_TYPE_F32 ? 4 : 2; }
+static bool sizes_ok(int32_t K, int64_t N, int64_t V, int64_t d)
+{
+    return K >= 1 && K <= 65535 && N >= 0 && V >= 1 && V < ((int64_t)1 << 31) && d >= 1 && d <= ((int64_t)1 << 22);
+}
+// elements of a run: 16 bytes of the rows that are read, or one in rows that are shorter
+static int run_elements(int type, int64_t d)
+{
+    const int E = type == QSR_TYPE_F32 ? 4 : 8;
+    return d < E ? 1 : E;
+}
+
+extern "C" int qsr_embedding(const qsr_embedding_args *q, void *stream)
+{
+    if (!q || !sizes_ok(q->K, q->tokens_each, q->vocab, q->d) || !is_type(q->type) || !is_type(q->y_type)) return QSR_EINVAL;
+    if (!std::isfinite((float)q->scale)) return QSR_EINVAL;
+    if (q->tokens_each > EMBED_MOST) return QSR_ELIMIT;
+    if (q->tokens_each == 0) return QSR_OK;
+    if (!q->table || off(q->table, size_of(q->type)) || !q->tokens || off(q->tokens, 8) || !q->y || off(q->y, size_of(q->y_type))) return QSR_EINVAL;
+    if (q->table_stride < q->d || q->y_stride < q->d || (q->K > 1 && q->worker_stride < q->d)) return QSR_EINVAL;
+    LookupArgs a{q->table, q->tokens, q->y, q->tokens_each, q->vocab, q->table_stride, q->worker_stride, q->y_stride, (int)q->d, 0, (float)q->scale};
+    const hipStream_t s = (hipStream_t)stream;
+    const bool wide = q->y_type == QSR_TYPE_F32;
+    return finish(q->type == QSR_TYPE_F32 ? (wide ? launch_lookup<float, float>(a, q->K, s) : launch_lookup<float, bf16_t>(a, q->K, s))
+                                          : (wide ? launch_lookup<bf16_t, float>(a, q->K, s) : launch_lookup<bf16_t, bf16_t>(a, q->K, s)));
+}
+
+extern "C" int qsr_embedding_workspace_bytes(int32_t K, int64_t tokens_each, int64_t vocab, int64_t d, int32_t type, size_t *bytes)
+{
+    if (!bytes) return QSR_EINVAL;
+    *bytes = 0;
+    if (!sizes_ok(K, tokens_each, vocab, d) || !is_type(type)) return QSR_EINVAL;
+    if (tokens_each > EMBED_MOST) return QSR_ELIMIT;
+    *bytes = grad_plan(K, tokens_each, vocab, d, run_elements(type, d)).bytes;
+    return QSR_OK;
+}
+
+extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q || !sizes_ok(q->K, q->tokens_each, q->vocab, q->d) || !is_type(q->type) || !is_type(q->grad_type)) return QSR_EINVAL;
+    if (!std::isfinite((float)q->scale) || (q->accumulate != 0 && q->accumulate != 1)) return QSR_EINVAL;
+    if (!q->grad || off(q->grad, size_of(q->grad_type)) || q->grad_stride < q->d) return QSR_EINVAL;
+    if (q->K > 1 && q->worker_stride < (q->vocab - 1) * q->grad_stride + q->d) return QSR_EINVAL;
+    if (q->tokens_each > 0 && (!q->y_grad || off(q->y_grad, size_of(q->type)) || !q->tokens || off(q->tokens, 8) || q->y_grad_stride < q->d))
+        return QSR_EINVAL;
+    size_t need = 0;
+    const int rc = qsr_embedding_workspace_bytes(q->K, q->tokens_each, q->vocab, q->d, q->type, &need);
+    if (rc != QSR_OK) return rc;
+    if (need > 0 && (!workspace || off(workspace, 16))) return QSR_EINVAL;
+    if (workspace_bytes < need) return QSR_ENOMEM;
+    const hipStream_t s = (hipStream_t)stream;
+    const int K = q->K, E = run_elements(q->type, q->d);
+    const long long N = q->tokens_each;
+    const GradPlan p = grad_plan(K, N, q->vocab, q->d, E);
+    char *const ws = (char *)workspace;
+    int done = 0;                              // which of the two lists holds the result
+    if (N > 0) {
+        SortArgs a{q->tokens, nullptr, nullptr, (uint32_t *)(ws + p.keys[0]), (int *)(ws + p.place[0]), (int *)(ws + p.counts), N, q->vocab, p.per, 0,
+                   p.bits, p.passes};
+        hipError_t e = hipSuccess;
+        if (p.blocks == 0) {
+            sort_small_kernel<<<dim3((unsigned)K), SMALL_THREADS, 0, s>>>(a);
+            e = hipGetLastError();
+        }
+        for (int pass = 0; p.blocks > 0 && pass < p.passes && e == hipSuccess; ++pass) {
+            done = pass & 1;
+            a.keys = (uint32_t *)(ws + p.keys[done]);
+            a.place = (int *)(ws + p.place[done]);
+            if (pass > 0) { a.tokens = nullptr; a.keys_in = (uint32_t *)(ws + p.keys[done ^ 1]); a.place_in = (int *)(ws + p.place[done ^ 1]); }
+            a.shift = pass * p.bits;
+            const dim3 grid((unsigned)p.blocks, (unsigned)K);
+            sort_count_kernel<<<grid, SORT_THREADS, 0, s>>>(a);
+            e = hipGetLastError();
+            if (e == hipSuccess) sort_move_kernel<<<grid, SORT_THREADS, 0, s>>>(a);
+            if (e == hipSuccess) e = hipGetLastError();
+        }
+        if (e != hipSuccess) return finish(e);
+    }
+    GradArgs a{q->y_grad, (const uint32_t *)(ws + p.keys[done]), (const int *)(ws + p.place[done]), q->grad, (float *)(ws + p.parts), N, q->vocab, p.chunks,
+               q->y_grad_stride, q->grad_stride, q->worker_stride, 0, (int)q->d, p.lanes, p.chunk, 0, (float)q->scale, q->accumulate != 0};
+#define EMBED_SUMS(TI, TO) (E == 1 ? launch_sums<TI, TO, 1>(a, p, K, s) : launch_sums<TI, TO, wide_of<TI>()>(a, p, K, s))
+    const bool wide = q->grad_type == QSR_TYPE_F32;
+    return finish(q->type == QSR_TYPE_F32 ? (wide ? EMBED_SUMS(float, float) : EMBED_SUMS(float, bf16_t))
+                                          : (wide ? EMBED_SUMS(bf16_t, float) : EMBED_SUMS(bf16_t, bf16_t)));
+#undef EMBED_SUMS
+}

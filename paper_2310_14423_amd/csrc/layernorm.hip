@@ -1,0 +1,344 @@
+// layernorm.hip -- layer norm of rows with the residual's addition, for K workers with a weight and a bias each, and its gradients.
+//
+//   s = x + res (or x);  mean = mean(s);  rstd = 1 / sqrt(mean((s - mean)^2) + eps);  y = (s - mean) rstd w_k + b_k
+//   h = s rounded to the rows' type, the residual stream behind;  y in the rows' type, or as e4m3 codes with one fp32 scale for each
+//   row, scale = max|y| / 448 over the row's finite entries
+// and backward, from h as it is kept, with n = (h - mean) rstd, u = dy w and dres what comes down the residual stream:
+//   dx = rstd (u - mean(u) - n mean(u n)) + dres  (the gradient of x and of res)
+//   dw_k = sum over the worker's rows of dy n;  db_k = sum of dy
+// All arithmetic is fp32.  The deviation is taken from the row in the registers, about its mean, and not from a sum of squares: rows whose
+// mean is large beside their deviation keep it.  rstd is 0 where mean((s - mean)^2) + eps is 0 as a float.
+#include <cmath>
+
+#include "norm_rows.h"
+#include "qsr_internal.h"
+
+namespace qsr {
+
+struct LayerArgs {
+    const void *x, *res;
+    const float *w, *b;
+    void *sum, *y;
+    float *scale, *mean, *rstd;
+    long long rows, s_x, s_res, s_sum, s_y;    // rows of a worker; strides from row to row
+    long long s_w, s_b;                        // and from worker to worker
+    int d;
+    float eps;
+};
+
+// `turn` counts the sums over a group of wavefronts, which take turns at their words
+template <typename T, int L, int W, int NV, bool FP8>
+__device__ __forceinline__ void layernorm_row(const LayerArgs &a, int k, long long row, int lane, float (*red)[W], int &turn)
+{
+    constexpr int E = wide_of<T>();
+    Row<T, NV> x, res;
+    RowPart<T, NV> s, w;
+    load_row<T, L, W, NV, true>((const T *)a.x + row * a.s_x, lane, a.d, x);
+    if (a.res != nullptr) load_row<T, L, W, NV, true>((const T *)a.res + row * a.s_res, lane, a.d, res);
+    load_words<T, L, W, NV>(a.w + k * a.s_w, lane, a.d, w);
+    each<T, NV>([](float &y, float v) { y = v; }, s, x);
+    if (a.res != nullptr) each<T, NV>([](float &y, float v) { y += v; }, s, res);
+    const int runs = a.d / E, rest = a.d - runs * E;
+    float q = lane < rest ? s.t : 0.f;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        float part = 0.f;
+#pragma unroll
+        for (int u = 0; u < E; ++u) part += s.v[c][u];
+        q += lane + c * L * W < runs ? part : 0.f;
+    }
+    if (a.sum != nullptr) store_row<T, L, W, NV, false>((T *)a.sum + row * a.s_sum, lane, a.d, s);
+    const float mean = group_sum<L, W>(q, red, turn++) / (float)a.d;
+    each<T, NV>([&](float &y) { y -= mean; }, s);
+    q = lane < rest ? s.t * s.t : 0.f;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) {
+        float part = 0.f;
+#pragma unroll
+        for (int u = 0; u < E; ++u) part = fmaf(s.v[c][u], s.v[c][u], part);
+        q += lane + c * L * W < runs ? part : 0.f;
+    }
+    const float var = group_sum<L, W>(q, red, turn++) / (float)a.d + a.eps;
+    const float rstd = var == 0.f ? 0.f : 1.f / sqrtf(var);                // equal numbers without eps: the bias, and no gradient
+    if (lane == 0 && a.mean != nullptr) a.mean[row] = mean;
+    if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
+    each<T, NV>([&](float &y, float &f) { y = y * rstd * f; }, s, w);
+    if (a.b != nullptr) {
+        load_words<T, L, W, NV>(a.b + k * a.s_b, lane, a.d, w);
+        each<T, NV>([](float &y, float &f) { y += f; }, s, w);
+    }
+    if (!FP8) {
+        store_row<T, L, W, NV, false>((T *)a.y + row * a.s_y, lane, a.d, s);
+        return;
+    }
+    // (a lane without a run has the last one's numbers without weight and bias: zeros)
+    float top = 0.f;
+    each<T, NV>([&](float &y) { if (fabsf(y) < INFINITY) top = fmaxf(top, fabsf(y)); }, s);
+    top = group_max<L, W>(top, red, turn++);
+    const float scale = top >= 1e-35f ? top * (1.f / E4M3_MAX) : 0.f;      // less would leave the range of floats
+    if (lane == 0) a.scale[row] = scale;
+    const float f = scale > 0.f ? 1.f / scale : 0.f;
+    // a rounding above 448 at most, which still becomes 448; what is not finite becomes NaN
+    each<T, NV>([&](float &y) { y *= f; }, s);
+    store_codes<T, L, W, NV>((uint8_t *)a.y + row * a.s_y, lane, a.d, s);
+}
+
+template <typename T, int L, int W, int NV, bool FP8>
+__global__ __launch_bounds__(rms_threads<W>()) void layernorm_kernel(LayerArgs a)
+{
+    __shared__ float red[2][W];
+    constexpr int side = rms_side<L, W>();
+    const int k = blockIdx.y, lane = rms_lane<L, W>(), place = rms_place<L, W>();
+    int turn = 0;
+    for (long long r = (long long)blockIdx.x * side + place; r < a.rows; r += (long long)gridDim.x * side)
+        layernorm_row<T, L, W, NV, FP8>(a, k, k * a.rows + r, lane, red, turn);
+}
+
+struct LayerBackArgs {
+    const void *dy, *h;
+    const float *w, *mean, *rstd;
+    const void *dres;
+    void *dx;
+    float *part_w, *part_b;                    // each workgroup's sums, s_part apart
+    long long rows, s_part, s_dy, s_h, s_dres, s_dx, s_w;
+    int d;
+};
+
+// Two sums over the lanes of a row with one barrier
+template <int L, int W>
+__device__ __forceinline__ void group_sums(float &p, float &q, float (*red)[2][W], int turn)
+{
+    if (W == 1) {
+        p = group_sum<L, 1>(p, nullptr, 0);
+        q = group_sum<L, 1>(q, nullptr, 0);
+        return;
+    }
+    p = wave_sum(p);
+    q = wave_sum(q);
+    if ((threadIdx.x & 63) == 0) { red[turn & 1][0][threadIdx.x >> 6] = p; red[turn & 1][1][threadIdx.x >> 6] = q; }
+    __syncthreads();
+    p = q = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) { p += red[turn & 1][0][i]; q += red[turn & 1][1][i]; }
+}
+
+// A workgroup takes every gridDim.x-th row (W == 1: four of them at a time) and keeps its parts of the gradients of weight and bias in
+// registers.  The next row's loads are under way while a row is worked on where that takes few registers.
+template <typename T, int L, int W, int NV, bool BIAS>
+__global__ __launch_bounds__(rms_threads<W>(), 4) void layernorm_back_kernel(LayerBackArgs a)
+{
+    constexpr int E = wide_of<T>();
+    constexpr bool AHEAD = NV * (3 * E + 3 * 2 * 4) <= 48;
+    __shared__ float red[2][2][W];
+    __shared__ float side_sum[W == 1 ? 3 * L * (NV * E + 1) : 1];
+    constexpr int side = rms_side<L, W>();
+    const int k = blockIdx.y, lane = rms_lane<L, W>(), place = rms_place<L, W>();
+    const long long step = (long long)gridDim.x * side, last = (k + 1) * a.rows;
+    RowPart<T, NV> w, dw, db;
+    load_words<T, L, W, NV>(a.w + k * a.s_w, lane, a.d, w);
+    each<T, NV>([](float &x, float &y) { x = 0.f; y = 0.f; }, dw, db);
+    Row<T, NV> g, h, e = {};
+    float rstd = 0.f, mean = 0.f;
+    auto load = [&](long long row) {
+        load_row<T, L, W, NV, true>((const T *)a.dy + row * a.s_dy, lane, a.d, g);
+        load_row<T, L, W, NV, true>((const T *)a.h + row * a.s_h, lane, a.d, h);
+        if (a.dres != nullptr) load_row<T, L, W, NV, true>((const T *)a.dres + row * a.s_dres, lane, a.d, e);
+        rstd = a.rstd[row];
+        mean = a.mean[row];
+    };
+    long long row = k * a.rows + (long long)blockIdx.x * side + place;
+    if (AHEAD && row < last) load(row);
+#pragma unroll 1
+    for (int turn = 0; row < last; row += step, ++turn) {
+        if (!AHEAD) load(row);
+        Row<T, NV> g0 = g, h0 = h, e0 = e;
+        const float rs = rstd, mu = mean;
+        if (AHEAD) load(min(row + step, last - 1));
+        float p = 0.f, q = 0.f;
+        each<T, NV>([&](float &acc, float &sum, float f, float y, float x) {
+            const float n = (x - mu) * rs, u = y * f;
+            acc = fmaf(y, n, acc);
+            if (BIAS) sum += y;
+            p += u;
+            q = fmaf(u, n, q);
+        }, dw, db, w, g0, h0);
+        group_sums<L, W>(p, q, red, turn);
+        p /= (float)a.d;
+        q /= (float)a.d;
+        as_in_memory(g0);
+        as_in_memory(h0);
+        auto dx = [&](float f, float y, float x, float z) { return fmaf(rs, fmaf(-((x - mu) * rs), q, y * f - p), z); };
+        T *const to = (T *)a.dx + row * a.s_dx;
+        const int runs = a.d / E, rest = a.d - runs * E;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) {
+            float v[E];
+#pragma unroll
+            for (int u = 0; u < E; ++u) v[u] = dx(w.v[c][u], (float)g0.v[c][u], (float)h0.v[c][u], (float)e0.v[c][u]);
+            const int i = lane + c * L * W;
+            if (i < runs) store_wide<T, E, true>(behind(to, (uint32_t)i * 16), v);
+        }
+        if (lane < rest) to[runs * E + lane] = (T)dx(w.t, (float)g0.t, (float)h0.t, (float)e0.t);
+    }
+    const long long part = ((long long)k * gridDim.x + blockIdx.x) * a.s_part;
+#pragma unroll
+    for (int kind = 0; kind < (BIAS ? 2 : 1); ++kind) {
+        RowPart<T, NV> &sum = kind ? db : dw;
+        if (W == 1) {                          // the sums of a wavefront's rows and of the four wavefronts become one, in their order
+            const int wave = threadIdx.x >> 6;
+#pragma unroll
+            for (int o = L; o < 64; o <<= 1) each<T, NV>([&](float &x) { x += __shfl_xor(x, o, 64); }, sum);
+            float *const mine = side_sum + (wave > 0 ? wave - 1 : 0) * L * (NV * E + 1) + lane * (NV * E + 1);
+            int n = 0;
+            if (kind) __syncthreads();         // the weight's have been read
+            if (wave > 0 && (threadIdx.x & 63) < L) each<T, NV>([&](float &x) { mine[n++] = x; }, sum);
+            __syncthreads();
+            if (threadIdx.x < L) {
+#pragma unroll
+                for (int o = 0; o < 3; ++o) {
+                    const float *const other = side_sum + (o * L + lane) * (NV * E + 1);
+                    n = 0;
+                    each<T, NV>([&](float &x) { x += other[n++]; }, sum);
+                }
+            }
+        }
+        if (W > 1 || threadIdx.x < L) store_words<T, L, W, NV>((kind ? a.part_b : a.part_w) + part, lane, a.d, sum);
+    }
+}
+
+// The gradients of weight and bias: sums over the parts [K][parts][cols], in a fixed order, COLS columns and 1024 / COLS runs of parts, four of
+// each in flight, to a workgroup.  The first d columns are the weight's.  Latency is everything: fewer columns, on more workgroups,
+// where there are few of them.
+constexpr int SUM_THREADS = 1024;
+template <int COLS>
+__global__ __launch_bounds__(SUM_THREADS) void layernorm_sums_kernel(const float *__restrict__ partial, int parts, int cols, int d, float *__restrict__ dw,
+                                                                     float *__restrict__ db)
+{
+    constexpr int RUNS = SUM_THREADS / COLS, WAVES = SUM_THREADS / 64;
+    __shared__ float red[WAVES][COLS];
+    const int k = blockIdx.y, col = threadIdx.x % COLS, run = threadIdx.x / COLS;
+    const int j = blockIdx.x * COLS + col;
+    const float *p = partial + (long long)k * parts * cols + j;
+    float s[4] = {0.f, 0.f, 0.f, 0.f};
+    if (j < cols)
+        for (int i = run; i < parts; i += 4 * RUNS)
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (i + u * RUNS < parts) s[u] += p[(long long)(i + u * RUNS) * cols];
+    float sum = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+    for (int o = COLS; o < 64; o <<= 1) sum += __shfl_xor(sum, o, 64);
+    if ((threadIdx.x & 63) < COLS) red[threadIdx.x >> 6][col] = sum;
+    __syncthreads();
+    if (run != 0 || j >= cols) return;
+    sum = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; ++i) sum += red[i][col];
+    if (j < d) dw[(long long)k * d + j] = sum;
+    else db[(long long)k * d + j - d] = sum;
+}
+
+template <typename T>
+static hipError_t launch_layer(const LayerArgs &a, int K, bool fp8, hipStream_t s)
+{
+#define LAYER_FWD(T, L, W, NV) do { const dim3 grid((unsigned)fwd_groups(a.rows, rms_side<L, W>()), (unsigned)K); \
+    if (fp8) layernorm_kernel<T, L, W, NV, true><<<grid, rms_threads<W>(), 0, s>>>(a); \
+    else layernorm_kernel<T, L, W, NV, false><<<grid, rms_threads<W>(), 0, s>>>(a); } while (0)
+    RMS_BY_WIDTH(T, a.d, LAYER_FWD);
+#undef LAYER_FWD
+    return hipGetLastError();
+}
+
+template <typename T>
+static hipError_t launch_layer_back(LayerBackArgs &a, int K, float *workspace, float *dw, float *db, hipStream_t s)
+{
+    const long long groups = back_groups(K, a.rows, rms_plan(a.d, (int)sizeof(T)));
+    const int cols = a.d * (db != nullptr ? 2 : 1);
+    if (groups == 1) { a.part_w = dw; a.part_b = db; a.s_part = a.d; }
+    else { a.part_w = workspace; a.part_b = workspace + a.d; a.s_part = cols; }
+#define LAYER_BACK(T, L, W, NV) do { const dim3 grid((unsigned)groups, (unsigned)K); \
+    if (db != nullptr) layernorm_back_kernel<T, L, W, NV, true><<<grid, rms_threads<W>(), 0, s>>>(a); \
+    else layernorm_back_kernel<T, L, W, NV, false><<<grid, rms_threads<W>(), 0, s>>>(a); } while (0)
+    RMS_BY_WIDTH(T, a.d, LAYER_BACK);
+#undef LAYER_BACK
+    hipError_t e = hipGetLastError();
+    if (e != hipSuccess || groups == 1) return e;
+    const long long all = (long long)K * cols;
+    const auto sums = all >= 256 * 32 ? layernorm_sums_kernel<32> : all >= 256 * 16 ? layernorm_sums_kernel<16> : layernorm_sums_kernel<8>;
+    const int per = all >= 256 * 32 ? 32 : all >= 256 * 16 ? 16 : 8;
+    sums<<<dim3((unsigned)((cols + per - 1) / per), (unsigned)K), SUM_THREADS, 0, s>>>(workspace, (int)groups, cols, a.d, dw, db);
+    return hipGetLastError();
+}
+
+}  // namespace qsr
+
+using namespace qsr;
+
+static int finish(hipError_t e)
+{
+    if (e == hipSuccess) return QSR_OK;
+    set_last_hip_error((int)e);
+    return QSR_EHIP;
+}
+static bool off(const void *p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) != 0; }
+static uintptr_t size_of(int type) { return type == QSR_TYPE_F32 ? 4 : 2; }
+static bool sizes_ok(int32_t K, int64_t rows, int64_t d)
+{
+    return K >= 1 && K <= 65535 && rows >= 0 && rows <= ((long long)1 << 31) && d >= 1;
+}
+
+extern "C" int qsr_layernorm(const qsr_layernorm_args *q, void *stream)
+{
+    if (!q || !sizes_ok(q->K, q->rows, q->d)) return QSR_EINVAL;
+    if (q->type != QSR_TYPE_F32 && q->type != QSR_TYPE_BF16) return QSR_EINVAL;
+    const bool fp8 = q->y_type == QSR_TYPE_E4M3;
+    if (!fp8 && q->y_type != q->type) return QSR_EINVAL;
+    const uintptr_t es = size_of(q->type);
+    if (!(std::isfinite(q->eps) && q->eps >= 0.0)) return QSR_EINVAL;
+    if (q->d > RMS_MAX_D) return QSR_ELIMIT;
+    if (q->rows == 0) return QSR_OK;
+    if (!q->x || off(q->x, es) || off(q->residual, es) || !q->weight || off(q->weight, 4) || off(q->bias, 4) || off(q->sum, es) || !q->y ||
+        (!fp8 && off(q->y, es)) || off(q->mean, 4) || off(q->rstd, 4) || off(q->scale, 4) || (fp8 && !q->scale))
+        return QSR_EINVAL;
+    if (q->x_stride < q->d || q->y_stride < q->d || (q->residual && q->residual_stride < q->d) || (q->sum && q->sum_stride < q->d) ||
+        (q->K > 1 && (q->weight_stride < q->d || (q->bias && q->bias_stride < q->d))))
+        return QSR_EINVAL;
+    const LayerArgs a{q->x, q->residual, q->weight, q->bias, q->sum, q->y, fp8 ? q->scale : nullptr, q->mean, q->rstd, q->rows, q->x_stride,
+                      q->residual_stride, q->sum_stride, q->y_stride, q->weight_stride, q->bias_stride, (int)q->d, (float)q->eps};
+    return finish(q->type == QSR_TYPE_F32 ? launch_layer<float>(a, q->K, fp8, (hipStream_t)stream)
+                                          : launch_layer<bf16_t>(a, q->K, fp8, (hipStream_t)stream));
+}
+
+extern "C" int qsr_layernorm_workspace_bytes(int32_t K, int64_t rows, int64_t d, int32_t type, size_t *bytes)
+{
+    if (!bytes) return QSR_EINVAL;
+    *bytes = 0;
+    if (!sizes_ok(K, rows, d) || (type != QSR_TYPE_F32 && type != QSR_TYPE_BF16)) return QSR_EINVAL;
+    if (d > RMS_MAX_D) return QSR_ELIMIT;
+    const long long groups = back_groups(K, rows, rms_plan(d, (int)size_of(type)));
+    *bytes = groups == 1 ? 0 : (size_t)K * (size_t)groups * (size_t)(2 * d) * sizeof(float);
+    return QSR_OK;
+}
+
+extern "C" int qsr_layernorm_backward(const qsr_layernorm_backward_args *q, void *workspace, size_t workspace_bytes, void *stream)
+{
+    if (!q || !sizes_ok(q->K, q->rows, q->d)) return QSR_EINVAL;
+    if (q->type != QSR_TYPE_F32 && q->type != QSR_TYPE_BF16) return QSR_EINVAL;
+    const uintptr_t es = size_of(q->type);
+    if (!q->weight || off(q->weight, 4) || !q->weight_grad || off(q->weight_grad, 4) || off(q->bias_grad, 4)) return QSR_EINVAL;
+    if (q->rows > 0 && (!q->y_grad || off(q->y_grad, es) || !q->sum || off(q->sum, es) || !q->mean || off(q->mean, 4) || !q->rstd ||
+                        off(q->rstd, 4) || off(q->residual_grad, es) || !q->x_grad || off(q->x_grad, es)))
+        return QSR_EINVAL;
+    if (q->y_grad_stride < q->d || q->sum_stride < q->d || q->x_grad_stride < q->d ||
+        (q->residual_grad && q->residual_grad_stride < q->d) || (q->K > 1 && q->weight_stride < q->d))
+        return QSR_EINVAL;
+    size_t need = 0;
+    const int rc = qsr_layernorm_workspace_bytes(q->K, q->rows, q->d, q->type, &need);
+    if (rc != QSR_OK) return rc;
+    if (need > 0 && (!workspace || off(workspace, 4))) return QSR_EINVAL;
+    if (workspace_bytes < need) return QSR_ENOMEM;
+    LayerBackArgs a{q->y_grad, q->sum, q->weight, q->mean, q->rstd, q->residual_grad, q->x_grad, nullptr, nullptr, q->rows, 0,
+                    q->y_grad_stride, q->sum_stride, q->residual_grad_stride, q->x_grad_stride, q->weight_stride, (int)q->d};
+    return finish(q->type == QSR_TYPE_F32 ? launch_layer_back<float>(a, q->K, (float *)workspace, q->weight_grad, q->bias_grad, (hipStream_t)stream)
+                                          : launch_layer_back<bf16_t>(a, q->K, (float *)workspace, q->weight_grad, q->bias_grad, (hipStream_t)stream));
+}

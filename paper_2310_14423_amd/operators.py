@@ -1,5 +1,6 @@
 """The operators around a caller's own matrix products (include/qsr.h): AdamW over many tensors, the root-mean-square norm with
-the residual's addition, and the log probabilities of given tokens, each with its gradients.
+the residual's addition, layer norm, the embedding, a gated linear recurrence, and the log probabilities of given tokens, each with its
+gradients.
 
 As in the binding, this is marshalling and the allocation of results and workspaces; nothing is computed in torch.  The calls that a
 model makes in every step go through a small extension (csrc/torch_calls.cpp), the others through ctypes.  All of them work on the
@@ -45,7 +46,7 @@ def _setup():
         from . import _calls as calls
     except ImportError as e:
         raise RuntimeError("the operators' extension cannot be loaded: run `python -m paper_2310_14423_amd.build` (%s)" % e) from e
-    calls.setup(_check, RMSNorm, TokenLogprobs)
+    calls.setup(_check, RMSNorm, TokenLogprobs, LayerNorm, GatedScan)
     _torch, _calls = torch, calls
 
 
@@ -107,6 +108,100 @@ def rmsnorm_backward(y_grad, sum, weight, rstd, residual_grad=None, stream=None)
         return _calls.rmsnorm_backward(y_grad, sum, weight, rstd, residual_grad, s)
     with place:
         return _calls.rmsnorm_backward(y_grad, sum, weight, rstd, residual_grad, s)
+
+
+# ---------------------------------------------------------------------------------------------------
+# layer norm
+# ---------------------------------------------------------------------------------------------------
+LayerNorm = namedtuple("LayerNorm", "y sum mean rstd scale")
+
+
+def layernorm(x, weight, bias=None, residual=None, eps=1e-5, out="same", sum_out=None, stream=None):
+    """y = (s - mean(s)) * rstd * weight + bias for the rows of s = x + residual (or x), as rmsnorm takes and returns them: bias as weight,
+    or None; the result (y, sum, mean, rstd, scale) with the rows' means and rstd = 1 / sqrt(mean((s - mean)^2) + eps), both float32."""
+    if _calls is None:
+        _setup()
+    _need(out == "same" or out == "fp8", "out: 'same' or 'fp8'")
+    s, place = _place(x, stream)
+    with place or _nothing:
+        return _calls.layernorm(x, weight, bias, residual, eps, out == "fp8", sum_out, s)
+
+
+def layernorm_backward(y_grad, sum, weight, mean, rstd, residual_grad=None, bias=True, stream=None):
+    """(x_grad, weight_grad, bias_grad) of layernorm from its `sum`, `mean` and `rstd`, as rmsnorm_backward has them; bias_grad is shaped
+    as weight, or None with bias=False."""
+    if _calls is None:
+        _setup()
+    s, place = _place(sum, stream)
+    with place or _nothing:
+        return _calls.layernorm_backward(y_grad, sum, weight, mean, rstd, residual_grad, bool(bias), s)
+
+
+# ---------------------------------------------------------------------------------------------------
+# embedding
+# ---------------------------------------------------------------------------------------------------
+_TYPES = {"same": -1, "f32": F32, "bf16": BF16}
+
+
+def embedding(tokens, table, scale=1.0, out="same", stream=None):
+    """Rows scale * table[token] of a table [V][d], or [K][V][d] for tokens [K][...], each worker's its own: float32 or bfloat16, rows of
+    any even stride.  tokens: int64, contiguous; outside 0..V-1: none, a row of zeros.  Returns tokens' shape + [d], in the table's type
+    (out="same"), float32 ("f32") or bfloat16 ("bf16")."""
+    if _calls is None:
+        _setup()
+    _need(out in _TYPES, "out: 'same', 'f32' or 'bf16'")
+    s, place = _place(table, stream)
+    with place or _nothing:
+        return _calls.embedding(tokens, table, scale, _TYPES[out], s)
+
+
+def embedding_backward(y_grad, tokens, table, scale=1.0, out=None, accumulate=False, stream=None):
+    """The gradient of embedding's table for y_grad (float32 or bfloat16, rows of any even stride): scale times the sum of the rows of
+    y_grad of each token, zero for the others, shaped and typed as table, of which nothing else is used.  out: a tensor for it, float32 or
+    bfloat16.  accumulate: it is added to what `out` holds (a table that the head shares, several batches); rows that no token names are
+    left alone.  Sums are in a fixed order."""
+    if _calls is None:
+        _setup()
+    s, place = _place(table, stream)
+    with place or _nothing:
+        return _calls.embedding_backward(y_grad, tokens, table, scale, out, bool(accumulate), s)
+
+
+# ---------------------------------------------------------------------------------------------------
+# gated linear recurrence
+# ---------------------------------------------------------------------------------------------------
+GatedScan = namedtuple("GatedScan", "h last states")
+_INPUTS = {"complement": 0, "plain": 1}     # QSR_SCAN_*
+
+
+def gated_scan(x, gate, initial=None, reset=None, lengths=None, input="complement", keep=False, state_out=None, stream=None):
+    """h_t = a_t h_{t-1} + (1 - a_t) x_t (input="complement") or a_t h_{t-1} + x_t ("plain") with a_t = sigmoid(gate_t), over the steps t of
+    x and gate [..., T, d], for each channel by itself; float32 or bfloat16, each step's channels side by side, steps and sequences at any
+    even stride (two parts of one product's output, time before batch).  States are float32.
+      initial    [..., d]: h_{-1}; None: zeros
+      reset      [..., T] bool: steps that take no state from before them (documents that are packed into one sequence)
+      lengths    [...] int64: steps that there are; what is behind them is not read, h is 0 there
+      keep       return `states` for the backward pass
+      state_out  a float32 tensor [..., d] for `last`, which may be initial
+    Returns (h, last, states): h in x's type, last [..., d] the states behind the sequences' ends, from which the next steps go on (one
+    token at a time: T = 1), states or None."""
+    if _calls is None:
+        _setup()
+    _need(input in _INPUTS, "input: 'complement' or 'plain'")
+    s, place = _place(x, stream)
+    with place or _nothing:
+        return _calls.gated_scan(x, gate, initial, reset, lengths, _INPUTS[input], bool(keep), state_out, s)
+
+
+def gated_scan_backward(h_grad, x, gate, states, reset=None, lengths=None, last_grad=None, input="complement", stream=None):
+    """(x_grad, gate_grad, initial_grad) of gated_scan for the gradients of h (in x's type) and of last (float32, or None: zero), from the
+    same x, gate, reset, lengths and input and the `states` that were kept.  initial_grad is float32."""
+    if _calls is None:
+        _setup()
+    _need(input in _INPUTS, "input: 'complement' or 'plain'")
+    s, place = _place(x, stream)
+    with place or _nothing:
+        return _calls.gated_scan_backward(h_grad, x, gate, states, reset, lengths, last_grad, _INPUTS[input], s)
 
 
 # ---------------------------------------------------------------------------------------------------
