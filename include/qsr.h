@@ -443,7 +443,7 @@ int qsr_embedding_backward(const qsr_embedding_backward_args *args, void *worksp
  * there are (less than 0 is none, more than `steps` is all); x and gate behind them are not read, h behind them is 0, last is the
  * state at the end.  states: [batch][ceil(steps / QSR_SCAN_STEPS)][d] floats for the backward pass, the state that every
  * QSR_SCAN_STEPS-th step begins with, or NULL.  reset, lengths: without gaps.  The rows of h share no element, with each other or with
- * x and gate.  steps at most 2^30, d at most 2^28 (QSR_ELIMIT). */
+ * x and gate.  QSR_ELIMIT above 2^30 steps, 2^28 channels, or 2^24 elements from step to step. */
 enum { QSR_SCAN_STEPS = 16 };
 enum { QSR_SCAN_COMPLEMENT = 0, QSR_SCAN_PLAIN = 1 };
 typedef struct {

@@ -13,6 +13,8 @@
 // A reset cuts a map off from what was before: A = -1 stands for that (A is never negative), so that an infinity or a NaN ends there too.
 // All arithmetic is fp32.
 #include <cmath>
+#include <initializer_list>
+#include <type_traits>
 
 #include "qsr_internal.h"
 #include "row_io.h"
@@ -21,7 +23,7 @@
 namespace qsr {
 
 constexpr int STEPS = QSR_SCAN_STEPS;
-constexpr int SCAN_WAVES = 8;                  // wavefronts to a workgroup, where sequences are longer than one of them takes
+constexpr int WAVES = 8, MANY_WAVES = 16;      // wavefronts to a workgroup, where sequences are longer than one of them takes
 
 struct ScanArgs {
     const void *x, *f, *dh;
@@ -32,66 +34,101 @@ struct ScanArgs {
     const uint8_t *reset;
     const int64_t *lengths;
     float2 *maps;                              // [B][parts + 1][d]: forward, the initial state, then the maps of all parts but the last
-    long long s_x, s_f, s_dh, s_h, s_dx, s_df; // from step to step
-    long long b_x, b_f, b_dh, b_h, b_dx, b_df; // and from sequence to sequence
+    long long b_x, b_f, b_dh, b_h, b_dx, b_df; // from sequence to sequence
+    int s_x, s_f, s_dh, s_h, s_dx, s_df;       // and from step to step, in bytes
     long long tiles;
     int T, d, groups, parts, part_len;
 };
 
-// a and c of the gate f.  exp(-|f|) has no overflow, and both come out with the relative precision of a float.
-template <typename T> __device__ __forceinline__ void gates(float f, float &a, float &c)
+// exp(-x) for 0 <= x.  What the argument to the base 2 loses to rounding is put back, since a state remembers thousands of steps' gates: a
+// number in bf16 times a factor of 16 bits loses nothing, and the rest of the factor is small.
+template <typename T> __device__ __forceinline__ float exp_minus(float x)
 {
-    float e, big;
-    if constexpr (sizeof(T) == 2) {            // 2^-20 of an error at most, beside the gate's own 2^-9
-        e = __builtin_amdgcn_exp2f(-1.44269504f * fabsf(f));
-        big = __builtin_amdgcn_rcpf(1.f + e);
+    constexpr float LN2 = 0.693147181f;
+    if constexpr (sizeof(T) == 2) {
+        constexpr float L = 1.44268799f, L_REST = 7.05260771e-6f;          // log2(e) = L + L_REST
+        const float e = __builtin_amdgcn_exp2f(-L * x);
+        return fmaf(e, (-LN2 * L_REST) * x, e);
     } else {
-        e = expf(-fabsf(f));
-        const float s = 1.f + e, r = __builtin_amdgcn_rcpf(s);
-        big = fmaf(fmaf(-s, r, 1.f), r, r);
+        constexpr float L = 1.44269504f, L_REST = 1.92596303e-8f;
+        const float t = L * x, rest = fmaf(L_REST, x, fmaf(L, x, -t)), e = __builtin_amdgcn_exp2f(-t);
+        return fmaf(e, -LN2 * rest, e);
     }
-    const float small = e * big;
+}
+// The larger and the smaller one of a = sigmoid(f) and c = 1 - a, both with the relative precision of a float.  a is the larger one
+// where f has no sign.  From |f| = 200 on the smaller one is 0; a NaN stays.
+template <typename T> __device__ __forceinline__ void gates(float f, float &big, float &small)
+{
+    const float e = exp_minus<T>(__builtin_elementwise_minimum(fabsf(f), 200.f));
+    const float s = 1.f + e, r = __builtin_amdgcn_rcpf(s);
+    big = fmaf(fmaf(-s, r, 1.f), r, r);
+    small = e * big;
+}
+template <typename T> __device__ __forceinline__ void gates_of(float f, float &a, float &c)
+{
+    float big, small;
+    gates<T>(f, big, small);
     a = f >= 0.f ? big : small;
     c = f >= 0.f ? small : big;
 }
+// Both in one number: the smaller one, with a's place in the sign.  1 - small is the larger one with a rounding of half a unit.
+template <typename T> __device__ __forceinline__ float gates_in_one(float f) { float big, small; gates<T>(f, big, small); return copysignf(small, f); }
+__device__ __forceinline__ float a_of(float v) { return __float_as_int(v) >= 0 ? 1.f - v : -v; }
+__device__ __forceinline__ float c_of(float v) { return __float_as_int(v) >= 0 ? v : 1.f + v; }
 
 // A map (A, H) behind h
 __device__ __forceinline__ float behind_map(float A, float H, float h) { return A < 0.f ? H : fmaf(A, h, H); }
 
-template <typename T, int V> struct Rows { typename Wide<T, V>::vec v[STEPS]; };
-
-// The rows first .. first + n - 1 of a sequence at p (which points at the lane's channels); those behind them again the last one
-template <typename T, int V>
-__device__ __forceinline__ void load_rows(const T *p, uint32_t at, long long stride, long long first, int n, Rows<T, V> &r)
+// A lane's V channels in a word (V = 1 in bf16: half of one)
+template <typename T, int V> __device__ __forceinline__ float channel(uint32_t w, int u)
 {
-    if (n <= 0) return;
-    p += first * stride;
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s) r.v[s] = *(const typename Wide<T, V>::vec *)behind(p + min(s, n - 1) * stride, at);
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w);
+    else return __uint_as_float(u == 0 ? w << 16 : w & 0xffff0000u);
 }
-// without loads of rows that are not there, for few of them
-template <typename T, int V>
-__device__ __forceinline__ void load_few(const T *p, uint32_t at, long long stride, int n, Rows<T, V> &r)
+template <typename T, int V> __device__ __forceinline__ uint32_t word_of(const float (&v)[V])
 {
-#pragma unroll
-    for (int s = 0; s < STEPS; ++s)
-        if (s < n) r.v[s] = *(const typename Wide<T, V>::vec *)behind(p + s * stride, at);
-}
-
-template <typename T, int V>
-__device__ __forceinline__ void store_channels(T *p, uint32_t at, const float (&v)[V], int skip)
-{
-    if (skip == 0) store_wide<T, V, true>(behind(p, at), v);
+    if constexpr (sizeof(T) == 4) return __float_as_uint(v[0]);
     else {
+        typedef bf16_t Two __attribute__((ext_vector_type(2)));
+        const Two two = {(bf16_t)v[0], (bf16_t)v[V - 1]};
+        return __builtin_bit_cast(uint32_t, two);
+    }
+}
+
+// Rows of a sequence as a buffer: what is the same for a wavefront (where the rows are, how far apart) stays out of its lanes' registers
+// and instructions.  2^31 bytes from a tile's first row on; an offset of NOWHERE is outside, and its store is dropped.
+constexpr uint32_t NOWHERE = 0x80000000u;
+typedef __amdgpu_buffer_rsrc_t Rows;
+__device__ __forceinline__ Rows rows_at(const void *base, long long seq, int t, int step)
+{
+    return __builtin_amdgcn_make_buffer_rsrc((char *)const_cast<void *>(base) + seq + (long long)t * step, 0, NOWHERE, 0x00020000);
+}
+template <typename T, int V> __device__ __forceinline__ uint32_t load_word(Rows r, uint32_t at, int row)
+{
+    if constexpr (V * sizeof(T) == 2) return __builtin_amdgcn_raw_buffer_load_b16(r, (int)at, row, 0);
+    else return __builtin_amdgcn_raw_buffer_load_b32(r, (int)at, row, 0);
+}
+// The first n of STEPS rows; zeros for the others
+template <typename T, int V>
+__device__ __forceinline__ void load_rows(Rows r, uint32_t at, int step, int n, uint32_t (&w)[STEPS])
+{
+    if (n >= STEPS) {
 #pragma unroll
-        for (int u = 0; u < V; ++u)
-            if (u >= skip && skip < V) behind(p, at)[u] = (T)v[u];
+        for (int s = 0; s < STEPS; ++s) w[s] = load_word<T, V>(r, at, s * step);
+    } else {
+#pragma unroll
+        for (int s = 0; s < STEPS; ++s) {
+            w[s] = 0;
+            if (s < n) w[s] = load_word<T, V>(r, at, s * step);
+        }
     }
 }
 
 // A lane's place: V channels from `at`, of which the first `skip` are another lane's (V: all of them)
-template <int V> struct Place {
+template <typename T, int V> struct Place {
     int b, part, at, skip, len;
+    uint32_t in, out, half;                    // offsets in a row: for loads, for stores of all V channels, and of the last one alone
+    bool halves;                               // some lane of the wavefront has that
     __device__ __forceinline__ bool find(const ScanArgs &a, int lane, int parts)
     {
         const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
@@ -102,6 +139,10 @@ template <int V> struct Place {
         part = (int)(seq - (long long)b * parts);
         at = min(first, a.d - V);
         skip = min(first - at, V);
+        in = (uint32_t)at * (uint32_t)sizeof(T);
+        out = skip == 0 ? in : NOWHERE;
+        half = skip == 1 && V == 2 ? in + (uint32_t)sizeof(T) : NOWHERE;
+        halves = V == 2 && __ballot(skip == 1) != 0;
         len = a.T;
         if (a.lengths != nullptr) {
             const long long n = a.lengths[b];
@@ -109,9 +150,27 @@ template <int V> struct Place {
         }
         return true;
     }
+    // STREAM: lines that are written as a whole and need not stay
+    template <bool STREAM> __device__ __forceinline__ void store(Rows r, int row, const float (&v)[V]) const
+    {
+        constexpr int NT = STREAM ? 2 : 0;
+        const uint32_t w = word_of<T, V>(v);
+        if constexpr (V * sizeof(T) == 2) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)w, r, (int)out, row, NT);
+        else {
+            __builtin_amdgcn_raw_buffer_store_b32(w, r, (int)out, row, NT);
+            if (V == 2 && halves) __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w >> 16), r, (int)half, row, NT);
+        }
+    }
+    // fp32 numbers of one row of d
+    __device__ __forceinline__ void store_floats(float *row, const float (&v)[V]) const
+    {
+#pragma unroll
+        for (int u = 0; u < V; ++u)
+            if (u >= skip) row[at + u] = v[u];
+    }
 };
 
-// The marks of steps t .. t + STEPS - 1, a bit each
+// The marks of steps t .. t + n - 1, a bit each
 __device__ __forceinline__ uint32_t marks(const ScanArgs &a, int b, int t, int n, int lane)
 {
     if (a.reset == nullptr || n <= 0) return 0;
@@ -119,22 +178,27 @@ __device__ __forceinline__ uint32_t marks(const ScanArgs &a, int b, int t, int n
     return (uint32_t)__ballot(m != 0 && lane < n);
 }
 
+// f(true) where a tile ends early or has marks, f(false) where every step is as the others
+template <typename F> __device__ __forceinline__ void by_tile(bool plain, F f)
+{
+    if (plain) f(std::integral_constant<bool, false>());
+    else f(std::integral_constant<bool, true>());
+}
+
 // Forward, W wavefronts to a workgroup
-template <typename T, int V, int W, bool COMP>
-__global__ __launch_bounds__(64 * W) void scan_kernel(ScanArgs a)
+template <typename T, int V, int W, bool COMP, bool STREAM>
+__global__ __launch_bounds__(64 * W, 4) void scan_kernel(ScanArgs a)
 {
     __shared__ float2 maps[2][W][V][64];
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Place<V> q;
+    Place<T, V> q;
     if (!q.find(a, lane, a.parts)) return;
-    const T *const px = (const T *)a.x + q.b * a.b_x, *const pf = (const T *)a.f + q.b * a.b_f;
-    const uint32_t at = (uint32_t)q.at * (uint32_t)sizeof(T);
     float carry[V];
     if (a.parts > 1) {
         const float2 *const m = a.maps + ((long long)q.b * (a.parts + 1)) * a.d + q.at;
 #pragma unroll
         for (int u = 0; u < V; ++u) carry[u] = 0.f;
-#pragma unroll 4
+#pragma unroll 16
         for (int p = 0; p <= q.part; ++p)
 #pragma unroll
             for (int u = 0; u < V; ++u) { const float2 f = m[(long long)p * a.d + u]; carry[u] = behind_map(f.x, f.y, carry[u]); }
@@ -146,44 +210,49 @@ __global__ __launch_bounds__(64 * W) void scan_kernel(ScanArgs a)
         }
     }
     const int begin = q.part * a.part_len, end = min(a.T, begin + a.part_len);
-    Rows<T, V> rx, rf;
-    uint32_t bits = 0;
+    uint32_t rx[STEPS], rf[STEPS], bits = 0;
     auto load = [&](int t0) {
         const int t = t0 + wave * STEPS, n = min(q.len - t, STEPS);
-        if (W == 1) { load_few<T, V>(px, at, a.s_x, n, rx); load_few<T, V>(pf, at, a.s_f, n, rf); }
-        else { load_rows<T, V>(px, at, a.s_x, t, n, rx); load_rows<T, V>(pf, at, a.s_f, t, n, rf); }
+        load_rows<T, V>(rows_at(a.x, q.b * a.b_x, t, a.s_x), q.in, a.s_x, n, rx);
+        load_rows<T, V>(rows_at(a.f, q.b * a.b_f, t, a.s_f), q.in, a.s_f, n, rf);
         bits = marks(a, q.b, t, n, lane);
     };
-    if (begin < end) load(begin);
     int turn = 0;
 #pragma unroll 1
     for (int t0 = begin; t0 < end; t0 += W * STEPS, turn ^= 1) {
         const int t = t0 + wave * STEPS, n = min(q.len - t, STEPS);
+        load(t0);
         const uint32_t cut = bits;
-        float ga[STEPS][V], gb[STEPS][V];
+        float ga[STEPS][V], gb[STEPS][V], A[V], H[V], h[V];
 #pragma unroll
         for (int s = 0; s < STEPS; ++s)
 #pragma unroll
             for (int u = 0; u < V; ++u) {
                 float c;
-                gates<T>((float)rf.v[s][u], ga[s][u], c);
-                gb[s][u] = COMP ? c * (float)rx.v[s][u] : (float)rx.v[s][u];
-                if (s >= n) { ga[s][u] = 1.f; gb[s][u] = 0.f; }            // behind the end the state stays
+                const float x = channel<T, V>(rx[s], u);
+                gates_of<T>(channel<T, V>(rf[s], u), ga[s][u], c);
+                gb[s][u] = COMP ? c * x : x;
             }
-        if (t0 + W * STEPS < end) load(t0 + W * STEPS);
-        float h[V];
-        if (W > 1) {
-            float A[V], H[V];
-#pragma unroll
-            for (int u = 0; u < V; ++u) { A[u] = 1.f; H[u] = 0.f; }
+        if (n < STEPS) {                       // behind the end the state stays
 #pragma unroll
             for (int s = 0; s < STEPS; ++s)
 #pragma unroll
-                for (int u = 0; u < V; ++u) {
-                    if (cut >> s & 1) H[u] = 0.f;
-                    H[u] = fmaf(ga[s][u], H[u], gb[s][u]);
-                    A[u] *= ga[s][u];
-                }
+                for (int u = 0; u < V; ++u)
+                    if (s >= n) { ga[s][u] = 1.f; gb[s][u] = 0.f; }
+        }
+#pragma unroll
+        for (int u = 0; u < V; ++u) { A[u] = 1.f; H[u] = 0.f; }
+        if (W > 1) {
+            by_tile(cut == 0, [&](auto marked) {
+#pragma unroll
+                for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                    for (int u = 0; u < V; ++u) {
+                        if (marked() && (cut >> s & 1)) H[u] = 0.f;
+                        H[u] = fmaf(ga[s][u], H[u], gb[s][u]);
+                        A[u] *= ga[s][u];
+                    }
+            });
 #pragma unroll
             for (int u = 0; u < V; ++u) maps[turn][wave][u][lane] = make_float2(cut ? -1.f : A[u], H[u]);
             __syncthreads();
@@ -199,84 +268,102 @@ __global__ __launch_bounds__(64 * W) void scan_kernel(ScanArgs a)
 #pragma unroll
             for (int u = 0; u < V; ++u) h[u] = carry[u];
         }
-        if (a.states != nullptr && t < end)
-            store_channels<float, V>(a.states + ((long long)q.b * ((a.T + STEPS - 1) / STEPS) + t / STEPS) * a.d, (uint32_t)q.at * 4, h, q.skip);
-        T *const ph = (T *)a.h + q.b * a.b_h + t * a.s_h;
+        if (t < end) {
+            if (a.states != nullptr) q.store_floats(a.states + ((long long)q.b * ((a.T + STEPS - 1) / STEPS) + t / STEPS) * a.d, h);
+            const Rows rh = rows_at(a.h, q.b * a.b_h, t, a.s_h);
+            by_tile(cut == 0 && n >= STEPS, [&](auto marked) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s) {
-            float y[V];
+                for (int s = 0; s < STEPS; ++s) {
+                    float y[V];
 #pragma unroll
-            for (int u = 0; u < V; ++u) {
-                if (cut >> s & 1) h[u] = 0.f;
-                h[u] = fmaf(ga[s][u], h[u], gb[s][u]);
-                y[u] = s < n ? h[u] : 0.f;
-            }
-            if (t + s < end) store_channels<T, V>(ph + s * a.s_h, at, y, q.skip);
+                    for (int u = 0; u < V; ++u) {
+                        if (marked() && (cut >> s & 1)) h[u] = 0.f;
+                        h[u] = fmaf(ga[s][u], h[u], gb[s][u]);
+                        y[u] = !marked() || s < n ? h[u] : 0.f;
+                    }
+                    if (!marked() || t + s < end) q.template store<STREAM>(rh, s * a.s_h, y);
+                }
+            });
         }
         if (W == 1)
 #pragma unroll
             for (int u = 0; u < V; ++u) carry[u] = h[u];
     }
-    if (a.last != nullptr && q.part == a.parts - 1 && wave == 0)
-        store_channels<float, V>(a.last + (long long)q.b * a.d, (uint32_t)q.at * 4, carry, q.skip);
+    if (a.last != nullptr && q.part == a.parts - 1 && wave == 0) q.store_floats(a.last + (long long)q.b * a.d, carry);
 }
 
-// The maps of parts: a wavefront goes through a run of its part's steps.  Forward: all parts but the last, and the initial state.
-// Backward: e before a part from e behind it, all parts but the first.
+// The maps of parts: a wavefront goes through a run of its part's steps, from its end.  Forward: all parts but the last, and the initial
+// state.  Backward: e before a part from e behind it, all parts but the first.
 template <typename T, int V, bool COMP, bool BACK>
-__global__ __launch_bounds__(64 * SCAN_WAVES) void scan_maps_kernel(ScanArgs a)
+__global__ __launch_bounds__(64 * WAVES) void scan_maps_kernel(ScanArgs a)
 {
-    __shared__ float2 maps[SCAN_WAVES][V][64];
+    __shared__ float2 maps[WAVES][V][64];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Place<V> q;
+    Place<T, V> q;
     if (!q.find(a, lane, a.parts - 1)) return;
     const int part = BACK ? q.part + 1 : q.part;
-    const T *const px = (const T *)(BACK ? a.dh : a.x) + q.b * (BACK ? a.b_dh : a.b_x), *const pf = (const T *)a.f + q.b * a.b_f;
-    const long long s_x = BACK ? a.s_dh : a.s_x;
-    const uint32_t at = (uint32_t)q.at * (uint32_t)sizeof(T);
-    const int each = a.part_len / SCAN_WAVES, begin = part * a.part_len + wave * each, end = min(a.T, begin + each);
+    const void *const vx = BACK ? a.dh : a.x;
+    const long long b_x = q.b * (BACK ? a.b_dh : a.b_x);
+    const int s_x = BACK ? a.s_dh : a.s_x;
+    const int each = a.part_len / WAVES, begin = part * a.part_len + wave * each, end = min(a.T, begin + each);
     const int trips = begin < end ? (end - begin + STEPS - 1) / STEPS : 0;
-    Rows<T, V> rx, rf;
-    uint32_t bits = 0;
-    auto start_of = [&](int i) { return begin + (BACK ? trips - 1 - i : i) * STEPS; };
+    uint32_t rx[STEPS], rf[STEPS], bits = 0, any = 0;
+    // Forward, a part's first steps are read last: the launch behind begins with them, and finds them in the last-level cache
+    auto start_of = [&](int i) { return begin + (BACK ? i : trips - 1 - i) * STEPS; };
     auto load = [&](int t) {
         const int n = min(q.len - t, STEPS);
-        load_rows<T, V>(px, at, s_x, t, n, rx);
-        load_rows<T, V>(pf, at, a.s_f, t, n, rf);
+        load_rows<T, V>(rows_at(vx, b_x, t, s_x), q.in, s_x, n, rx);
+        load_rows<T, V>(rows_at(a.f, q.b * a.b_f, t, a.s_f), q.in, a.s_f, n, rf);
         bits = marks(a, q.b, t, n, lane);
     };
     float A[V], H[V];
-    uint32_t any = 0;
 #pragma unroll
     for (int u = 0; u < V; ++u) { A[u] = 1.f; H[u] = 0.f; }
-    if (trips > 0) load(start_of(0));
 #pragma unroll 1
     for (int i = 0; i < trips; ++i) {
         const int n = min(q.len - start_of(i), STEPS);
+        load(start_of(i));
         const uint32_t cut = bits;
-        const Rows<T, V> x = rx, f = rf;
-        if (i + 1 < trips) load(start_of(i + 1));
-        any |= cut;
+        float ga[STEPS][V], gb[STEPS][V], P[V], E[V];
 #pragma unroll
-        for (int o = 0; o < STEPS; ++o) {
-            const int s = BACK ? STEPS - 1 - o : o;
-            if (s < n) {
+        for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+            for (int u = 0; u < V; ++u) {
+                float c;
+                const float x = channel<T, V>(rx[s], u);
+                gates_of<T>(channel<T, V>(rf[s], u), ga[s][u], c);
+                gb[s][u] = BACK || !COMP ? x : c * x;
+            }
+        if (n < STEPS) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int u = 0; u < V; ++u)
+                    if (s >= n) { ga[s][u] = 1.f; gb[s][u] = 0.f; }
+        }
+#pragma unroll
+        for (int u = 0; u < V; ++u) { P[u] = 1.f; E[u] = 0.f; }
+        // the map of these steps
+        by_tile(cut == 0, [&](auto marked) {
+#pragma unroll
+            for (int o = 0; o < STEPS; ++o) {
+                const int s = BACK ? STEPS - 1 - o : o;
 #pragma unroll
                 for (int u = 0; u < V; ++u) {
-                    float ga, c;
-                    gates<T>((float)f.v[s][u], ga, c);
-                    const float v = (float)x.v[s][u];
-                    if (BACK) {
-                        H[u] = ga * (v + H[u]);
-                        if (cut >> s & 1) H[u] = 0.f;
-                    } else {
-                        if (cut >> s & 1) H[u] = 0.f;
-                        H[u] = fmaf(ga, H[u], COMP ? c * v : v);
-                    }
-                    A[u] *= ga;
+                    if (!BACK && marked() && (cut >> s & 1)) E[u] = 0.f;
+                    E[u] = BACK ? ga[s][u] * (gb[s][u] + E[u]) : fmaf(ga[s][u], E[u], gb[s][u]);
+                    if (BACK && marked() && (cut >> s & 1)) E[u] = 0.f;
+                    P[u] *= ga[s][u];
                 }
             }
+        });
+        // in front of (forward, from the end) or behind (backward, from the start, where later steps come first) those before
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            H[u] = any ? H[u] : fmaf(A[u], E[u], H[u]);
+            A[u] *= P[u];
         }
+        any |= cut;
     }
 #pragma unroll
     for (int u = 0; u < V; ++u) maps[wave][u][lane] = make_float2(any ? -1.f : A[u], H[u]);
@@ -285,10 +372,10 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void scan_maps_kernel(ScanArgs a)
 #pragma unroll
     for (int u = 0; u < V; ++u) { A[u] = 1.f; H[u] = 0.f; }
 #pragma unroll
-    for (int i = 0; i < SCAN_WAVES; ++i)
+    for (int i = 0; i < WAVES; ++i)
 #pragma unroll
         for (int u = 0; u < V; ++u) {
-            const float2 m = maps[BACK ? SCAN_WAVES - 1 - i : i][u][lane];
+            const float2 m = maps[BACK ? WAVES - 1 - i : i][u][lane];
             H[u] = behind_map(m.x, m.y, H[u]);
             A[u] = m.x < 0.f || A[u] < 0.f ? -1.f : A[u] * m.x;
         }
@@ -302,45 +389,37 @@ __global__ __launch_bounds__(64 * SCAN_WAVES) void scan_maps_kernel(ScanArgs a)
 }
 
 // Backward, W wavefronts to a workgroup, from the end
-template <typename T, int V, int W, bool COMP>
+template <typename T, int V, int W, bool COMP, bool STREAM>
 __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
 {
     __shared__ float2 maps[2][W][V][64];
     const int lane = threadIdx.x & 63, wave = W == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    Place<V> q;
+    Place<T, V> q;
     if (!q.find(a, lane, a.parts)) return;
-    const T *const px = (const T *)a.x + q.b * a.b_x, *const pf = (const T *)a.f + q.b * a.b_f, *const pg = (const T *)a.dh + q.b * a.b_dh;
-    const float *const ps = a.states + (long long)q.b * ((a.T + STEPS - 1) / STEPS) * a.d + q.at;
-    const uint32_t at = (uint32_t)q.at * (uint32_t)sizeof(T);
     float carry[V];
 #pragma unroll
     for (int u = 0; u < V; ++u) carry[u] = a.initial != nullptr ? a.initial[(long long)q.b * a.d + q.at + u] : 0.f;
     if (a.parts > 1) {
         const float2 *const m = a.maps + ((long long)q.b * (a.parts + 1)) * a.d + q.at;
-#pragma unroll 4
+#pragma unroll 16
         for (int p = a.parts - 1; p > q.part; --p)
 #pragma unroll
             for (int u = 0; u < V; ++u) { const float2 f = m[(long long)p * a.d + u]; carry[u] = behind_map(f.x, f.y, carry[u]); }
     }
     const int begin = q.part * a.part_len, end = min(a.T, begin + a.part_len);
     const int trips = begin < end ? (end - begin + W * STEPS - 1) / (W * STEPS) : 0;
-    Rows<T, V> rx, rf, rg;
+    uint32_t rx[STEPS], rf[STEPS], rg[STEPS], bits = 0;
     float rs[V] = {};
-    uint32_t bits = 0;
     auto load = [&](int t0) {
         const int t = t0 + wave * STEPS, n = min(q.len - t, STEPS);
-        if (W == 1) {
-            load_few<T, V>(px, at, a.s_x, n, rx);
-            load_few<T, V>(pf, at, a.s_f, n, rf);
-            load_few<T, V>(pg, at, a.s_dh, n, rg);
-        } else {
-            load_rows<T, V>(px, at, a.s_x, t, n, rx);
-            load_rows<T, V>(pf, at, a.s_f, t, n, rf);
-            load_rows<T, V>(pg, at, a.s_dh, t, n, rg);
-        }
-        if (n > 0)
+        load_rows<T, V>(rows_at(a.f, q.b * a.b_f, t, a.s_f), q.in, a.s_f, n, rf);
+        load_rows<T, V>(rows_at(a.x, q.b * a.b_x, t, a.s_x), q.in, a.s_x, n, rx);
+        load_rows<T, V>(rows_at(a.dh, q.b * a.b_dh, t, a.s_dh), q.in, a.s_dh, n, rg);
+        if (n > 0) {
+            const float *const row = a.states + ((long long)q.b * ((a.T + STEPS - 1) / STEPS) + t / STEPS) * a.d + q.at;
 #pragma unroll
-            for (int u = 0; u < V; ++u) rs[u] = ps[(long long)(t / STEPS) * a.d + u];
+            for (int u = 0; u < V; ++u) rs[u] = row[u];
+        }
         bits = marks(a, q.b, t, n, lane);
     };
     if (trips > 0) load(begin + (trips - 1) * W * STEPS);
@@ -349,31 +428,49 @@ __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
     for (int i = trips - 1; i >= 0; --i, turn ^= 1) {
         const int t = begin + i * W * STEPS + wave * STEPS, n = min(q.len - t, STEPS);
         const uint32_t cut = bits;
-        float ga[STEPS][V], gc[STEPS][V], h[V];
-        const Rows<T, V> x = rx, g = rg;
-#pragma unroll
-        for (int s = 0; s < STEPS; ++s)
-#pragma unroll
-            for (int u = 0; u < V; ++u) {
-                gates<T>((float)rf.v[s][u], ga[s][u], gc[s][u]);
-                if (s >= n) ga[s][u] = 1.f;
-            }
+        uint32_t x[STEPS], g[STEPS];
+        float v[STEPS][V], before[STEPS][V], h[V], e[V];
 #pragma unroll
         for (int u = 0; u < V; ++u) h[u] = rs[u];
+        // the gates, and the states before each step
+        by_tile(cut == 0, [&](auto marked) {
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s) {
+                x[s] = rx[s];
+                g[s] = rg[s];
+#pragma unroll
+                for (int u = 0; u < V; ++u) {
+                    v[s][u] = gates_in_one<T>(channel<T, V>(rf[s], u));
+                    if (marked() && (cut >> s & 1)) h[u] = 0.f;
+                    before[s][u] = h[u];
+                    const float y = channel<T, V>(x[s], u);
+                    h[u] = fmaf(a_of(v[s][u]), h[u], COMP ? c_of(v[s][u]) * y : y);
+                }
+            }
+        });
         if (i > 0) load(begin + (i - 1) * W * STEPS);
-        float e[V];
+        if (n < STEPS) {                       // behind the end: a = 1, and no gradients (g is 0)
+#pragma unroll
+            for (int s = 0; s < STEPS; ++s)
+#pragma unroll
+                for (int u = 0; u < V; ++u)
+                    if (s >= n) v[s][u] = 0.f;
+        }
         if (W > 1) {
             float A[V], H[V];
 #pragma unroll
             for (int u = 0; u < V; ++u) { A[u] = 1.f; H[u] = 0.f; }
+            by_tile(cut == 0, [&](auto marked) {
 #pragma unroll
-            for (int s = STEPS - 1; s >= 0; --s)
+                for (int s = STEPS - 1; s >= 0; --s)
 #pragma unroll
-                for (int u = 0; u < V; ++u) {
-                    H[u] = ga[s][u] * (H[u] + (s < n ? (float)g.v[s][u] : 0.f));
-                    if (cut >> s & 1) H[u] = 0.f;
-                    A[u] *= ga[s][u];
-                }
+                    for (int u = 0; u < V; ++u) {
+                        const float ga = a_of(v[s][u]);
+                        H[u] = ga * (H[u] + channel<T, V>(g[s], u));
+                        if (marked() && (cut >> s & 1)) H[u] = 0.f;
+                        A[u] *= ga;
+                    }
+            });
 #pragma unroll
             for (int u = 0; u < V; ++u) maps[turn][wave][u][lane] = make_float2(cut ? -1.f : A[u], H[u]);
             __syncthreads();
@@ -389,41 +486,33 @@ __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
 #pragma unroll
             for (int u = 0; u < V; ++u) e[u] = carry[u];
         }
-        float before[STEPS][V];
+        if (t < end) {
+            const Rows rdx = rows_at(a.dx, q.b * a.b_dx, t, a.s_dx), rdf = rows_at(a.df, q.b * a.b_df, t, a.s_df);
+            by_tile(cut == 0 && n >= STEPS, [&](auto marked) {
 #pragma unroll
-        for (int s = 0; s < STEPS; ++s)
+                for (int s = STEPS - 1; s >= 0; --s) {
+                    float dx[V], df[V];
 #pragma unroll
-            for (int u = 0; u < V; ++u) {
-                if (cut >> s & 1) h[u] = 0.f;
-                before[s][u] = h[u];
-                const float v = (float)x.v[s][u];
-                h[u] = fmaf(ga[s][u], h[u], COMP ? gc[s][u] * v : v);
-            }
-        T *const pdx = (T *)a.dx + q.b * a.b_dx + t * a.s_dx, *const pdf = (T *)a.df + q.b * a.b_df + t * a.s_df;
-#pragma unroll
-        for (int s = STEPS - 1; s >= 0; --s) {
-            float dx[V], df[V];
-#pragma unroll
-            for (int u = 0; u < V; ++u) {
-                if (s < n) {
-                    const float v = (float)x.v[s][u], grad = (float)g.v[s][u] + e[u];
-                    dx[u] = COMP ? gc[s][u] * grad : grad;
-                    e[u] = ga[s][u] * grad;
-                    df[u] = e[u] * gc[s][u] * (COMP ? before[s][u] - v : before[s][u]);
-                    if (cut >> s & 1) e[u] = 0.f;
-                } else dx[u] = df[u] = 0.f;
-            }
-            if (t + s < end) {
-                store_channels<T, V>(pdx + s * a.s_dx, at, dx, q.skip);
-                store_channels<T, V>(pdf + s * a.s_df, at, df, q.skip);
-            }
+                    for (int u = 0; u < V; ++u) {
+                        const float ga = a_of(v[s][u]), gc = c_of(v[s][u]), grad = channel<T, V>(g[s], u) + e[u];
+                        dx[u] = COMP ? gc * grad : grad;
+                        const float down = ga * grad;
+                        df[u] = down * gc * (COMP ? before[s][u] - channel<T, V>(x[s], u) : before[s][u]);
+                        e[u] = marked() && (cut >> s & 1) ? 0.f : down;
+                        if (marked() && s >= n) { dx[u] = df[u] = 0.f; }
+                    }
+                    if (!marked() || t + s < end) {
+                        q.template store<STREAM>(rdx, s * a.s_dx, dx);
+                        q.template store<STREAM>(rdf, s * a.s_df, df);
+                    }
+                }
+            });
         }
         if (W == 1)
 #pragma unroll
             for (int u = 0; u < V; ++u) carry[u] = e[u];
     }
-    if (a.last != nullptr && q.part == 0 && wave == 0)
-        store_channels<float, V>(a.last + (long long)q.b * a.d, (uint32_t)q.at * 4, carry, q.skip);
+    if (a.last != nullptr && q.part == 0 && wave == 0) q.store_floats(a.last + (long long)q.b * a.d, carry);
 }
 
 // ---------------------------------------------------------------------------------------------------
@@ -432,24 +521,49 @@ __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
 // Channels of a lane: four bytes of them, one where there are not as many
 static int scan_channels(int type, long long d) { return type == QSR_TYPE_BF16 && d >= 2 ? 2 : 1; }
 
+// A workgroup has all steps of 64 lanes' channels, or a part of them.  Parts cost a second read of two of three to five arrays and a
+// launch; they are taken where workgroups are too few otherwise.
+// What a trip of a workgroup costs, in tenths of its time: 10 without parts and 14 with them, a part's start 3, the second launch 8; the maps of the
+// parts before, which each part joins, count too.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them, bf16,
+// forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 105 and 356 / 158; 32768 steps of 2048
+// 942 / 113.  With 128 workgroups and more forward and 192 backward the second read costs what is won (16 x 1024 steps of 1024,
+// forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs up to 512 workgroups; from there on eight
+// are faster, 76 against 80 at 64 x 1024 steps of 1024).
 struct ScanPlan { int waves, parts, part_len; long long groups; };
-static ScanPlan scan_plan(long long B, long long T, long long d, int type)
+static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool back)
 {
     ScanPlan p;
     const int V = scan_channels(type, d);
     p.groups = (d + 64 * V - 1) / (64 * V);
-    p.waves = T <= STEPS ? 1 : SCAN_WAVES;
     p.parts = 1;
-    const long long trip = (long long)p.waves * STEPS, trips = (T + trip - 1) / trip, have = B * p.groups;
-    if (have < 256 && trips >= 8) {
-        long long want = (512 + have - 1) / have;
-        if (want > trips / 4) want = trips / 4;
-        const long long each = (trips + want - 1) / want;
-        p.parts = (int)((trips + each - 1) / each);
-        p.part_len = (int)(each * trip);
-    } else p.part_len = (int)(trips * trip < T ? T : trips * trip);
+    const long long have = B * p.groups, slots = back ? 256 : 512, few = back ? 192 : 128;
+    p.waves = T <= STEPS ? 1 : !back && have >= few && have < 512 ? MANY_WAVES : WAVES;
+    const long long trip = (long long)p.waves * STEPS, trips = (T + trip - 1) / trip;
+    long long each = trips, best = 10 * trips;
+    for (long long n = 2; have < few && p.waves == WAVES && n <= trips && n <= 4 * slots / have; ++n) {
+        const long long e = (trips + n - 1) / n, rounds = (have * n + slots - 1) / slots, cost = rounds * (14 * e + 3) + n / 8 + 8;
+        if ((trips + e - 1) / e == n && cost < best) { best = cost; each = e; }
+    }
+    if (trips > 0) p.parts = (int)((trips + each - 1) / each);
+    p.part_len = (int)(each * trip);
     return p;
 }
+
+template <typename T, int V, bool COMP, bool STREAM>
+static void launch_back(const ScanArgs &a, const ScanPlan &p, dim3 grid, hipStream_t s)
+{
+    if (p.waves == 1) scan_back_kernel<T, V, 1, COMP, STREAM><<<grid, 64, 0, s>>>(a);
+    else scan_back_kernel<T, V, WAVES, COMP, STREAM><<<grid, 64 * WAVES, 0, s>>>(a);
+}
+template <typename T, int V, bool COMP, bool STREAM>
+static void launch_forward(const ScanArgs &a, const ScanPlan &p, dim3 grid, hipStream_t s)
+{
+    if (p.waves == 1) scan_kernel<T, V, 1, COMP, STREAM><<<grid, 64, 0, s>>>(a);
+    else if (p.waves == WAVES) scan_kernel<T, V, WAVES, COMP, STREAM><<<grid, 64 * WAVES, 0, s>>>(a);
+    else scan_kernel<T, V, MANY_WAVES, COMP, STREAM><<<grid, 64 * MANY_WAVES, 0, s>>>(a);
+}
+// whole lines to a wavefront's part of a row
+static bool lines(const void *p, long long seq, int step) { return (((uintptr_t)p | (uintptr_t)seq | (uintptr_t)step) & 127) == 0; }
 
 template <typename T, int V, bool COMP>
 static hipError_t launch_scan(ScanArgs &a, const ScanPlan &p, long long B, bool back, hipStream_t s)
@@ -459,10 +573,10 @@ static hipError_t launch_scan(ScanArgs &a, const ScanPlan &p, long long B, bool 
     a.part_len = p.part_len;
     if (p.parts > 1) {
         a.tiles = B * (p.parts - 1) * p.groups;
-        const TileGrid g = tile_grid(a.tiles, 64 * SCAN_WAVES);
+        const TileGrid g = tile_grid(a.tiles, 64 * WAVES);
         if (g.x == 0) return hipErrorInvalidConfiguration;
-        if (back) scan_maps_kernel<T, V, COMP, true><<<dim3(g.x, g.y), 64 * SCAN_WAVES, 0, s>>>(a);
-        else scan_maps_kernel<T, V, COMP, false><<<dim3(g.x, g.y), 64 * SCAN_WAVES, 0, s>>>(a);
+        if (back) scan_maps_kernel<T, V, COMP, true><<<dim3(g.x, g.y), 64 * WAVES, 0, s>>>(a);
+        else scan_maps_kernel<T, V, COMP, false><<<dim3(g.x, g.y), 64 * WAVES, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
@@ -470,18 +584,18 @@ static hipError_t launch_scan(ScanArgs &a, const ScanPlan &p, long long B, bool 
     const TileGrid g = tile_grid(a.tiles, 64 * p.waves);
     if (g.x == 0) return hipErrorInvalidConfiguration;
     const dim3 grid(g.x, g.y);
-    if (p.waves == 1) {
-        if (back) scan_back_kernel<T, V, 1, COMP><<<grid, 64, 0, s>>>(a);
-        else scan_kernel<T, V, 1, COMP><<<grid, 64, 0, s>>>(a);
+    if (back) {
+        if (lines(a.dx, a.b_dx, a.s_dx) && lines(a.df, a.b_df, a.s_df)) launch_back<T, V, COMP, true>(a, p, grid, s);
+        else launch_back<T, V, COMP, false>(a, p, grid, s);
     } else {
-        if (back) scan_back_kernel<T, V, SCAN_WAVES, COMP><<<grid, 64 * SCAN_WAVES, 0, s>>>(a);
-        else scan_kernel<T, V, SCAN_WAVES, COMP><<<grid, 64 * SCAN_WAVES, 0, s>>>(a);
+        if (lines(a.h, a.b_h, a.s_h)) launch_forward<T, V, COMP, true>(a, p, grid, s);
+        else launch_forward<T, V, COMP, false>(a, p, grid, s);
     }
     return hipGetLastError();
 }
 static hipError_t launch_scan(ScanArgs &a, int type, int input, long long B, bool back, hipStream_t s)
 {
-    const ScanPlan p = scan_plan(B, a.T, a.d, type);
+    const ScanPlan p = scan_plan(B, a.T, a.d, type, back);
     const bool comp = input == QSR_SCAN_COMPLEMENT;
     if (type == QSR_TYPE_F32) return comp ? launch_scan<float, 1, true>(a, p, B, back, s) : launch_scan<float, 1, false>(a, p, B, back, s);
     if (scan_channels(type, a.d) == 2) return comp ? launch_scan<bf16_t, 2, true>(a, p, B, back, s) : launch_scan<bf16_t, 2, false>(a, p, B, back, s);
@@ -508,6 +622,13 @@ static bool scan_limits_ok(int64_t B, int64_t T, int64_t d)
     return B < ((int64_t)1 << 31) && T <= ((int64_t)1 << 30) && d <= ((int64_t)1 << 28) &&
            B * ((d + 63) / 64) < ((int64_t)1 << 36);
 }
+constexpr int64_t MOST_STRIDE = 1 << 24;       // elements from step to step: a tile's rows lie within 2^31 bytes
+static bool steps_near(int64_t T, std::initializer_list<int64_t> strides)
+{
+    for (int64_t s : strides)
+        if (T > 1 && s > MOST_STRIDE) return false;
+    return true;
+}
 // Rows of d elements, `step` from step to step and `seq` from sequence to sequence.  written: no two of them share an element.
 static bool strides_ok(int64_t B, int64_t T, int64_t d, int64_t seq, int64_t step, bool written)
 {
@@ -523,8 +644,8 @@ extern "C" int qsr_gated_scan_workspace_bytes(int64_t batch, int64_t steps, int6
     if (!scan_sizes_ok(batch, steps, d, type)) return QSR_EINVAL;
     if (!scan_limits_ok(batch, steps, d)) return QSR_ELIMIT;
     if (batch == 0) return QSR_OK;
-    const ScanPlan p = scan_plan(batch, steps, d, type);
-    *bytes = p.parts > 1 ? (size_t)batch * (size_t)(p.parts + 1) * (size_t)d * sizeof(float2) : 0;
+    const int f = scan_plan(batch, steps, d, type, false).parts, b = scan_plan(batch, steps, d, type, true).parts, parts = f > b ? f : b;
+    *bytes = parts > 1 ? (size_t)batch * (size_t)(parts + 1) * (size_t)d * sizeof(float2) : 0;
     return QSR_OK;
 }
 
@@ -533,7 +654,7 @@ extern "C" int qsr_gated_scan(const qsr_gated_scan_args *q, void *workspace, siz
     if (!q || !scan_sizes_ok(q->batch, q->steps, q->d, q->type)) return QSR_EINVAL;
     if (q->input != QSR_SCAN_COMPLEMENT && q->input != QSR_SCAN_PLAIN) return QSR_EINVAL;
     if (!scan_limits_ok(q->batch, q->steps, q->d)) return QSR_ELIMIT;
-    const uintptr_t es = q->type == QSR_TYPE_F32 ? 4 : 2;
+    const int64_t es = q->type == QSR_TYPE_F32 ? 4 : 2;
     if (q->batch == 0 || (q->steps == 0 && !q->last)) return QSR_OK;
     if (off(q->initial, 4) || off(q->last, 4) || off(q->states, 4) || off(q->lengths, 8)) return QSR_EINVAL;
     if (q->steps > 0 && (!q->x || off(q->x, es) || !q->gate || off(q->gate, es) || !q->h || off(q->h, es))) return QSR_EINVAL;
@@ -541,6 +662,7 @@ extern "C" int qsr_gated_scan(const qsr_gated_scan_args *q, void *workspace, siz
         !strides_ok(q->batch, q->steps, q->d, q->gate_batch_stride, q->gate_stride, false) ||
         !strides_ok(q->batch, q->steps, q->d, q->h_batch_stride, q->h_stride, true))
         return QSR_EINVAL;
+    if (!steps_near(q->steps, {q->x_stride, q->gate_stride, q->h_stride})) return QSR_ELIMIT;
     size_t need = 0;
     const int rc = qsr_gated_scan_workspace_bytes(q->batch, q->steps, q->d, q->type, &need);
     if (rc != QSR_OK) return rc;
@@ -550,8 +672,10 @@ extern "C" int qsr_gated_scan(const qsr_gated_scan_args *q, void *workspace, siz
     a.x = q->x; a.f = q->gate; a.h = q->h;
     a.initial = q->initial; a.last = q->last; a.states = q->states;
     a.reset = q->reset; a.lengths = q->lengths; a.maps = (float2 *)workspace;
-    a.s_x = q->x_stride; a.s_f = q->gate_stride; a.s_h = q->h_stride;
-    a.b_x = q->x_batch_stride; a.b_f = q->gate_batch_stride; a.b_h = q->h_batch_stride;
+    auto step = [&](int64_t n) { return q->steps > 1 ? (int)(n * es) : 0; };               // in bytes
+    auto seq = [&](int64_t n) { return q->batch > 1 ? n * es : 0; };
+    a.s_x = step(q->x_stride); a.s_f = step(q->gate_stride); a.s_h = step(q->h_stride);
+    a.b_x = seq(q->x_batch_stride); a.b_f = seq(q->gate_batch_stride); a.b_h = seq(q->h_batch_stride);
     a.T = (int)q->steps; a.d = (int)q->d;
     return finish(launch_scan(a, q->type, q->input, q->batch, false, (hipStream_t)stream));
 }
@@ -561,7 +685,7 @@ extern "C" int qsr_gated_scan_backward(const qsr_gated_scan_backward_args *q, vo
     if (!q || !scan_sizes_ok(q->batch, q->steps, q->d, q->type)) return QSR_EINVAL;
     if (q->input != QSR_SCAN_COMPLEMENT && q->input != QSR_SCAN_PLAIN) return QSR_EINVAL;
     if (!scan_limits_ok(q->batch, q->steps, q->d)) return QSR_ELIMIT;
-    const uintptr_t es = q->type == QSR_TYPE_F32 ? 4 : 2;
+    const int64_t es = q->type == QSR_TYPE_F32 ? 4 : 2;
     if (q->batch == 0 || (q->steps == 0 && !q->initial_grad)) return QSR_OK;
     if (off(q->last_grad, 4) || off(q->initial_grad, 4) || off(q->lengths, 8)) return QSR_EINVAL;
     if (q->steps > 0 && (!q->h_grad || off(q->h_grad, es) || !q->x || off(q->x, es) || !q->gate || off(q->gate, es) || !q->states ||
@@ -573,6 +697,7 @@ extern "C" int qsr_gated_scan_backward(const qsr_gated_scan_backward_args *q, vo
         !strides_ok(q->batch, q->steps, q->d, q->x_grad_batch_stride, q->x_grad_stride, true) ||
         !strides_ok(q->batch, q->steps, q->d, q->gate_grad_batch_stride, q->gate_grad_stride, true))
         return QSR_EINVAL;
+    if (!steps_near(q->steps, {q->x_stride, q->gate_stride, q->h_grad_stride, q->x_grad_stride, q->gate_grad_stride})) return QSR_ELIMIT;
     size_t need = 0;
     const int rc = qsr_gated_scan_workspace_bytes(q->batch, q->steps, q->d, q->type, &need);
     if (rc != QSR_OK) return rc;
@@ -582,9 +707,12 @@ extern "C" int qsr_gated_scan_backward(const qsr_gated_scan_backward_args *q, vo
     a.x = q->x; a.f = q->gate; a.dh = q->h_grad; a.dx = q->x_grad; a.df = q->gate_grad;
     a.initial = q->last_grad; a.last = q->initial_grad; a.states = (float *)q->states;
     a.reset = q->reset; a.lengths = q->lengths; a.maps = (float2 *)workspace;
-    a.s_x = q->x_stride; a.s_f = q->gate_stride; a.s_dh = q->h_grad_stride; a.s_dx = q->x_grad_stride; a.s_df = q->gate_grad_stride;
-    a.b_x = q->x_batch_stride; a.b_f = q->gate_batch_stride; a.b_dh = q->h_grad_batch_stride;
-    a.b_dx = q->x_grad_batch_stride; a.b_df = q->gate_grad_batch_stride;
+    auto step = [&](int64_t n) { return q->steps > 1 ? (int)(n * es) : 0; };
+    auto seq = [&](int64_t n) { return q->batch > 1 ? n * es : 0; };
+    a.s_x = step(q->x_stride); a.s_f = step(q->gate_stride); a.s_dh = step(q->h_grad_stride);
+    a.s_dx = step(q->x_grad_stride); a.s_df = step(q->gate_grad_stride);
+    a.b_x = seq(q->x_batch_stride); a.b_f = seq(q->gate_batch_stride); a.b_dh = seq(q->h_grad_batch_stride);
+    a.b_dx = seq(q->x_grad_batch_stride); a.b_df = seq(q->gate_grad_batch_stride);
     a.T = (int)q->steps; a.d = (int)q->d;
     return finish(launch_scan(a, q->type, q->input, q->batch, true, (hipStream_t)stream));
 }

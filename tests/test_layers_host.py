@@ -124,13 +124,13 @@ def _call(a, ws=BIG):
 BOTH = [(dict(type=2), -1), (dict(input=2), -1), (dict(input=-1), -1), (dict(batch=-1), -1), (dict(steps=-1), -1), (dict(d=0), -1),
         (dict(steps=(1 << 30) + 1), -7), (dict(d=(1 << 28) + 1), -7), (dict(batch=1 << 31), -7), (dict(x=None), -1), (dict(x=P + 2), -1),
         (dict(gate=None), -1), (dict(gate=P + 1), -1), (dict(type=1, gate=P + 1), -1), (dict(lengths=P + 4), -1), (dict(states=P + 2), -1),
-        (dict(x_stride=9), -1), (dict(gate_stride=9), -1), (dict(x_batch_stride=9), -1), (dict(gate_batch_stride=9), -1),
+        (dict(x_stride=9), -1), (dict(gate_stride=9), -1), (dict(x_stride=(1 << 24) + 1), -7), (dict(gate_stride=1 << 40), -7), (dict(x_batch_stride=9), -1), (dict(gate_batch_stride=9), -1),
         (dict(batch=0, x=None), 0)]
 
 
 @pytest.mark.parametrize("over,code", BOTH + [
     (dict(h=None), -1), (dict(h=P + 2), -1), (dict(initial=P + 2), -1), (dict(last=P + 1), -1), (dict(h_stride=9), -1), (dict(h_batch_stride=199), -1),
-    (dict(h_stride=29, h_batch_stride=10), -1), (dict(steps=0, last=None, x=None, gate=None, h=None), 0),
+    (dict(h_stride=29, h_batch_stride=10), -1), (dict(h_stride=(1 << 24) + 1), -7), (dict(steps=0, last=None, x=None, gate=None, h=None), 0),
 ])
 def test_gated_scan_arguments(over, code):
     """Among them rows of h that share elements, steps before sequences and the other way round."""
@@ -140,7 +140,7 @@ def test_gated_scan_arguments(over, code):
 @pytest.mark.parametrize("over,code", BOTH + [
     (dict(h_grad=None), -1), (dict(states=None), -1), (dict(x_grad=None), -1), (dict(gate_grad=P + 2), -1), (dict(last_grad=P + 2), -1),
     (dict(initial_grad=P + 1), -1), (dict(h_grad_stride=9), -1), (dict(h_grad_batch_stride=9), -1), (dict(x_grad_batch_stride=199), -1),
-    (dict(gate_grad_stride=29, gate_grad_batch_stride=10), -1), (dict(steps=0, initial_grad=None, x=None), 0),
+    (dict(gate_grad_stride=29, gate_grad_batch_stride=10), -1), (dict(h_grad_stride=(1 << 24) + 1), -7), (dict(x_grad_stride=(1 << 24) + 1), -7), (dict(steps=0, initial_grad=None, x=None), 0),
 ])
 def test_gated_scan_backward_arguments(over, code):
     assert _call(_scan(abi.GatedScanBackwardArgs, **over)) == code
@@ -152,7 +152,7 @@ def test_gated_scan_workspace():
     call = lambda B, T, d, ty: L.qsr_gated_scan_workspace_bytes(C.c_int64(B), C.c_int64(T), C.c_int64(d), C.c_int32(ty), C.byref(n))  # noqa: E731
     assert call(1, 1, 0, 0) == -1 and n.value == 0
     assert call(1, 1, 1, 2) == -1 and call(1, (1 << 30) + 1, 1, 0) == -7
-    for B, T, d, parts in ((1, 1, 64, False), (1, 16, 64, False), (1, 300, 64, False), (1, 5000, 64, True), (1000, 5000, 64, False), (0, 5000, 64, False)):
+    for B, T, d, parts in ((1, 1, 64, False), (1, 16, 64, False), (1, 100, 64, False), (1, 5000, 64, True), (1000, 5000, 64, False), (0, 5000, 64, False)):
         assert call(B, T, d, 0) == 0 and (n.value > 0) == parts
     assert call(1, 5000, 64, 0) == 0
     need = n.value
