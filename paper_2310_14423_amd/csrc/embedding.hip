@@ -32,7 +32,7 @@ __device__ __forceinline__ Run run_of(int first, int d, int E) { const int at = 
 template <typename T, int E>
 __device__ __forceinline__ void store_run(T *p, const float (&v)[E], int skip)
 {
-    if (skip == 0) store_wide<T, E, true>(p, v);
+    if (skip == 0) store_wide<T, E, sizeof(T) * E <= 16>(p, v);           // (two accesses of a lane leave lines to be joined in the cache)
     else {
 #pragma unroll
         for (int u = 0; u < E; ++u)
@@ -64,8 +64,8 @@ __global__ __launch_bounds__(EMBED_THREADS) void embedding_kernel(LookupArgs a)
 // tokens in order
 // ---------------------------------------------------------------------------------------------------
 constexpr int DIGITS = 512;                    // at most, of a pass of the sort
-constexpr int SORT_SMALL = 4096;               // tokens of a worker that one workgroup sorts in LDS
-constexpr int SORT_THREADS = 256, SMALL_THREADS = 1024;
+constexpr int SORT_SMALL = 16384;              // tokens of a worker that one workgroup sorts in LDS
+constexpr int SORT_THREADS = 512, SMALL_THREADS = 1024;
 
 struct SortArgs {
     const int64_t *tokens;                     // first pass: these, and places as they come
@@ -74,7 +74,7 @@ struct SortArgs {
     uint32_t *keys;                            // [K][N]
     int *place;
     int *counts;                               // [K][blocks][DIGITS]
-    long long N, V, per;                       // tokens to a workgroup: a multiple of SORT_THREADS
+    long long N, V, per;                       // tokens to a workgroup: whole rounds
     int shift, bits, passes;
 };
 
@@ -88,16 +88,21 @@ __device__ __forceinline__ uint32_t sort_key(const SortArgs &a, int k, long long
 // How many lanes of the wavefront that take part and lie before this one have its digit, and how many have it in all
 __device__ __forceinline__ void same_digit(uint32_t digit, bool in, int bits, int &before, int &all)
 {
-    uint64_t mask = __ballot(in);
-    for (int b = 0; b < bits; ++b) {
-        const uint64_t one = __ballot((digit >> b) & 1);
-        mask &= (digit >> b) & 1 ? one : ~one;
-    }
-    before = __popcll(mask & ((1ull << (threadIdx.x & 63)) - 1));
-    all = __popcll(mask);
+    const uint64_t there = __ballot(in);
+    uint32_t lo = (uint32_t)there, hi = (uint32_t)(there >> 32);
+#pragma unroll
+    for (int b = 0; b < 9; ++b)
+        if (b < bits) {
+            const uint32_t own = (uint32_t)((int32_t)(digit << (31 - b)) >> 31);           // all ones where the bit is one
+            const uint64_t one = __ballot(own != 0);
+            lo &= ~(own ^ (uint32_t)one);
+            hi &= ~(own ^ (uint32_t)(one >> 32));
+        }
+    before = (int)__builtin_amdgcn_mbcnt_hi(hi, __builtin_amdgcn_mbcnt_lo(lo, 0));
+    all = __popc(lo) + __popc(hi);
 }
 
-// counts[digit], digit < DIGITS, to the sums over all digits before (THREADS * 4 >= DIGITS).  Every thread has to be here.
+// counts[digit], digit < DIGITS, to the sums over all digits before.  Every thread has to be here.
 template <int THREADS>
 __device__ __forceinline__ void sums_before(int *counts, int *waves)
 {
@@ -121,117 +126,161 @@ __device__ __forceinline__ void sums_before(int *counts, int *waves)
     __syncthreads();
 }
 
+// A wavefront's next EACH * 64 keys, of which `left` are there: each one's place among those of its digit, from `count` on, which goes on.
+// (No atomics: the keys of frequent tokens would wait for each other.)
+template <int EACH>
+__device__ __forceinline__ void rank_keys(const uint32_t (&key)[EACH], int left, int shift, int bits, int *count, int (&rank)[EACH])
+{
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) {
+        if (i * 64 >= left) break;
+        const bool in = i * 64 + lane < left;
+        const uint32_t digit = (key[i] >> shift) & ((1u << bits) - 1);
+        int before, all;
+        same_digit(digit, in, bits, before, all);
+        const int here = count[digit];
+        rank[i] = here + before;
+        __builtin_amdgcn_wave_barrier();
+        if (in && before == 0) count[digit] = here + all;
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+constexpr int SORT_EACH = 4, SORT_WAVES = SORT_THREADS / 64, SORT_ROUND = SORT_THREADS * SORT_EACH;
+
+// Each digit's number in a workgroup's tokens
 __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(SortArgs a)
 {
-    __shared__ int count[DIGITS];
-    const int k = blockIdx.y;
-    for (int i = threadIdx.x; i < DIGITS; i += SORT_THREADS) count[i] = 0;
+    __shared__ int count[SORT_WAVES][DIGITS];
+    const int k = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; ++w) count[w][tid] = 0;
     __syncthreads();
-    const long long from = blockIdx.x * a.per, end = min(a.N, from + a.per);
-    for (long long i = from + threadIdx.x; i < end; i += SORT_THREADS)
-        atomicAdd(&count[(sort_key(a, k, i) >> a.shift) & ((1u << a.bits) - 1)], 1);
+    const long long start = blockIdx.x * a.per, stop = min(a.N, start + a.per);
+    for (long long from = start + wave * (SORT_EACH * 64); from < stop; from += SORT_ROUND) {
+        const int left = (int)min(stop - from, (long long)SORT_EACH * 64);
+        uint32_t key[SORT_EACH];
+        int rank[SORT_EACH];
+#pragma unroll
+        for (int i = 0; i < SORT_EACH; ++i) key[i] = sort_key(a, k, from + min(i * 64 + lane, left - 1));
+        rank_keys<SORT_EACH>(key, left, a.shift, a.bits, count[wave], rank);
+    }
     __syncthreads();
-    for (int i = threadIdx.x; i < DIGITS; i += SORT_THREADS) a.counts[((long long)k * gridDim.x + blockIdx.x) * DIGITS + i] = count[i];
+    int sum = 0;
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; ++w) sum += count[w][tid];
+    a.counts[((long long)k * gridDim.x + blockIdx.x) * DIGITS + tid] = sum;
 }
 
-// A wavefront moves a run of its workgroup's tokens, 64 at a time, in their order
+// A workgroup moves its tokens in rounds, in which each wavefront has a run of them; DIGITS = SORT_THREADS: a thread has a digit
 __global__ __launch_bounds__(SORT_THREADS) void sort_move_kernel(SortArgs a)
 {
-    constexpr int WAVES = SORT_THREADS / 64;
-    __shared__ int start[DIGITS], mine[DIGITS], to[WAVES][DIGITS], sums[WAVES];
+    static_assert(DIGITS == SORT_THREADS, "a thread has a digit");
+    __shared__ int start[DIGITS], to[SORT_WAVES][DIGITS], sums[SORT_WAVES];
     const int k = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-    const uint32_t mask = (1u << a.bits) - 1;
-    for (int i = tid; i < DIGITS; i += SORT_THREADS) {
-#pragma unroll
-        for (int w = 0; w < WAVES; ++w) to[w][i] = 0;
-        const int *c = a.counts + (long long)k * gridDim.x * DIGITS + i;
-        int all = 0, before = 0;
-#pragma unroll 8
-        for (unsigned b = 0; b < gridDim.x; ++b) {
-            const int n = c[b * DIGITS];
-            all += n;
-            before += b < blockIdx.x ? n : 0;
-        }
-        start[i] = all;
-        mine[i] = before;
+    const long long begin = blockIdx.x * a.per, stop = min(a.N, begin + a.per);
+    const int *const c = a.counts + (long long)k * gridDim.x * DIGITS + tid;
+    int total = 0, next = 0;
+#pragma unroll 16
+    for (unsigned b = 0; b < gridDim.x; ++b) {
+        const int n = c[b * DIGITS];
+        total += n;
+        next += b < blockIdx.x ? n : 0;
     }
+    start[tid] = total;
     __syncthreads();
     sums_before<SORT_THREADS>(start, sums);
-    const long long quarter = a.per / WAVES;
-    const long long from = min(a.N, blockIdx.x * a.per + wave * quarter), end = min(a.N, from + quarter);
-    for (long long i = from + lane; i < end; i += 64) atomicAdd(&to[wave][(sort_key(a, k, i) >> a.shift) & mask], 1);
-    __syncthreads();
-    for (int i = tid; i < DIGITS; i += SORT_THREADS) {
-        int at = start[i] + mine[i];
+    next += start[tid];                        // where this digit's next one goes
+    for (long long round = begin; round < stop; round += SORT_ROUND) {
+        const long long from = round + wave * (SORT_EACH * 64);
+        const int left = (int)max(0ll, min(stop - from, (long long)SORT_EACH * 64));
+        uint32_t key[SORT_EACH];
+        int place[SORT_EACH], rank[SORT_EACH];
+        if (left > 0)
 #pragma unroll
-        for (int w = 0; w < WAVES; ++w) { const int n = to[w][i]; to[w][i] = at; at += n; }
-    }
-    __syncthreads();
-    for (long long i = from; i < end; i += 64) {
-        const bool in = i + lane < end;
-        const long long j = in ? i + lane : end - 1;
-        const uint32_t key = sort_key(a, k, j), digit = (key >> a.shift) & mask;
-        int before, all;
-        same_digit(digit, in, a.bits, before, all);
-        const int at = to[wave][digit];
-        if (in) {
-            a.keys[k * a.N + at + before] = key;
-            a.place[k * a.N + at + before] = a.tokens != nullptr ? (int)j : a.place_in[k * a.N + j];
-        }
-        __builtin_amdgcn_wave_barrier();
-        if (in && before == 0) to[wave][digit] = at + all;
-        __builtin_amdgcn_wave_barrier();
+            for (int i = 0; i < SORT_EACH; ++i) {
+                const long long j = from + min(i * 64 + lane, left - 1);
+                key[i] = sort_key(a, k, j);
+                place[i] = a.tokens != nullptr ? (int)j : a.place_in[k * a.N + j];
+            }
+#pragma unroll
+        for (int w = 0; w < SORT_WAVES; ++w) to[w][tid] = 0;
+        __syncthreads();
+        rank_keys<SORT_EACH>(key, left, a.shift, a.bits, to[wave], rank);
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < SORT_WAVES; ++w) { const int n = to[w][tid]; to[w][tid] = next; next += n; }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < SORT_EACH; ++i)
+            if (i * 64 + lane < left) {
+                const long long at = k * a.N + to[wave][(key[i] >> a.shift) & ((1u << a.bits) - 1)] + rank[i];
+                a.keys[at] = key[i];
+                a.place[at] = place[i];
+            }
+        __syncthreads();
     }
 }
 
-// Few tokens: all passes in LDS
+// Few tokens: all passes in LDS.  A pass takes a wavefront's run of the list into registers before it is written again.
+template <int MOST>
 __global__ __launch_bounds__(SMALL_THREADS) void sort_small_kernel(SortArgs a)
 {
-    constexpr int WAVES = SMALL_THREADS / 64;
-    __shared__ uint32_t keys[2][SORT_SMALL];
-    __shared__ uint16_t place[2][SORT_SMALL];
+    constexpr int WAVES = SMALL_THREADS / 64, EACH = MOST / SMALL_THREADS;
+    __shared__ uint32_t keys[MOST];
+    __shared__ uint16_t place[MOST];
     __shared__ int start[DIGITS], to[WAVES][DIGITS], sums[WAVES];
     const int k = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63, N = (int)a.N;
-    const uint32_t mask = (1u << a.bits) - 1;
-    for (int i = tid; i < N; i += SMALL_THREADS) { keys[0][i] = key_of(a.tokens[(long long)k * N + i], a.V); place[0][i] = (uint16_t)i; }
-    const int run = (N + SMALL_THREADS - 1) / SMALL_THREADS * 64, from = min(N, wave * run), end = min(N, from + run);
-    for (int pass = 0; pass < a.passes; ++pass) {
-        const int src = pass & 1, dst = src ^ 1, shift = pass * a.bits;
-        for (int i = tid; i < WAVES * DIGITS; i += SMALL_THREADS) to[i / DIGITS][i % DIGITS] = 0;
-        __syncthreads();
-        for (int i = from + lane; i < end; i += 64) atomicAdd(&to[wave][(keys[src][i] >> shift) & mask], 1);
-        __syncthreads();
-        if (tid < DIGITS) {
-            int all = 0;
+    const int run = (N + SMALL_THREADS - 1) / SMALL_THREADS * 64, from = min(N, wave * run), left = min(N - from, run);
+    uint32_t key[EACH];
+    int at[EACH], rank[EACH];
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) all += to[w][tid];
+    for (int i = 0; i < EACH; ++i) {
+        const int j = i * 64 + lane;
+        key[i] = j < left ? key_of(a.tokens[(long long)k * N + from + j], a.V) : 0;
+        at[i] = from + j;
+    }
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * a.bits;
+        for (int i = tid; i < WAVES * DIGITS; i += SMALL_THREADS) (&to[0][0])[i] = 0;
+        __syncthreads();
+        rank_keys<EACH>(key, left, shift, a.bits, to[wave], rank);
+        __syncthreads();
+        int n[WAVES], all = 0;
+        if (tid < DIGITS) {
+#pragma unroll
+            for (int w = 0; w < WAVES; ++w) { n[w] = to[w][tid]; all += n[w]; }
             start[tid] = all;
         }
         __syncthreads();
         sums_before<SMALL_THREADS>(start, sums);
         if (tid < DIGITS) {
-            int at = start[tid];
+            int here = start[tid];
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) { const int n = to[w][tid]; to[w][tid] = at; at += n; }
+            for (int w = 0; w < WAVES; ++w) { to[w][tid] = here; here += n[w]; }
         }
         __syncthreads();
-        for (int i = from; i < end; i += 64) {
-            const bool in = i + lane < end;
-            const int j = in ? i + lane : end - 1;
-            const uint32_t key = keys[src][j], digit = (key >> shift) & mask;
-            int before, all;
-            same_digit(digit, in, a.bits, before, all);
-            const int at = to[wave][digit];
-            if (in) { keys[dst][at + before] = key; place[dst][at + before] = place[src][j]; }
-            __builtin_amdgcn_wave_barrier();
-            if (in && before == 0) to[wave][digit] = at + all;
-            __builtin_amdgcn_wave_barrier();
-        }
+#pragma unroll
+        for (int i = 0; i < EACH; ++i)
+            if (i * 64 + lane < left) {
+                const int j = to[wave][(key[i] >> shift) & ((1u << a.bits) - 1)] + rank[i];
+                keys[j] = key[i];
+                place[j] = (uint16_t)at[i];
+            }
         __syncthreads();
+        if (pass + 1 < a.passes) {
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                const int j = min(from + i * 64 + lane, N - 1);
+                key[i] = keys[j];
+                at[i] = place[j];
+            }
+        }
     }
     for (int i = tid; i < N; i += SMALL_THREADS) {
-        a.keys[(long long)k * N + i] = keys[a.passes & 1][i];
-        a.place[(long long)k * N + i] = place[a.passes & 1][i];
+        a.keys[(long long)k * N + i] = keys[i];
+        a.place[(long long)k * N + i] = place[i];
     }
 }
 
@@ -246,10 +295,13 @@ struct GradArgs {
     float *parts;                              // [K][chunks][2][d]: of a chunk's first sum, which began before it, and of its last, which goes on
     long long N, V, chunks, s_dy, s_out, s_worker;
     long long chunk_groups;                    // workgroups with chunks; those behind clear rows
-    int d, lanes, chunk, clear_rows;
+    int d, lanes, chunk, clear_rows, clear_lanes;
     float scale;
     bool add;
 };
+
+// Elements of a store that clears: 16 bytes, in rows of E elements at least
+constexpr int clear_elements(int E, int size) { return E < 16 / size ? E : 16 / size; }
 
 template <typename TO, int E>
 __device__ __forceinline__ void finish_run(const GradArgs &a, int k, uint32_t v, const Run &r, const float (&sum)[E])
@@ -287,21 +339,26 @@ __global__ __launch_bounds__(EMBED_THREADS) void embedding_sums_kernel(GradArgs 
     __shared__ int splace[EMBED_THREADS / 16 * CHUNK_MOST];
     const int k = blockIdx.y, lane = threadIdx.x & (a.lanes - 1), place = threadIdx.x / a.lanes, side = EMBED_THREADS / a.lanes;
     const uint32_t *const keys = a.keys + k * a.N;
-    const int first = ((int)blockIdx.z * a.lanes + lane) * E;
-    const Run run = run_of(min(first, a.d - 1), a.d, E);
     if ((long long)blockIdx.x >= a.chunk_groups) {
+        if (blockIdx.z != 0) return;
         const long long v0 = ((long long)blockIdx.x - a.chunk_groups) * a.clear_rows, rows = min((long long)a.clear_rows, a.V - v0);
         for (int i = threadIdx.x; i < rows; i += EMBED_THREADS) {
             const long long at = first_of(keys, 0, a.N, (uint32_t)(v0 + i));
             skey[i] = at < a.N && keys[at] == (uint32_t)(v0 + i);
         }
         __syncthreads();
-        if (first >= a.d) return;
-        const float zero[E] = {};
-        for (int i = place; i < rows; i += side)
-            if (!skey[i]) store_run<TO, E>((TO *)a.out + k * a.s_worker + (v0 + i) * a.s_out + run.at, zero, run.skip);
+        // 16 bytes to a lane, as many rows side by side as the workgroup's lanes hold
+        constexpr int C = clear_elements(E, (int)sizeof(TO));
+        const float zero[C] = {};
+        for (int i = threadIdx.x / a.clear_lanes; i < rows; i += EMBED_THREADS / a.clear_lanes) {
+            if (skey[i]) continue;
+            TO *const to = (TO *)a.out + k * a.s_worker + (v0 + i) * a.s_out;
+            for (int c = (threadIdx.x & (a.clear_lanes - 1)) * C; c < a.d; c += a.clear_lanes * C) store_wide<TO, C, true>(to + min(c, a.d - C), zero);
+        }
         return;
     }
+    const int first = ((int)blockIdx.z * a.lanes + lane) * E;
+    const Run run = run_of(min(first, a.d - 1), a.d, E);
     const long long c0 = (long long)blockIdx.x * side * a.chunk;
     for (int i = threadIdx.x; i < side * a.chunk; i += EMBED_THREADS) {
         const bool in = c0 + i < a.N;
@@ -359,9 +416,22 @@ __global__ __launch_bounds__(EMBED_THREADS) void embedding_join_kernel(GradArgs 
     const uint32_t *const keys = a.keys + k * a.N;
     const long long chunk = blockIdx.x, from = chunk * a.chunk, end = from + a.chunk;
     if (end >= a.N) return;
-    const uint32_t v = keys[end - 1];
-    if (v == (uint32_t)a.V || keys[end] != v || (keys[from] == v && from > 0 && keys[from - 1] == v)) return;
-    const long long last = (first_of(keys, end, a.N, v + 1) - 1) / a.chunk;        // chunk + 1 .. last: first sums of theirs
+    // all of these at once: most chunks have nothing here, and then it is their latency that counts.  Chunk + 1 + i has no other token
+    // if its last is v, since the list is in order; the last chunk of the sum is the one behind those.
+    const uint32_t before = keys[max(from, 1ll) - 1], start = keys[from], v = keys[end - 1], next = keys[end];
+    auto whole = [&](long long i) { const long long e = end + (i + lane + 1) * a.chunk; return e <= a.N && keys[min(e, a.N) - 1] == v; };
+    bool mine = whole(0);
+    if (v == (uint32_t)a.V || next != v || (start == v && from > 0 && before == v)) return;
+    long long count = 0;
+    for (;;) {
+        const uint64_t others = ~__ballot(mine);
+        if (others != 0) { count += __ffsll((unsigned long long)others) - 1; break; }
+        count += 64;
+        mine = whole(count);
+    }
+    // behind `count` whole chunks one more has a part, unless it begins with another token or is not there
+    const long long behind = end + count * a.chunk;
+    const long long last = chunk + count + (behind < a.N && keys[behind] == v ? 1 : 0);       // chunk + 1 .. last: first sums of theirs
     const int first = ((int)blockIdx.z * 64 + lane) * E;
     const Run run = run_of(min(first, a.d - 1), a.d, E);
     const float *const parts = a.parts + (k * a.chunks + chunk) * 2 * a.d + run.at;
@@ -390,6 +460,144 @@ __global__ __launch_bounds__(EMBED_THREADS) void embedding_join_kernel(GradArgs 
 }
 
 // ---------------------------------------------------------------------------------------------------
+// few tokens: all of it in one launch
+// ---------------------------------------------------------------------------------------------------
+constexpr int DIRECT_TOKENS = 2048, DIRECT_ROWS = 64;      // of a worker; of the table, to a workgroup
+
+struct DirectArgs {
+    const void *dy;
+    const int64_t *tokens;
+    void *out;
+    long long V, s_dy, s_out, s_worker;
+    int N, d, lanes, rows;                     // rows of the table to a workgroup
+    float scale;
+    bool add;
+};
+
+// A workgroup has some rows of the table and L * E columns.  It goes through all tokens of the worker, each wavefront through a run of
+// them, sorts those that are its own in LDS, gives each group of lanes the same number of them, and joins the sums that several groups have a part in.
+template <typename TI, typename TO, int E>
+__global__ __launch_bounds__(EMBED_THREADS) void embedding_direct_kernel(DirectArgs a)
+{
+    constexpr int WAVES = EMBED_THREADS / 64, RUN = DIRECT_TOKENS / WAVES;
+    __shared__ uint32_t found[WAVES][RUN], list[DIRECT_TOKENS];            // a row's number among the workgroup's, and a place
+    __shared__ int to[WAVES][DIRECT_ROWS], start[DIRECT_ROWS + 1];
+    __shared__ float parts[EMBED_THREADS * E];
+    const int k = blockIdx.y, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const long long v0 = (long long)blockIdx.x * a.rows;
+    const int rows = (int)min((long long)a.rows, a.V - v0);
+    to[wave][lane] = 0;
+    const int run = (a.N + EMBED_THREADS - 1) / EMBED_THREADS * 64, from = min(a.N, wave * run), end = min(a.N, from + run);
+    int mine = 0;
+    for (int i = from; i < end; i += 64) {
+        const int j = i + lane;
+        const long long row = (j < end ? a.tokens[(long long)k * a.N + j] : -1) - v0;
+        const bool in = j < end && row >= 0 && row < rows;
+        const uint64_t mask = __ballot(in);
+        if (in) {
+            found[wave][mine + __popcll(mask & ((1ull << lane) - 1))] = (uint32_t)row << 16 | (uint32_t)j;
+            atomicAdd(&to[wave][row], 1);
+        }
+        mine += __popcll(mask);
+    }
+    __syncthreads();
+    if (wave == 0) {                           // DIRECT_ROWS = 64: a lane to a row
+        int n[WAVES], all = 0;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) { n[w] = to[w][lane]; all += n[w]; }
+        int upto = all;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) { const int v = __shfl_up(upto, o, 64); upto += lane >= o ? v : 0; }
+        int at = upto - all;
+        start[lane] = at;
+        if (lane == 63) start[64] = upto;
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) { to[w][lane] = at; at += n[w]; }
+    }
+    __syncthreads();
+    for (int i = 0; i < mine; i += 64) {
+        const bool in = i + lane < mine;
+        const uint32_t entry = found[wave][min(i + lane, mine - 1)], row = entry >> 16;
+        int before, all;
+        same_digit(row, in, 6, before, all);
+        const int at = to[wave][row];
+        if (in) list[at + before] = entry;
+        __builtin_amdgcn_wave_barrier();
+        if (in && before == 0) to[wave][row] = at + all;
+        __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    const int groups = EMBED_THREADS / a.lanes, group = tid / a.lanes, place = tid & (a.lanes - 1), M = start[64], each = (M + groups - 1) / groups;
+    const int first = ((int)blockIdx.z * a.lanes + place) * E;
+    const Run r = run_of(min(first, a.d - 1), a.d, E);
+    const bool in = first < a.d;
+    auto write = [&](int row, const float (&sum)[E]) {
+        TO *const p = (TO *)a.out + k * a.s_worker + (v0 + row) * a.s_out + r.at;
+        float x[E];
+#pragma unroll
+        for (int u = 0; u < E; ++u) x[u] = a.scale * sum[u];
+        if (a.add) {
+            float old[E];
+            load_wide<TO, E, false>(p, old);
+#pragma unroll
+            for (int u = 0; u < E; ++u) x[u] += old[u];
+        }
+        store_run<TO, E>(p, x, r.skip);
+    };
+    const int c0 = min(M, group * each), c1 = min(M, c0 + each);
+    float sum[E] = {};
+    int cur = -1;
+    bool begun = false, on = false;
+    float *const own = parts + tid * E;        // of the first sum, where it began before
+    if (in && c0 < c1) {
+        const TI *const dy = (const TI *)a.dy + (long long)k * a.N * a.s_dy + r.at;
+        cur = (int)(list[c0] >> 16);
+        begun = c0 > 0 && (int)(list[c0 - 1] >> 16) == cur;
+        for (int i = c0; i < c1; i += 8) {
+            typename Wide<TI, E>::vec v[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u)
+                v[u] = __builtin_nontemporal_load((const typename Wide<TI, E>::vec *)(dy + (long long)(list[min(i + u, c1 - 1)] & 0xffff) * a.s_dy));
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                if (i + u >= c1) break;
+                const int row = (int)(list[i + u] >> 16);
+                if (row != cur) {
+                    if (begun) {
+#pragma unroll
+                        for (int e = 0; e < E; ++e) own[e] = sum[e];
+                    } else write(cur, sum);
+                    begun = false;
+                    cur = row;
+#pragma unroll
+                    for (int e = 0; e < E; ++e) sum[e] = 0.f;
+                }
+#pragma unroll
+                for (int e = 0; e < E; ++e) sum[e] += (float)v[u][e];
+            }
+        }
+        on = !begun && c1 < M && (int)(list[c1] >> 16) == cur;
+        if (begun) {
+#pragma unroll
+            for (int e = 0; e < E; ++e) own[e] = sum[e];
+        } else if (!on) write(cur, sum);
+    }
+    __syncthreads();
+    if (!in) return;
+    if (on) {                                  // the row's other parts, in their order
+        const int last = (start[cur + 1] - 1) / each;
+        for (int g = group + 1; g <= last; ++g)
+#pragma unroll
+            for (int e = 0; e < E; ++e) sum[e] += parts[(g * a.lanes + place) * E + e];
+        write(cur, sum);
+    }
+    if (a.add) return;
+    const float zero[E] = {};
+    for (int row = group; row < rows; row += groups)
+        if (start[row] == start[row + 1]) store_run<TO, E>((TO *)a.out + k * a.s_worker + (v0 + row) * a.s_out + r.at, zero, r.skip);
+}
+
+// ---------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------
 constexpr long long EMBED_MOST = 1ll << 27;    // tokens of a worker
@@ -400,6 +608,20 @@ static int lanes_for(long long d, int E)
     int L = 16;
     while (L < EMBED_THREADS && L < runs) L <<= 1;
     return L;
+}
+
+// Rows of the table to a workgroup that goes through all tokens: as many as make some thousand workgroups
+static int direct_rows(long long K, long long V)
+{
+    const long long rows = (K * V + 1023) / 1024;
+    return (int)(rows > DIRECT_ROWS ? DIRECT_ROWS : rows);
+}
+// Few tokens with little in their rows, and not too many workgroups that read all of the tokens: one launch
+static bool direct(long long K, long long N, long long V, long long d, int size)
+{
+    if (N < 1 || N > DIRECT_TOKENS || N * d * size > (2 << 20)) return false;
+    const long long rows = direct_rows(K, V);
+    return K * ((V + rows - 1) / rows) * N * 8 <= (1 << 27);
 }
 
 // How the tokens of K workers are sorted and summed, and where what lies in the workspace
@@ -415,7 +637,7 @@ static GradPlan grad_plan(int K, long long N, long long V, long long d, int E)
     while (bits < 32 && ((uint64_t)V >> bits) != 0) ++bits;                // V itself is a key
     p.passes = (bits + 8) / 9;
     p.bits = (bits + p.passes - 1) / p.passes;
-    p.per = 1024;
+    p.per = SORT_ROUND;
     while ((N + p.per - 1) / p.per > 128) p.per *= 2;
     p.blocks = N <= SORT_SMALL ? 0 : (N + p.per - 1) / p.per;
     p.lanes = lanes_for(d, E);
@@ -439,9 +661,10 @@ static hipError_t launch_sums(GradArgs &a, const GradPlan &p, int K, hipStream_t
 {
     const int side = EMBED_THREADS / p.lanes;
     a.chunk_groups = (p.chunks + side - 1) / side;
-    // some 64 KiB to a workgroup that clears, and a row to each of its threads at most
-    const long long row = (long long)a.d * (long long)sizeof(TO), rows = (65536 + row - 1) / row;
+    // some 128 KiB to a workgroup that clears, and a row to each of its threads at most
+    const long long row = (long long)a.d * (long long)sizeof(TO), rows = (131072 + row - 1) / row;
     a.clear_rows = (int)(rows < EMBED_THREADS ? rows : EMBED_THREADS);
+    a.clear_lanes = lanes_for(a.d, clear_elements(E, (int)sizeof(TO)));
     const long long clears = a.add ? 0 : (a.V + a.clear_rows - 1) / a.clear_rows;
     if (a.chunk_groups + clears > 0)
         embedding_sums_kernel<TI, TO, E><<<dim3((unsigned)(a.chunk_groups + clears), (unsigned)K, (unsigned)p.slices), EMBED_THREADS, 0, s>>>(a);
@@ -449,6 +672,14 @@ static hipError_t launch_sums(GradArgs &a, const GradPlan &p, int K, hipStream_t
     if (e != hipSuccess || p.chunks < 2) return e;
     constexpr int J = E < 4 ? 1 : 4;
     embedding_join_kernel<TO, J><<<dim3((unsigned)(p.chunks - 1), (unsigned)K, (unsigned)((a.d + 64 * J - 1) / (64 * J))), EMBED_THREADS, 0, s>>>(a);
+    return hipGetLastError();
+}
+
+template <typename TI, typename TO, int E>
+static hipError_t launch_direct(const DirectArgs &a, int K, hipStream_t s)
+{
+    const dim3 grid((unsigned)((a.V + a.rows - 1) / a.rows), (unsigned)K, (unsigned)((a.d + (long long)a.lanes * E - 1) / ((long long)a.lanes * E)));
+    embedding_direct_kernel<TI, TO, E><<<grid, EMBED_THREADS, 0, s>>>(a);
     return hipGetLastError();
 }
 
@@ -509,7 +740,7 @@ extern "C" int qsr_embedding_workspace_bytes(int32_t K, int64_t tokens_each, int
     *bytes = 0;
     if (!sizes_ok(K, tokens_each, vocab, d) || !is_type(type)) return QSR_EINVAL;
     if (tokens_each > EMBED_MOST) return QSR_ELIMIT;
-    *bytes = grad_plan(K, tokens_each, vocab, d, run_elements(type, d)).bytes;
+    if (!direct(K, tokens_each, vocab, d, (int)size_of(type))) *bytes = grad_plan(K, tokens_each, vocab, d, run_elements(type, d)).bytes;
     return QSR_OK;
 }
 
@@ -529,6 +760,15 @@ extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void
     const hipStream_t s = (hipStream_t)stream;
     const int K = q->K, E = run_elements(q->type, q->d);
     const long long N = q->tokens_each;
+    const bool wide = q->grad_type == QSR_TYPE_F32;
+#define EMBED_BY_TYPE(F) (q->type == QSR_TYPE_F32 ? (wide ? F(float, float) : F(float, bf16_t)) : (wide ? F(bf16_t, float) : F(bf16_t, bf16_t)))
+    if (direct(K, N, q->vocab, q->d, (int)size_of(q->type))) {
+        const DirectArgs a{q->y_grad, q->tokens, q->grad, q->vocab, q->y_grad_stride, q->grad_stride, q->worker_stride, (int)N, (int)q->d,
+                           lanes_for(q->d, E), direct_rows(K, q->vocab), (float)q->scale, q->accumulate != 0};
+#define EMBED_DIRECT(TI, TO) (E == 1 ? launch_direct<TI, TO, 1>(a, K, s) : launch_direct<TI, TO, wide_of<TI>()>(a, K, s))
+        return finish(EMBED_BY_TYPE(EMBED_DIRECT));
+#undef EMBED_DIRECT
+    }
     const GradPlan p = grad_plan(K, N, q->vocab, q->d, E);
     char *const ws = (char *)workspace;
     int done = 0;                              // which of the two lists holds the result
@@ -537,7 +777,8 @@ extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void
                    p.bits, p.passes};
         hipError_t e = hipSuccess;
         if (p.blocks == 0) {
-            sort_small_kernel<<<dim3((unsigned)K), SMALL_THREADS, 0, s>>>(a);
+            if (N <= SORT_SMALL / 4) sort_small_kernel<SORT_SMALL / 4><<<dim3((unsigned)K), SMALL_THREADS, 0, s>>>(a);
+            else sort_small_kernel<SORT_SMALL><<<dim3((unsigned)K), SMALL_THREADS, 0, s>>>(a);
             e = hipGetLastError();
         }
         for (int pass = 0; p.blocks > 0 && pass < p.passes && e == hipSuccess; ++pass) {
@@ -555,10 +796,9 @@ extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void
         if (e != hipSuccess) return finish(e);
     }
     GradArgs a{q->y_grad, (const uint32_t *)(ws + p.keys[done]), (const int *)(ws + p.place[done]), q->grad, (float *)(ws + p.parts), N, q->vocab, p.chunks,
-               q->y_grad_stride, q->grad_stride, q->worker_stride, 0, (int)q->d, p.lanes, p.chunk, 0, (float)q->scale, q->accumulate != 0};
+               q->y_grad_stride, q->grad_stride, q->worker_stride, 0, (int)q->d, p.lanes, p.chunk, 0, 0, (float)q->scale, q->accumulate != 0};
 #define EMBED_SUMS(TI, TO) (E == 1 ? launch_sums<TI, TO, 1>(a, p, K, s) : launch_sums<TI, TO, wide_of<TI>()>(a, p, K, s))
-    const bool wide = q->grad_type == QSR_TYPE_F32;
-    return finish(q->type == QSR_TYPE_F32 ? (wide ? EMBED_SUMS(float, float) : EMBED_SUMS(float, bf16_t))
-                                          : (wide ? EMBED_SUMS(bf16_t, float) : EMBED_SUMS(bf16_t, bf16_t)));
+    return finish(EMBED_BY_TYPE(EMBED_SUMS));
 #undef EMBED_SUMS
+#undef EMBED_BY_TYPE
 }

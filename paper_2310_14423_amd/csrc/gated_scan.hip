@@ -38,6 +38,7 @@ struct ScanArgs {
     int s_x, s_f, s_dh, s_h, s_dx, s_df;       // and from step to step, in bytes
     long long tiles;
     int T, d, groups, parts, part_len;
+    bool near;                                 // neighbouring channels on one die
 };
 
 // exp(-x) for 0 <= x.  What the argument to the base 2 loses to rounding is put back, since a state remembers thousands of steps' gates: a
@@ -131,7 +132,11 @@ template <typename T, int V> struct Place {
     bool halves;                               // some lane of the wavefront has that
     __device__ __forceinline__ bool find(const ScanArgs &a, int lane, int parts)
     {
-        const long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+        long long id = blockIdx.x + (long long)blockIdx.y * gridDim.x;
+        if (a.near) {                          // workgroups go to the eight dies in turn
+            const long long each = (a.tiles + 7) / 8, nth = id / 8;
+            id = nth < each ? id % 8 * each + nth : a.tiles;
+        }
         if (id >= a.tiles) return false;
         const long long seq = id / a.groups;
         const int first = ((int)(id - seq * a.groups) * 64 + lane) * V;
@@ -562,7 +567,11 @@ static void launch_forward(const ScanArgs &a, const ScanPlan &p, dim3 grid, hipS
     else if (p.waves == WAVES) scan_kernel<T, V, WAVES, COMP, STREAM><<<grid, 64 * WAVES, 0, s>>>(a);
     else scan_kernel<T, V, MANY_WAVES, COMP, STREAM><<<grid, 64 * MANY_WAVES, 0, s>>>(a);
 }
-// whole lines to a wavefront's part of a row
+// Whole lines to a wavefront's part of a row.  Then what is written streams past the caches.  Otherwise neighbouring parts share lines, which
+// are read and written as a whole where both parts are on one die, in its cache; there, what is written does not stream, but for
+// forward passes with lengths.  us with / without neighbours on one die, forward and backward: fp32, 2 x 4000 steps of 3001 100 / 116 and
+// 144 / 170, 13 x 1001 of 1003 39 / 48 and 62 / 77, with lengths 40 / 43 and 54 / 68; 64 x 1024 of 1024 in bf16, whole lines, 79 / 76 and
+// 163 / 152.  Streamed / not: whole lines as the last 76 / 90 and 151 / 156; the fp32 ones 41 / 39 and 70 / 62, with lengths 30 / 40 and 58 / 54.
 static bool lines(const void *p, long long seq, int step) { return (((uintptr_t)p | (uintptr_t)seq | (uintptr_t)step) & 127) == 0; }
 
 template <typename T, int V, bool COMP>
@@ -573,22 +582,26 @@ static hipError_t launch_scan(ScanArgs &a, const ScanPlan &p, long long B, bool 
     a.part_len = p.part_len;
     if (p.parts > 1) {
         a.tiles = B * (p.parts - 1) * p.groups;
-        const TileGrid g = tile_grid(a.tiles, 64 * WAVES);
+        a.near = !(lines(a.f, a.b_f, a.s_f) && (back ? lines(a.dh, a.b_dh, a.s_dh) : lines(a.x, a.b_x, a.s_x)));
+        const TileGrid g = tile_grid((a.tiles + 7) / 8 * 8, 64 * WAVES);
         if (g.x == 0) return hipErrorInvalidConfiguration;
         if (back) scan_maps_kernel<T, V, COMP, true><<<dim3(g.x, g.y), 64 * WAVES, 0, s>>>(a);
         else scan_maps_kernel<T, V, COMP, false><<<dim3(g.x, g.y), 64 * WAVES, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
     }
+    const bool in = lines(a.f, a.b_f, a.s_f) && lines(a.x, a.b_x, a.s_x) && (!back || lines(a.dh, a.b_dh, a.s_dh));
+    const bool out = back ? lines(a.dx, a.b_dx, a.s_dx) && lines(a.df, a.b_df, a.s_df) : lines(a.h, a.b_h, a.s_h);
+    a.near = !(in && out);
     a.tiles = B * p.parts * p.groups;
-    const TileGrid g = tile_grid(a.tiles, 64 * p.waves);
+    const TileGrid g = tile_grid((a.tiles + 7) / 8 * 8, 64 * p.waves);
     if (g.x == 0) return hipErrorInvalidConfiguration;
     const dim3 grid(g.x, g.y);
     if (back) {
-        if (lines(a.dx, a.b_dx, a.s_dx) && lines(a.df, a.b_df, a.s_df)) launch_back<T, V, COMP, true>(a, p, grid, s);
+        if (out) launch_back<T, V, COMP, true>(a, p, grid, s);
         else launch_back<T, V, COMP, false>(a, p, grid, s);
     } else {
-        if (lines(a.h, a.b_h, a.s_h)) launch_forward<T, V, COMP, true>(a, p, grid, s);
+        if (out || a.lengths != nullptr) launch_forward<T, V, COMP, true>(a, p, grid, s);
         else launch_forward<T, V, COMP, false>(a, p, grid, s);
     }
     return hipGetLastError();

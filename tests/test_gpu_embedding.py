@@ -54,7 +54,8 @@ def _want(dy, tok, V, scale, old=None):
 
 
 SIZES = [(1, 1, 1, 1), (1, 4, 9, 7), (2, 5, 3, 8), (1, 100, 40, 9), (3, 65, 513, 64), (1, 1000, 512, 130), (2, 1025, 17, 300), (1, 4096, 700, 24),
-         (1, 4097, 700, 24), (2, 9000, 3000, 36), (1, 300, 70000, 12), (1, 5000, 300000, 5), (1, 600, 20, 2100), (1, 40, 11, 9001)]
+         (1, 4097, 700, 24), (2, 9000, 3000, 36), (1, 300, 70000, 12), (1, 5000, 300000, 5), (1, 600, 20, 2100), (1, 40, 11, 9001),
+         (2, 2048, 130, 40), (1, 2049, 1000, 16), (1, 1500, 65, 1100), (1, 16384, 40, 9), (2, 17000, 500, 12), (8, 2000, 60000, 4)]
 
 
 @pytest.mark.parametrize("table", ["f32", "bf16"])
