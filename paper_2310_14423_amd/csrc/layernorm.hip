@@ -15,6 +15,8 @@
 
 namespace qsr {
 
+template <typename T, int NV, int W = 0> __device__ __forceinline__ float at(const RowPart<T, NV> &r, int c, int u) { return c < NV ? r.v[c][u] : r.t; }
+
 struct LayerArgs {
     const void *x, *res;
     const float *w, *b;
@@ -28,14 +30,14 @@ struct LayerArgs {
 
 // `turn` counts the sums over a group of wavefronts, which take turns at their words
 template <typename T, int L, int W, int NV, bool FP8>
-__device__ __forceinline__ void layernorm_row(const LayerArgs &a, int k, long long row, int lane, float (*red)[W], int &turn)
+__device__ __forceinline__ void layernorm_row(const LayerArgs &a, const RowPart<T, NV> &w, const RowPart<T, NV> &b, long long row, int lane,
+                                              float (*red)[W], int &turn)
 {
     constexpr int E = wide_of<T>();
     Row<T, NV> x, res;
-    RowPart<T, NV> s, w;
+    RowPart<T, NV> s;
     load_row<T, L, W, NV, true>((const T *)a.x + row * a.s_x, lane, a.d, x);
     if (a.res != nullptr) load_row<T, L, W, NV, true>((const T *)a.res + row * a.s_res, lane, a.d, res);
-    load_words<T, L, W, NV>(a.w + k * a.s_w, lane, a.d, w);
     each<T, NV>([](float &y, float v) { y = v; }, s, x);
     if (a.res != nullptr) each<T, NV>([](float &y, float v) { y += v; }, s, res);
     const int runs = a.d / E, rest = a.d - runs * E;
@@ -62,11 +64,7 @@ __device__ __forceinline__ void layernorm_row(const LayerArgs &a, int k, long lo
     const float rstd = var == 0.f ? 0.f : 1.f / sqrtf(var);                // equal numbers without eps: the bias, and no gradient
     if (lane == 0 && a.mean != nullptr) a.mean[row] = mean;
     if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
-    each<T, NV>([&](float &y, float &f) { y = y * rstd * f; }, s, w);
-    if (a.b != nullptr) {
-        load_words<T, L, W, NV>(a.b + k * a.s_b, lane, a.d, w);
-        each<T, NV>([](float &y, float &f) { y += f; }, s, w);
-    }
+    each<T, NV>([&](float &y, float f, float g) { y = fmaf(y * rstd, f, g); }, s, w, b);
     if (!FP8) {
         store_row<T, L, W, NV, false>((T *)a.y + row * a.s_y, lane, a.d, s);
         return;
@@ -90,8 +88,12 @@ __global__ __launch_bounds__(rms_threads<W>()) void layernorm_kernel(LayerArgs a
     constexpr int side = rms_side<L, W>();
     const int k = blockIdx.y, lane = rms_lane<L, W>(), place = rms_place<L, W>();
     int turn = 0;
+    RowPart<T, NV> w, b;
+    load_words<T, L, W, NV>(a.w + k * a.s_w, lane, a.d, w);
+    if (a.b != nullptr) load_words<T, L, W, NV>(a.b + k * a.s_b, lane, a.d, b);
+    else each<T, NV>([](float &x) { x = 0.f; }, b);
     for (long long r = (long long)blockIdx.x * side + place; r < a.rows; r += (long long)gridDim.x * side)
-        layernorm_row<T, L, W, NV, FP8>(a, k, k * a.rows + r, lane, red, turn);
+        layernorm_row<T, L, W, NV, FP8>(a, w, b, k * a.rows + r, lane, red, turn);
 }
 
 struct LayerBackArgs {
@@ -123,12 +125,15 @@ __device__ __forceinline__ void group_sums(float &p, float &q, float (*red)[2][W
 }
 
 // A workgroup takes every gridDim.x-th row (W == 1: four of them at a time) and keeps its parts of the gradients of weight and bias in
-// registers.  The next row's loads are under way while a row is worked on where that takes few registers.
+// registers.  There are two wavefronts to a SIMD at most (four in the widest rows), so that each may have half of its registers: with a quarter
+// the sixteen elements of bf16 rows go to memory and back, 8 x 12608 rows of 768 130 us instead of 116, 8192 rows of 4096 74 instead of
+// 56.  The next row's loads are under way while a row is worked on where that takes few registers, and where a workgroup of eight
+// wavefronts is alone on its compute unit (4096 rows of 8192 54 us, 60 without).
 template <typename T, int L, int W, int NV, bool BIAS>
-__global__ __launch_bounds__(rms_threads<W>(), 4) void layernorm_back_kernel(LayerBackArgs a)
+__global__ __launch_bounds__(rms_threads<W>(), W == 16 ? 4 : 2) void layernorm_back_kernel(LayerBackArgs a)
 {
     constexpr int E = wide_of<T>();
-    constexpr bool AHEAD = NV * (3 * E + 3 * 2 * 4) <= 48;
+    constexpr bool AHEAD = NV * (3 * E + 3 * 2 * 4) <= 48 || (W == 8 && E == 8);
     __shared__ float red[2][2][W];
     __shared__ float side_sum[W == 1 ? 3 * L * (NV * E + 1) : 1];
     constexpr int side = rms_side<L, W>();
@@ -241,7 +246,11 @@ __global__ __launch_bounds__(SUM_THREADS) void layernorm_sums_kernel(const float
 template <typename T>
 static hipError_t launch_layer(const LayerArgs &a, int K, bool fp8, hipStream_t s)
 {
-#define LAYER_FWD(T, L, W, NV) do { const dim3 grid((unsigned)fwd_groups(a.rows, rms_side<L, W>()), (unsigned)K); \
+    // a trip for each workgroup, but for the widest rows, whose weight and bias are as much as a row: two workgroups to a compute unit (2048
+    // rows of 16384 54 us, 59 with a trip each; narrower ones are 1 to 3 % faster with a trip each)
+    const long long wide = (512 + K - 1) / K;
+#define LAYER_FWD(T, L, W, NV) do { const long long trips = fwd_groups(a.rows, rms_side<L, W>()); \
+    const dim3 grid((unsigned)(W == 16 && trips > wide ? wide : trips), (unsigned)K); \
     if (fp8) layernorm_kernel<T, L, W, NV, true><<<grid, rms_threads<W>(), 0, s>>>(a); \
     else layernorm_kernel<T, L, W, NV, false><<<grid, rms_threads<W>(), 0, s>>>(a); } while (0)
     RMS_BY_WIDTH(T, a.d, LAYER_FWD);
