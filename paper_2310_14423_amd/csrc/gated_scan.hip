@@ -297,6 +297,35 @@ __global__ __launch_bounds__(64 * W, 4) void scan_kernel(ScanArgs a)
     if (a.last != nullptr && q.part == a.parts - 1 && wave == 0) q.store_floats(a.last + (long long)q.b * a.d, carry);
 }
 
+// One step of every sequence: a thread has V channels of one
+template <typename T, int V, bool COMP>
+__global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
+{
+    const long long id = (blockIdx.x + (long long)blockIdx.y * gridDim.x) * 256 + threadIdx.x, each = (a.d + V - 1) / V;
+    if (id >= a.tiles) return;
+    const long long b = id / each;
+    const int first = (int)(id - b * each) * V, at = min(first, a.d - V), skip = first - at;
+    typedef typename Wide<T, V>::vec Vec;
+    const Vec x = *(const Vec *)((const char *)a.x + b * a.b_x + at * (long long)sizeof(T));
+    const Vec f = *(const Vec *)((const char *)a.f + b * a.b_f + at * (long long)sizeof(T));
+    float h[V], y[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) h[u] = a.initial != nullptr ? a.initial[b * a.d + at + u] : 0.f;
+    const bool live = a.lengths == nullptr || a.lengths[b] > 0, cut = a.reset != nullptr && a.reset[b] != 0;
+    T *const to = (T *)((char *)a.h + b * a.b_h) + at;
+#pragma unroll
+    for (int u = 0; u < V; ++u) {
+        if (u < skip) continue;
+        if (a.states != nullptr) a.states[b * a.d + at + u] = h[u];
+        float ga, gc;
+        gates_of<T>((float)f[u], ga, gc);
+        const float v = (float)x[u];
+        y[u] = fmaf(ga, cut ? 0.f : h[u], COMP ? gc * v : v);
+        to[u] = (T)(live ? y[u] : 0.f);
+        if (a.last != nullptr) a.last[b * a.d + at + u] = live ? y[u] : h[u];
+    }
+}
+
 // The maps of parts: a wavefront goes through a run of its part's steps, from its end.  Forward: all parts but the last, and the initial
 // state.  Backward: e before a part from e behind it, all parts but the first.
 template <typename T, int V, bool COMP, bool BACK>
@@ -577,6 +606,13 @@ static bool lines(const void *p, long long seq, int step) { return (((uintptr_t)
 template <typename T, int V, bool COMP>
 static hipError_t launch_scan(ScanArgs &a, const ScanPlan &p, long long B, bool back, hipStream_t s)
 {
+    if (a.T == 1 && !back) {
+        a.tiles = B * ((a.d + V - 1) / V);
+        const TileGrid g = tile_grid((a.tiles + 255) / 256, 256);
+        if (g.x == 0) return hipErrorInvalidConfiguration;
+        scan_step_kernel<T, V, COMP><<<dim3(g.x, g.y), 256, 0, s>>>(a);
+        return hipGetLastError();
+    }
     a.groups = (int)p.groups;
     a.parts = p.parts;
     a.part_len = p.part_len;

@@ -123,7 +123,9 @@ def layernorm(x, weight, bias=None, residual=None, eps=1e-5, out="same", sum_out
         _setup()
     _need(out == "same" or out == "fp8", "out: 'same' or 'fp8'")
     s, place = _place(x, stream)
-    with place or _nothing:
+    if place is None:
+        return _calls.layernorm(x, weight, bias, residual, eps, out == "fp8", sum_out, s)
+    with place:
         return _calls.layernorm(x, weight, bias, residual, eps, out == "fp8", sum_out, s)
 
 
@@ -133,7 +135,9 @@ def layernorm_backward(y_grad, sum, weight, mean, rstd, residual_grad=None, bias
     if _calls is None:
         _setup()
     s, place = _place(sum, stream)
-    with place or _nothing:
+    if place is None:
+        return _calls.layernorm_backward(y_grad, sum, weight, mean, rstd, residual_grad, bool(bias), s)
+    with place:
         return _calls.layernorm_backward(y_grad, sum, weight, mean, rstd, residual_grad, bool(bias), s)
 
 
@@ -151,7 +155,9 @@ def embedding(tokens, table, scale=1.0, out="same", stream=None):
         _setup()
     _need(out in _TYPES, "out: 'same', 'f32' or 'bf16'")
     s, place = _place(table, stream)
-    with place or _nothing:
+    if place is None:
+        return _calls.embedding(tokens, table, scale, _TYPES[out], s)
+    with place:
         return _calls.embedding(tokens, table, scale, _TYPES[out], s)
 
 
@@ -163,7 +169,9 @@ def embedding_backward(y_grad, tokens, table, scale=1.0, out=None, accumulate=Fa
     if _calls is None:
         _setup()
     s, place = _place(table, stream)
-    with place or _nothing:
+    if place is None:
+        return _calls.embedding_backward(y_grad, tokens, table, scale, out, bool(accumulate), s)
+    with place:
         return _calls.embedding_backward(y_grad, tokens, table, scale, out, bool(accumulate), s)
 
 
@@ -189,7 +197,9 @@ def gated_scan(x, gate, initial=None, reset=None, lengths=None, input="complemen
         _setup()
     _need(input in _INPUTS, "input: 'complement' or 'plain'")
     s, place = _place(x, stream)
-    with place or _nothing:
+    if place is None:
+        return _calls.gated_scan(x, gate, initial, reset, lengths, _INPUTS[input], bool(keep), state_out, s)
+    with place:
         return _calls.gated_scan(x, gate, initial, reset, lengths, _INPUTS[input], bool(keep), state_out, s)
 
 
@@ -200,7 +210,9 @@ def gated_scan_backward(h_grad, x, gate, states, reset=None, lengths=None, last_
         _setup()
     _need(input in _INPUTS, "input: 'complement' or 'plain'")
     s, place = _place(x, stream)
-    with place or _nothing:
+    if place is None:
+        return _calls.gated_scan_backward(h_grad, x, gate, states, reset, lengths, last_grad, _INPUTS[input], s)
+    with place:
         return _calls.gated_scan_backward(h_grad, x, gate, states, reset, lengths, last_grad, _INPUTS[input], s)
 
 
