@@ -41,38 +41,32 @@ struct ScanArgs {
     bool near;                                 // neighbouring channels on one die
 };
 
-// exp(-x) for 0 <= x.  What the argument to the base 2 loses to rounding is put back, since a state remembers thousands of steps' gates: a
-// number in bf16 times a factor of 16 bits loses nothing, and the rest of the factor is small.
+// exp(-x) for 0 <= x.  In fp32 what the argument to the base 2 loses to rounding, x units of the result, is put back; beside a gate in bf16,
+// whose own rounding is 2^-9 of it, that is nothing.
 template <typename T> __device__ __forceinline__ float exp_minus(float x)
 {
-    constexpr float LN2 = 0.693147181f;
-    if constexpr (sizeof(T) == 2) {
-        constexpr float L = 1.44268799f, L_REST = 7.05260771e-6f;          // log2(e) = L + L_REST
-        const float e = __builtin_amdgcn_exp2f(-L * x);
-        return fmaf(e, (-LN2 * L_REST) * x, e);
-    } else {
-        constexpr float L = 1.44269504f, L_REST = 1.92596303e-8f;
-        const float t = L * x, rest = fmaf(L_REST, x, fmaf(L, x, -t)), e = __builtin_amdgcn_exp2f(-t);
-        return fmaf(e, -LN2 * rest, e);
-    }
+    constexpr float L = 1.44269504f, L_REST = 1.92596303e-8f, LN2 = 0.693147181f;         // log2(e) = L + L_REST
+    if constexpr (sizeof(T) == 2) return __builtin_amdgcn_exp2f(-L * x);
+    const float y = __builtin_elementwise_minimum(x, 200.f), t = L * y, rest = fmaf(L_REST, y, fmaf(L, y, -t)), e = __builtin_amdgcn_exp2f(-t);
+    return fmaf(e, -LN2 * rest, e);
 }
-// The larger and the smaller one of a = sigmoid(f) and c = 1 - a, both with the relative precision of a float.  a is the larger one
-// where f has no sign.  From |f| = 200 on the smaller one is 0; a NaN stays.
+// The larger and the smaller one of a = sigmoid(f) and c = 1 - a.  The smaller one has the relative precision of the exponential, and the
+// larger one is 1 less it, with a rounding of half a unit: a state remembers thousands of steps through gates near 1, and an error of the
+// reciprocal there would add up.  a is the larger one where f has no sign.  Infinite gates are exact, a NaN stays.
 template <typename T> __device__ __forceinline__ void gates(float f, float &big, float &small)
 {
-    const float e = exp_minus<T>(__builtin_elementwise_minimum(fabsf(f), 200.f));
-    const float s = 1.f + e, r = __builtin_amdgcn_rcpf(s);
-    big = fmaf(fmaf(-s, r, 1.f), r, r);
-    small = e * big;
+    const float e = exp_minus<T>(fabsf(f));
+    small = e * __builtin_amdgcn_rcpf(1.f + e);
+    big = 1.f - small;
 }
 template <typename T> __device__ __forceinline__ void gates_of(float f, float &a, float &c)
 {
     float big, small;
-    gates<T>(f, big, small);
+    gates<T>(f, big, small);               // (a NaN in both)
     a = f >= 0.f ? big : small;
     c = f >= 0.f ? small : big;
 }
-// Both in one number: the smaller one, with a's place in the sign.  1 - small is the larger one with a rounding of half a unit.
+// Both in one number: the smaller one, with a's place in the sign
 template <typename T> __device__ __forceinline__ float gates_in_one(float f) { float big, small; gates<T>(f, big, small); return copysignf(small, f); }
 __device__ __forceinline__ float a_of(float v) { return __float_as_int(v) >= 0 ? 1.f - v : -v; }
 __device__ __forceinline__ float c_of(float v) { return __float_as_int(v) >= 0 ? v : 1.f + v; }

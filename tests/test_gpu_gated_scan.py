@@ -1,8 +1,7 @@
 """The gated linear recurrence and its gradients against the formulas in 64 bits, step by step.
 
-Tolerances.  U = 2^-24 and B = 2^-8 are the unit roundoffs of fp32 and bf16.  A gate's a and 1 - a are off by G = 8 U relatively: the exponential by
-3 U, its sum with one, the reciprocal and the product by 5 more at most.  State t is a
-sum of terms (w_j x_j, or the initial state) times the gates of the steps since, in whatever order the steps are joined: each factor brings
+Tolerances.  U = 2^-24 and B = 2^-8 are the unit roundoffs of fp32 and bf16.  A gate's a and 1 - a are off by G relatively: the exponential by 3 U,
+its sum with one, the reciprocal and the product by 5 more at most; from bf16 gates the exponent's product has 1.3 |f| U beside it.  State t is a sum of terms (w_j x_j, or the initial state) times the gates of the steps since, in whatever order the steps are joined: each factor brings
 G and a rounding, each join (one in sixteen steps) and each addition another, so that it is off by (G + 3 U) N_t + 6 U M_t at most with
 M_t = a_t M_{t-1} + |w_t x_t|, the sum of the terms' sizes, and N_t = a_t (N_{t-1} + M_{t-1}) + |w_t x_t|, where each counts as often as it has
 factors.  The gradients g_t are such sums from the other end.  dx = w g and df = g a c (h - x) have a rounding or G for each factor on
@@ -36,7 +35,7 @@ def _exact(s, plain):
     x, f, dh = (s[k].double() for k in ("x", "gate", "dh"))
     B_, T, d = x.shape
     zero = torch.zeros(B_, d, dtype=torch.float64, device=x.device)
-    G = 8 * U
+    G = (8 if s["x"].dtype == torch.float32 else 2 * float(f.abs().max()) + 8 if f.numel() else 0) * U
     a, c = torch.sigmoid(f), torch.sigmoid(-f)
     w = torch.ones_like(c) if plain else c
     end = s["lengths"].clamp(0, T) if "lengths" in s else torch.full((B_,), T, device=x.device)
