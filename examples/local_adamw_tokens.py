@@ -5,7 +5,7 @@ The model is an embedding, a residual sub-block and a head:
     x = E[token];  m = relu(norm(x) W1) W2;  logits = norm(x + m) Wo
 
 Its matrix products are torch's, batched over the workers, on bf16 copies of the parameters.  Everything around them is this
-package's: both norms with the residual's addition, log probabilities and their gradient, AdamW over all tensors at once (moments in
+package's: the embedding and its gradient, both norms with the residual's addition, log probabilities and their gradient, AdamW over all tensors at once (moments in
 8 or in 32 bits, copies written by the same pass), the synchronization periods of Eq. (2) and the averaging of the workers.  Tokens
 come from a random chain: each has one likely successor.
 
@@ -68,7 +68,7 @@ class Model:
 
     def forward(self, tok):
         c = self.copy
-        x = torch.stack([c["E"][k][tok[k]] for k in range(self.K)])
+        x = qsr.embedding(tok, c["E"])
         n1 = qsr.rmsnorm(x, self.p["g1"])
         a = torch.bmm(n1.y, c["W1"]).relu_()
         n2 = qsr.rmsnorm(torch.bmm(a, c["W2"]), self.p["g2"], residual=x)
@@ -90,8 +90,7 @@ class Model:
         dx, dg1 = qsr.rmsnorm_backward(torch.bmm(da, turn(c["W1"])), x, self.p["g1"], n1.rstd, residual_grad=dm)
         g["g1"].copy_(dg1)
         g["g2"].copy_(dg2)
-        for k in range(self.K):
-            g["E"][k].copy_(torch.zeros(self.V, self.d, device=x.device).index_add_(0, tok[k], dx[k].float()))
+        qsr.embedding_backward(dx, tok, c["E"], out=g["E"])
         return -lp.logp.mean(1)
 
 
@@ -129,7 +128,7 @@ def continue_from(model, first, n, top=3):
     W8 = (W / scale[:, None]).to(torch.float8_e4m3fn)
     got, tok = [], torch.tensor([first], device=W.device)
     for _ in range(n):
-        x = model.copy["E"][0][tok]
+        x = qsr.embedding(tok, model.copy["E"][0])
         a = (qsr.rmsnorm(x, model.p["g1"][0]).y @ model.copy["W1"][0]).relu_()
         y = qsr.rmsnorm(a @ model.copy["W2"][0], model.p["g2"][0], residual=x, out="fp8")
         logits = (y.y.float() @ W8.float().t()) * y.scale[:, None] * scale
