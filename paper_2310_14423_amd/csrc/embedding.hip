@@ -43,20 +43,20 @@ __device__ __forceinline__ void store_run(T *p, const float (&v)[E], int skip)
 template <typename TI, typename TO, int E>
 __global__ __launch_bounds__(EMBED_THREADS) void embedding_kernel(LookupArgs a)
 {
-    const int lane = threadIdx.x & (a.lanes - 1), place = threadIdx.x / a.lanes, k = blockIdx.y;
-    const long long row = (long long)blockIdx.x * (EMBED_THREADS / a.lanes) + place;
-    if (row >= a.N) return;
-    const long long tok = a.tokens[k * a.N + row];
-    const bool has = tok >= 0 && tok < a.V;
-    const TI *const from = (const TI *)a.table + k * a.s_worker + (has ? tok : 0) * a.s_table;
-    TO *const to = (TO *)a.y + (k * a.N + row) * a.s_y;
-    for (int first = lane * E; first < a.d; first += a.lanes * E) {
-        const Run r = run_of(first, a.d, E);
-        float v[E];
-        load_wide<TI, E, false>(from + r.at, v);
+    const int lane = threadIdx.x & (a.lanes - 1), place = threadIdx.x / a.lanes, side = EMBED_THREADS / a.lanes, k = blockIdx.y;
+    for (long long row = (long long)blockIdx.x * side + place; row < a.N; row += (long long)gridDim.x * side) {
+        const long long tok = a.tokens[k * a.N + row];
+        const bool has = tok >= 0 && tok < a.V;
+        const TI *const from = (const TI *)a.table + k * a.s_worker + (has ? tok : 0) * a.s_table;
+        TO *const to = (TO *)a.y + (k * a.N + row) * a.s_y;
+        for (int first = lane * E; first < a.d; first += a.lanes * E) {
+            const Run r = run_of(first, a.d, E);
+            float v[E];
+            load_wide<TI, E, false>(from + r.at, v);
 #pragma unroll
-        for (int u = 0; u < E; ++u) v[u] = has ? v[u] * a.scale : 0.f;
-        store_run<TO, E>(to + r.at, v, r.skip);
+            for (int u = 0; u < E; ++u) v[u] = has ? v[u] * a.scale : 0.f;
+            store_run<TO, E>(to + r.at, v, r.skip);
+        }
     }
 }
 
@@ -645,11 +645,15 @@ static int direct_rows(long long K, long long V)
     const long long rows = (K * V + 1023) / 1024;
     return (int)(rows > DIRECT_ROWS ? DIRECT_ROWS : rows);
 }
-// Few tokens with little in their rows, and not too many workgroups that read all of the tokens: one launch
+// Few tokens with little in their rows, and not too many workgroups that read all of the tokens: one launch.  A workgroup with several rows
+// of the table may have a third of all tokens, if the first rows are the frequent ones.  us with one launch / with a sort: 4 x 1024
+// tokens over 512 rows of 128 in bf16 5.6 / 15.1, 64 over 200000 of 64 8.5 / 12.2, 8 x 1000 over 100 of 700 in fp32 9.3 / 19.1, 2000 over 16 of 512
+// in bf16 10.8 / 12.8; but 2000 over 2 of 512 45 / 14, 2048, the first rows frequent, over 32768 of 512 40 / 17, 8 x 2048 over 200000 of 64 80 / 48.
 static bool direct(long long K, long long N, long long V, long long d, int size)
 {
-    if (N < 1 || N > DIRECT_TOKENS || N * d * size > (2 << 20)) return false;
-    const long long rows = direct_rows(K, V);
+    if (N < 1 || N > DIRECT_TOKENS) return false;
+    const long long rows = direct_rows(K, V), bytes = N * d * size;
+    if (bytes > (rows > 1 ? 1 << 19 : 1 << 21) || bytes * rows > V * (1 << 17)) return false;
     return K * ((V + rows - 1) / rows) * N * 8 <= (1 << 27);
 }
 
@@ -717,8 +721,8 @@ static hipError_t launch_lookup(LookupArgs &a, int K, hipStream_t s)
 {
     constexpr int E = wide_of<TI>();
     a.lanes = lanes_for(a.d, a.d < E ? 1 : E);
-    const long long side = EMBED_THREADS / a.lanes;
-    const dim3 grid((unsigned)((a.N + side - 1) / side), (unsigned)K);
+    const long long side = EMBED_THREADS / a.lanes, trips = (a.N + side - 1) / side;
+    const dim3 grid((unsigned)(trips < (1 << 20) ? trips : 1 << 20), (unsigned)K);
     if (a.d < E) embedding_kernel<TI, TO, 1><<<grid, EMBED_THREADS, 0, s>>>(a);
     else embedding_kernel<TI, TO, E><<<grid, EMBED_THREADS, 0, s>>>(a);
     return hipGetLastError();
