@@ -5,8 +5,13 @@
 // The gradient's sums are made in a fixed order and without atomics.  The worker's tokens are sorted with their places by a stable radix
 // sort, so that a row's terms lie side by side in the order of their places.  The sorted list is cut into chunks of equal length, however
 // often a token comes: a chunk's sums go to their rows, but for a sum that other chunks have a part in, which is kept aside and joined by a
-// second launch in the chunks' order.  Rows of the table that no token names are found by a search in the list, and cleared by the same
-// launch that writes the others.  All sums are fp32; a row is scaled, and rounded, once.
+// second launch in the chunks' order.  Few tokens are sorted, summed and joined in LDS, by one launch whose workgroups share the table's
+// rows.  Rows that no token names are cleared beside the sort, or where the list does not hold them.  All sums are fp32; a row is scaled,
+// and rounded, once.
+// Bound by memory: rows are read once and written once, the table is cleared once.  8 x 8192 tokens, the first rows frequent, over 32768 rows of 768,
+// rows in bf16, the table's gradient in fp32: 143 us for the sort and the clearing, 5.6 TB/s, 48 for the sums, 8.8 for what several chunks
+// share; lookup 30 us.  30011 tokens over 50021 rows of 1003 in fp32, added to what is there: 30 us for the sort (four launches, latency),
+// 42 and 7.3; lookup 28.  4 x 1024 tokens over 512 rows of 128: 6.2 us in one launch, a chain of latencies; lookup 2.6.
 #include <cmath>
 
 #include "qsr_internal.h"

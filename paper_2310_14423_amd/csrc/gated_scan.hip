@@ -12,6 +12,13 @@
 // nothing of h's rounding in the gradients.
 // A reset cuts a map off from what was before: A = -1 stands for that (A is never negative), so that an infinity or a NaN ends there too.
 // All arithmetic is fp32.
+// Rows are addressed as buffers (what is the same for a wavefront stays in scalar registers: forward a fifth fewer vector instructions than with
+// pointers, 85 -> 76 us below).  Bound by memory at 64 x 1024 steps of 1024 in bf16: forward 74 us, 5.7 TB/s, backward 150 us, 4.6 TB/s with one
+// workgroup of eight wavefronts to a compute unit (190 registers a lane; at 128 they go to memory and back, 230 us).  32768 steps of 2048 on
+// 512 workgroups: maps 43 us, 6.1 TB/s, and 65 us; 2 x 16384 of 768 22 + 35 us, backward 20 + 55.  fp32, 13 sequences of up to 1001
+// steps of 1003: 26 and 38 us, the time of the longest one.  Four single steps of 2048: 3 us, latency.
+// What the second read costs could be saved by workgroups that wait for each other's maps while they hold their steps in registers: forward
+// that leaves two of them to a compute unit, each idle for the way of a map through memory; backward one.
 #include <cmath>
 #include <initializer_list>
 #include <type_traits>

@@ -43,9 +43,12 @@ def _want(dy, tok, V, scale, old=None):
     x = torch.where(has[..., None], dy.double(), torch.zeros_like(dy, dtype=torch.float64))
     grad, size, count = (torch.zeros(K, V, n, dtype=torch.float64, device="cuda") for n in (d, d, 1))
     for k in range(K):
-        grad[k].index_add_(0, at[k], x[k])
-        size[k].index_add_(0, at[k], x[k].abs())
-        count[k].index_add_(0, at[k], has[k].double()[:, None])
+        rows = torch.unique(at[k])
+        for out, add in ((grad, x[k]), (size, x[k].abs()), (count, has[k].double()[:, None])):
+            if len(rows) == 1:          # (index_add_ would wait for itself)
+                out[k, rows[0]] = add.sum(0)
+            else:
+                out[k].index_add_(0, at[k], add)
     want, room = scale * grad, abs(scale) * U * (count + 2) * size
     if old is not None:
         want = want + old.double()
