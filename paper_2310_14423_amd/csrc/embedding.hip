@@ -9,8 +9,8 @@
 // rows.  Rows that no token names are cleared beside the sort, or where the list does not hold them.  All sums are fp32; a row is scaled,
 // and rounded, once.
 // Bound by memory: rows are read once and written once, the table is cleared once.  8 x 8192 tokens, the first rows frequent, over 32768 rows of 768,
-// rows in bf16, the table's gradient in fp32: 143 us for the sort and the clearing, 5.6 TB/s, 48 for the sums, 8.8 for what several chunks
-// share; lookup 30 us.  30011 tokens over 50021 rows of 1003 in fp32, added to what is there: 30 us for the sort (four launches, latency),
+// rows in bf16, the table's gradient in fp32: 141 us for the sort and the clearing, 5.7 TB/s, 45 for the sums, 9.5 for what several chunks
+// share; lookup 29 us.  30011 tokens over 50021 rows of 1003 in fp32, added to what is there: 30 us for the sort (four launches, latency),
 // 42 and 7.3; lookup 28.  4 x 1024 tokens over 512 rows of 128: 6.2 us in one launch, a chain of latencies; lookup 2.6.
 #include <cmath>
 
@@ -636,6 +636,10 @@ __global__ __launch_bounds__(EMBED_THREADS) void embedding_direct_kernel(DirectA
 // ---------------------------------------------------------------------------------------------------
 constexpr long long EMBED_MOST = 1ll << 27;    // tokens of a worker
 
+// Elements of a lane: 16 bytes of the wider of what is read and what is written, so that what is written streams in whole lines (8 x 8192
+// tokens over 32768 rows of 768, rows in bf16, the table's gradient in fp32: 222 us a pass, lookup included, 239 with 32 bytes of a lane to write)
+template <typename TI, typename TO> constexpr int lane_elements() { return wide_of<TI>() < wide_of<TO>() ? wide_of<TI>() : wide_of<TO>(); }
+
 static int lanes_for(long long d, int E)
 {
     const long long runs = (d + E - 1) / E;
@@ -664,7 +668,7 @@ static bool direct(long long K, long long N, long long V, long long d, int size)
 
 // How the tokens of K workers are sorted and summed, and where what lies in the workspace
 struct GradPlan {
-    int passes, bits, chunk, lanes, slices;
+    int passes, bits, chunk;
     long long blocks, per, chunks;
     size_t keys[2], place[2], counts, parts, bytes;
 };
@@ -678,9 +682,7 @@ static GradPlan grad_plan(int K, long long N, long long V, long long d, int E)
     p.per = SORT_ROUND;
     while ((N + p.per - 1) / p.per > 128) p.per *= 2;
     p.blocks = N <= SORT_SMALL ? 0 : (N + p.per - 1) / p.per;
-    p.lanes = lanes_for(d, E);
-    p.slices = (int)((d + (long long)p.lanes * E - 1) / ((long long)p.lanes * E));
-    const long long waves = (long long)K * ((N + CHUNK_MOST - 1) / CHUNK_MOST) * p.lanes * p.slices / 64;
+    const long long waves = (long long)K * ((N + CHUNK_MOST - 1) / CHUNK_MOST) * ((d + 64 * E - 1) / (64 * E));
     p.chunk = waves < 2048 ? 8 : CHUNK_MOST;
     p.chunks = (N + p.chunk - 1) / p.chunk;
     size_t at = 0;
@@ -697,7 +699,8 @@ static GradPlan grad_plan(int K, long long N, long long V, long long d, int E)
 template <typename TI, typename TO, int E>
 static hipError_t launch_sums(GradArgs &a, const GradPlan &p, int K, bool cleared, hipStream_t s)
 {
-    const int side = EMBED_THREADS / p.lanes;
+    a.lanes = lanes_for(a.d, E);
+    const int side = EMBED_THREADS / a.lanes, slices = (int)((a.d + (long long)a.lanes * E - 1) / ((long long)a.lanes * E));
     a.chunk_groups = (p.chunks + side - 1) / side;
     // some 128 KiB to a workgroup that clears, and a row to each of its threads at most
     const long long row = (long long)a.d * (long long)sizeof(TO), rows = (131072 + row - 1) / row;
@@ -705,7 +708,7 @@ static hipError_t launch_sums(GradArgs &a, const GradPlan &p, int K, bool cleare
     a.clear_lanes = lanes_for(a.d, clear_elements(E, (int)sizeof(TO)));
     const long long clears = a.add || cleared ? 0 : (a.V + a.clear_rows - 1) / a.clear_rows;
     if (a.chunk_groups + clears > 0)
-        embedding_sums_kernel<TI, TO, E><<<dim3((unsigned)(a.chunk_groups + clears), (unsigned)K, (unsigned)p.slices), EMBED_THREADS, 0, s>>>(a);
+        embedding_sums_kernel<TI, TO, E><<<dim3((unsigned)(a.chunk_groups + clears), (unsigned)K, (unsigned)slices), EMBED_THREADS, 0, s>>>(a);
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || p.chunks < 2) return e;
     constexpr int J = E < 4 ? 1 : 4;
@@ -714,8 +717,9 @@ static hipError_t launch_sums(GradArgs &a, const GradPlan &p, int K, bool cleare
 }
 
 template <typename TI, typename TO, int E>
-static hipError_t launch_direct(const DirectArgs &a, int K, hipStream_t s)
+static hipError_t launch_direct(DirectArgs &a, int K, hipStream_t s)
 {
+    a.lanes = lanes_for(a.d, E);
     const dim3 grid((unsigned)((a.V + a.rows - 1) / a.rows), (unsigned)K, (unsigned)((a.d + (long long)a.lanes * E - 1) / ((long long)a.lanes * E)));
     embedding_direct_kernel<TI, TO, E><<<grid, EMBED_THREADS, 0, s>>>(a);
     return hipGetLastError();
@@ -724,7 +728,7 @@ static hipError_t launch_direct(const DirectArgs &a, int K, hipStream_t s)
 template <typename TI, typename TO>
 static hipError_t launch_lookup(LookupArgs &a, int K, hipStream_t s)
 {
-    constexpr int E = wide_of<TI>();
+    constexpr int E = lane_elements<TI, TO>();
     a.lanes = lanes_for(a.d, a.d < E ? 1 : E);
     const long long side = EMBED_THREADS / a.lanes, trips = (a.N + side - 1) / side;
     const dim3 grid((unsigned)(trips < (1 << 20) ? trips : 1 << 20), (unsigned)K);
@@ -801,9 +805,9 @@ extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void
     const bool wide = q->grad_type == QSR_TYPE_F32;
 #define EMBED_BY_TYPE(F) (q->type == QSR_TYPE_F32 ? (wide ? F(float, float) : F(float, bf16_t)) : (wide ? F(bf16_t, float) : F(bf16_t, bf16_t)))
     if (direct(K, N, q->vocab, q->d, (int)size_of(q->type))) {
-        const DirectArgs a{q->y_grad, q->tokens, q->grad, q->vocab, q->y_grad_stride, q->grad_stride, q->worker_stride, (int)N, (int)q->d,
-                           lanes_for(q->d, E), direct_rows(K, q->vocab), (float)q->scale, q->accumulate != 0};
-#define EMBED_DIRECT(TI, TO) (E == 1 ? launch_direct<TI, TO, 1>(a, K, s) : launch_direct<TI, TO, wide_of<TI>()>(a, K, s))
+        DirectArgs a{q->y_grad, q->tokens, q->grad, q->vocab, q->y_grad_stride, q->grad_stride, q->worker_stride, (int)N, (int)q->d, 0,
+                     direct_rows(K, q->vocab), (float)q->scale, q->accumulate != 0};
+#define EMBED_DIRECT(TI, TO) (E == 1 ? launch_direct<TI, TO, 1>(a, K, s) : launch_direct<TI, TO, lane_elements<TI, TO>()>(a, K, s))
         return finish(EMBED_BY_TYPE(EMBED_DIRECT));
 #undef EMBED_DIRECT
     }
@@ -861,8 +865,8 @@ extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void
         if (e != hipSuccess) return finish(e);
     }
     GradArgs a{q->y_grad, (const uint32_t *)(ws + p.keys[done]), (const int *)(ws + p.place[done]), q->grad, (float *)(ws + p.parts), N, q->vocab, p.chunks,
-               q->y_grad_stride, q->grad_stride, q->worker_stride, 0, (int)q->d, p.lanes, p.chunk, 0, 0, (float)q->scale, q->accumulate != 0};
-#define EMBED_SUMS(TI, TO) (E == 1 ? launch_sums<TI, TO, 1>(a, p, K, cleared, s) : launch_sums<TI, TO, wide_of<TI>()>(a, p, K, cleared, s))
+               q->y_grad_stride, q->grad_stride, q->worker_stride, 0, (int)q->d, 0, p.chunk, 0, 0, (float)q->scale, q->accumulate != 0};
+#define EMBED_SUMS(TI, TO) (E == 1 ? launch_sums<TI, TO, 1>(a, p, K, cleared, s) : launch_sums<TI, TO, lane_elements<TI, TO>()>(a, p, K, cleared, s))
     return finish(EMBED_BY_TYPE(EMBED_SUMS));
 #undef EMBED_SUMS
 #undef EMBED_BY_TYPE
