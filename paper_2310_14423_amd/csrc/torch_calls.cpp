@@ -4,9 +4,11 @@
 //
 // Arguments are those of the functions in operators.py, with the stream's address behind.  ValueError for what is checked here; a
 // code of the library's other than QSR_OK goes to the function that setup() was given, which raises.
+#include <ATen/EmptyTensor.h>
 #include <ATen/core/Tensor.h>
 #include <ATen/core/grad_mode.h>
 #include <ATen/ops/empty.h>
+#include <c10/core/Allocator.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -83,12 +85,24 @@ const float *numbers(const at::Tensor &t, const at::Tensor &x, int64_t each, con
     return (const float *)t.const_data_ptr();
 }
 
-at::Tensor new_like(const at::Tensor &x, at::ScalarType type) { return at::empty(x.sizes(), x.options().dtype(type)); }
+// A new tensor on x's device, which is the current one (operators.py), from the allocator that x's memory is from: 0.3 us, where at::empty's
+// way through the dispatcher makes it 0.7, with up to ten of them in a call and its backward pass.  Memory from elsewhere has none.
+at::Tensor fresh(const at::Tensor &x, c10::IntArrayRef size, at::ScalarType type)
+{
+    c10::Allocator *const allocator = x.storage().unsafeGetStorageImpl()->allocator();
+    if (allocator != nullptr) {
+        at::Tensor t = at::detail::empty_generic(size, allocator, c10::DispatchKeySet(c10::DispatchKey::CUDA), type, std::nullopt);
+        if (t.device() == x.device()) return t;
+    }
+    return at::empty(size, x.options().dtype(type));
+}
+at::Tensor new_bytes(const at::Tensor &x, size_t n) { return n ? fresh(x, {(int64_t)n}, at::kByte) : at::Tensor(); }
+at::Tensor new_like(const at::Tensor &x, at::ScalarType type) { return fresh(x, x.sizes(), type); }
 at::Tensor new_rows(const at::Tensor &x, at::ScalarType type, int64_t each = 0)
 {
     c10::SmallVector<int64_t, 6> s(x.sizes().begin(), x.sizes().end() - 1);
     if (each) s.push_back(each);
-    return at::empty(s, x.options().dtype(type));
+    return fresh(x, s, type);
 }
 
 // Workers, rows of each, and the stride of their weights
@@ -199,7 +213,7 @@ PyObject *rmsnorm_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
         size_t bytes = 0;
         check(qsr_rmsnorm_workspace_bytes(a.K, a.rows, a.d, a.type, &bytes), "qsr_rmsnorm_workspace_bytes");
         at::Tensor ws, dx = new_like(h, h.scalar_type()), dw = new_like(w, at::kFloat);
-        if (bytes) ws = at::empty({(int64_t)bytes}, h.options().dtype(at::kByte));
+        ws = new_bytes(h, bytes);
         a.x_grad = dx.mutable_data_ptr();
         a.weight_grad = (float *)dw.mutable_data_ptr();
         check(qsr_rmsnorm_backward(&a, bytes ? ws.mutable_data_ptr() : nullptr, bytes, stream_of(o[5])), "qsr_rmsnorm_backward");
@@ -273,7 +287,7 @@ PyObject *layernorm_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
         check(qsr_layernorm_workspace_bytes(a.K, a.rows, a.d, a.type, &bytes), "qsr_layernorm_workspace_bytes");
         at::Tensor ws, dx = new_like(h, h.scalar_type()), dw = new_like(w, at::kFloat), db;
         if (o[6] == Py_True) { db = new_like(w, at::kFloat); a.bias_grad = (float *)db.mutable_data_ptr(); }
-        if (bytes) ws = at::empty({(int64_t)bytes}, h.options().dtype(at::kByte));
+        ws = new_bytes(h, bytes);
         a.x_grad = dx.mutable_data_ptr();
         a.weight_grad = (float *)dw.mutable_data_ptr();
         check(qsr_layernorm_backward(&a, bytes ? ws.mutable_data_ptr() : nullptr, bytes, stream_of(o[7])), "qsr_layernorm_backward");
@@ -313,7 +327,7 @@ PyObject *embedding(PyObject *, PyObject *const *o, Py_ssize_t n)
         a.d = a.y_stride = table.size(-1);
         c10::SmallVector<int64_t, 6> shape(tok.sizes().begin(), tok.sizes().end());
         shape.push_back(a.d);
-        at::Tensor y = at::empty(shape, table.options().dtype(a.y_type == QSR_TYPE_F32 ? at::kFloat : at::kBFloat16));
+        at::Tensor y = fresh(table, shape, a.y_type == QSR_TYPE_F32 ? at::kFloat : at::kBFloat16);
         a.table = table.const_data_ptr();
         a.tokens = (const int64_t *)tok.const_data_ptr();
         a.y = y.mutable_data_ptr();
@@ -352,7 +366,7 @@ PyObject *embedding_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
         size_t bytes = 0;
         check(qsr_embedding_workspace_bytes(a.K, a.tokens_each, a.vocab, a.d, a.type, &bytes), "qsr_embedding_workspace_bytes");
         at::Tensor ws;
-        if (bytes) ws = at::empty({(int64_t)bytes}, table.options().dtype(at::kByte));
+        ws = new_bytes(table, bytes);
         a.y_grad = dy.const_data_ptr();
         a.tokens = (const int64_t *)tok.const_data_ptr();
         a.grad = grad.mutable_data_ptr();
@@ -391,7 +405,7 @@ at::Tensor new_state(const at::Tensor &x, int64_t each = -1)
     c10::SmallVector<int64_t, 6> s(x.sizes().begin(), x.sizes().end() - 2);
     if (each >= 0) s.push_back(each);
     s.push_back(x.size(-1));
-    return at::empty(s, x.options().dtype(at::kFloat));
+    return fresh(x, s, at::kFloat);
 }
 
 // what both passes have
@@ -422,10 +436,10 @@ void scan_common(Args &a, const at::Tensor &x, const at::Tensor &gate, const at:
         a.lengths = (const int64_t *)lengths->const_data_ptr();
     }
 }
-at::Tensor scan_workspace(int64_t batch, int64_t steps, int64_t d, int32_t type, const at::Tensor &x, size_t &bytes)
+at::Tensor scan_workspace(const at::Tensor &x, int64_t batch, int64_t steps, int64_t d, int32_t type, size_t &bytes)
 {
     check(qsr_gated_scan_workspace_bytes(batch, steps, d, type, &bytes), "qsr_gated_scan_workspace_bytes");
-    return bytes ? at::empty({(int64_t)bytes}, x.options().dtype(at::kByte)) : at::Tensor();
+    return new_bytes(x, bytes);
 }
 
 // x, gate, initial, reset, lengths, input, keep, state_out, stream
@@ -451,7 +465,7 @@ PyObject *gated_scan(PyObject *, PyObject *const *o, Py_ssize_t n)
             a.states = (float *)states.mutable_data_ptr();
         }
         size_t bytes = 0;
-        at::Tensor ws = scan_workspace(a.batch, a.steps, a.d, a.type, x, bytes);
+        at::Tensor ws = scan_workspace(x, a.batch, a.steps, a.d, a.type, bytes);
         check(qsr_gated_scan(&a, bytes ? ws.mutable_data_ptr() : nullptr, bytes, stream_of(o[8])), "qsr_gated_scan");
         PyObject *l;
         if (out) { written(*out); l = o[7]; Py_INCREF(l); }
@@ -486,7 +500,7 @@ PyObject *gated_scan_backward(PyObject *, PyObject *const *o, Py_ssize_t n)
         a.x_grad_stride = a.gate_grad_stride = a.d;
         a.x_grad_batch_stride = a.gate_grad_batch_stride = a.steps > 0 ? a.steps * a.d : a.d;
         size_t bytes = 0;
-        at::Tensor ws = scan_workspace(a.batch, a.steps, a.d, a.type, x, bytes);
+        at::Tensor ws = scan_workspace(x, a.batch, a.steps, a.d, a.type, bytes);
         check(qsr_gated_scan_backward(&a, bytes ? ws.mutable_data_ptr() : nullptr, bytes, stream_of(o[8])), "qsr_gated_scan_backward");
         return result(nullptr, {wrap(std::move(dx)), wrap(std::move(dgate)), wrap(std::move(first))});
     });
@@ -533,7 +547,7 @@ PyObject *token_logprobs(PyObject *, PyObject *const *o, Py_ssize_t n)
             a.top_logp = (float *)top_logp.mutable_data_ptr();
             a.top_id = (int32_t *)top_id.mutable_data_ptr();
         }
-        if (bytes) ws = at::empty({(int64_t)bytes}, x.options().dtype(at::kByte));
+        ws = new_bytes(x, bytes);
         check(qsr_token_logprobs(&a, bytes ? ws.mutable_data_ptr() : nullptr, bytes, stream_of(o[4])), "qsr_token_logprobs");
         return result(g_logprobs, {wrap(std::move(logp)), wrap(std::move(entropy)), wrap(std::move(lse)), wrap(std::move(stats)),
                                    wrap(std::move(top_logp)), wrap(std::move(top_id))});
