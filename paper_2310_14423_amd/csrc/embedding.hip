@@ -11,7 +11,7 @@
 // Bound by memory: rows are read once and written once, the table is cleared once.  8 x 8192 tokens, the first rows frequent, over 32768 rows of 768,
 // rows in bf16, the table's gradient in fp32: 141 us for the sort and the clearing, 5.7 TB/s, 45 for the sums, 9.5 for what several chunks
 // share; lookup 29 us.  30011 tokens over 50021 rows of 1003 in fp32, added to what is there: 30 us for the sort (four launches, latency),
-// 42 and 7.3; lookup 28.  4 x 1024 tokens over 512 rows of 128: 6.2 us in one launch, a chain of latencies; lookup 2.6.
+// 42 and 7.3; lookup 28.  4 x 1024 tokens over 512 rows of 128: 6.0 us in one launch, a chain of latencies; lookup 2.5.
 #include <cmath>
 
 #include "qsr_internal.h"
@@ -523,9 +523,15 @@ __global__ __launch_bounds__(EMBED_THREADS) void embedding_direct_kernel(DirectA
     to[wave][lane] = 0;
     const int run = (a.N + EMBED_THREADS - 1) / EMBED_THREADS * 64, from = min(a.N, wave * run), end = min(a.N, from + run);
     int mine = 0;
-    for (int i = from; i < end; i += 64) {
-        const int j = i + lane;
-        const long long row = (j < end ? a.tokens[(long long)k * a.N + j] : -1) - v0;
+    long long tok[RUN / 64];                   // all of them on their way at once
+#pragma unroll
+    for (int i = 0; i < RUN / 64; ++i)
+        if (from + i * 64 < end) tok[i] = a.tokens[(long long)k * a.N + min(from + i * 64 + lane, end - 1)];
+#pragma unroll
+    for (int i = 0; i < RUN / 64; ++i) {
+        const int j = from + i * 64 + lane;
+        if (from + i * 64 >= end) break;
+        const long long row = tok[i] - v0;
         const bool in = j < end && row >= 0 && row < rows;
         const uint64_t mask = __ballot(in);
         if (in) {

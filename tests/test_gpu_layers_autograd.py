@@ -96,3 +96,14 @@ def test_two_streams_at_once():
             got.append(run(s.cuda_stream))
     torch.cuda.synchronize()
     assert all(torch.equal(p, q) for r in got for p, q in zip(r, want))
+
+
+def test_memory_from_elsewhere():
+    """Arguments whose memory is not from torch's allocator (a capsule of another library's): results are torch's all the same."""
+    x, w, tok = torch.randn(5, 3, 32, device="cuda"), torch.ones(32, device="cuda"), torch.tensor([1, 0, 4], device="cuda")
+    other = torch.from_dlpack(torch.utils.dlpack.to_dlpack(x))
+    for call in (lambda t: qsr.layernorm(t, w, w, residual=t), lambda t: qsr.gated_scan(t, t, keep=True), lambda t: (qsr.embedding(tok, t[0]),),
+                 lambda t: (qsr.embedding_backward(t[0], tok, t[:, 0]),), lambda t: qsr.rmsnorm(t, w)):
+        got = [v for v in call(other) if v is not None]
+        assert all(torch.equal(a, b) and a.device == x.device for a, b in zip(got, [v for v in call(x) if v is not None]))
+        assert all(v.is_contiguous() and not v.requires_grad for v in got)
