@@ -15,7 +15,7 @@
 // Rows are addressed as buffers (what is the same for a wavefront stays in scalar registers: forward a fifth fewer vector instructions than with
 // pointers, 85 -> 76 us below).  Bound by memory at 64 x 1024 steps of 1024 in bf16: forward 74 us, 5.7 TB/s, backward 150 us, 4.6 TB/s with one
 // workgroup of eight wavefronts to a compute unit (190 registers a lane; at 128 they go to memory and back, 230 us).  32768 steps of 2048 on
-// 512 workgroups: maps 43 us, 6.1 TB/s, and 65 us; 2 x 16384 of 768 22 + 35 us, backward 20 + 55.  fp32, 13 sequences of up to 1001
+// 512 workgroups: maps 44 us, 6.0 TB/s, and 65 us; 2 x 16384 of 768 19 + 33 us, backward 18 + 49.  fp32, 13 sequences of up to 1001
 // steps of 1003: 26 and 38 us, the time of the longest one.  Four single steps of 2048: 3 us, latency.
 // What the second read costs could be saved by workgroups that wait for each other's maps while they hold their steps in registers: forward
 // that leaves two of them to a compute unit, each idle for the way of a map through memory; backward one.
@@ -191,6 +191,32 @@ template <typename F> __device__ __forceinline__ void by_tile(bool plain, F f)
     else f(std::integral_constant<bool, true>());
 }
 
+// Behind the `count` maps first, first + step, ... of parts: a wavefront joins a run of them, and all of them the wavefronts' through `words`
+template <int V, int W>
+__device__ __forceinline__ void behind_parts(const float2 *m, long long d, int first, int step, int count, int wave, int lane, float2 (&words)[W][V][64],
+                                             float (&carry)[V])
+{
+    const int each = (count + W - 1) / W, from = min(count, wave * each), end = min(count, from + each);
+    float A[V], H[V];
+#pragma unroll
+    for (int u = 0; u < V; ++u) { A[u] = 1.f; H[u] = 0.f; }
+#pragma unroll 8
+    for (int i = from; i < end; ++i)
+#pragma unroll
+        for (int u = 0; u < V; ++u) {
+            const float2 f = m[(long long)(first + i * step) * d + u];
+            H[u] = behind_map(f.x, f.y, H[u]);
+            A[u] = f.x < 0.f || A[u] < 0.f ? -1.f : A[u] * f.x;
+        }
+#pragma unroll
+    for (int u = 0; u < V; ++u) words[wave][u][lane] = make_float2(A[u], H[u]);
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < W; ++w)
+#pragma unroll
+        for (int u = 0; u < V; ++u) { const float2 f = words[w][u][lane]; carry[u] = behind_map(f.x, f.y, carry[u]); }
+}
+
 // Forward, W wavefronts to a workgroup
 template <typename T, int V, int W, bool COMP, bool STREAM>
 __global__ __launch_bounds__(64 * W, 4) void scan_kernel(ScanArgs a)
@@ -201,13 +227,9 @@ __global__ __launch_bounds__(64 * W, 4) void scan_kernel(ScanArgs a)
     if (!q.find(a, lane, a.parts)) return;
     float carry[V];
     if (a.parts > 1) {
-        const float2 *const m = a.maps + ((long long)q.b * (a.parts + 1)) * a.d + q.at;
 #pragma unroll
         for (int u = 0; u < V; ++u) carry[u] = 0.f;
-#pragma unroll 16
-        for (int p = 0; p <= q.part; ++p)
-#pragma unroll
-            for (int u = 0; u < V; ++u) { const float2 f = m[(long long)p * a.d + u]; carry[u] = behind_map(f.x, f.y, carry[u]); }
+        behind_parts<V, W>(a.maps + ((long long)q.b * (a.parts + 1)) * a.d + q.at, a.d, 0, 1, q.part + 1, wave, lane, maps[1], carry);
     } else {
 #pragma unroll
         for (int u = 0; u < V; ++u) {
@@ -434,13 +456,8 @@ __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
     float carry[V];
 #pragma unroll
     for (int u = 0; u < V; ++u) carry[u] = a.initial != nullptr ? a.initial[(long long)q.b * a.d + q.at + u] : 0.f;
-    if (a.parts > 1) {
-        const float2 *const m = a.maps + ((long long)q.b * (a.parts + 1)) * a.d + q.at;
-#pragma unroll 16
-        for (int p = a.parts - 1; p > q.part; --p)
-#pragma unroll
-            for (int u = 0; u < V; ++u) { const float2 f = m[(long long)p * a.d + u]; carry[u] = behind_map(f.x, f.y, carry[u]); }
-    }
+    if (a.parts > 1)
+        behind_parts<V, W>(a.maps + ((long long)q.b * (a.parts + 1)) * a.d + q.at, a.d, a.parts - 1, -1, a.parts - 1 - q.part, wave, lane, maps[1], carry);
     const int begin = q.part * a.part_len, end = min(a.T, begin + a.part_len);
     const int trips = begin < end ? (end - begin + W * STEPS - 1) / (W * STEPS) : 0;
     uint32_t rx[STEPS], rf[STEPS], rg[STEPS], bits = 0;
@@ -553,17 +570,18 @@ __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
 // ---------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------
-// Channels of a lane: four bytes of them, one where there are not as many
-static int scan_channels(int type, long long d) { return type == QSR_TYPE_BF16 && d >= 2 ? 2 : 1; }
+// Channels of a lane: four bytes of them, or one where a wavefront has them all (us with one / two, 300 x 500 steps of 64, forward and backward: 24.8 / 31.1
+// and 37.9 / 49.6)
+static int scan_channels(int type, long long d) { return type == QSR_TYPE_BF16 && d > 64 ? 2 : 1; }
 
 // A workgroup has all steps of 64 lanes' channels, or a part of them.  Parts cost a second read of two of three to five arrays and a
 // launch; they are taken where workgroups are too few otherwise.
 // What a trip of a workgroup costs, in tenths of its time: 10 without parts and 14 with them, a part's start 3, the second launch 8; the maps of the
-// parts before, which each part joins, count too.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them, bf16,
-// forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 105 and 356 / 158; 32768 steps of 2048
-// 942 / 113.  With 128 workgroups and more forward and 192 backward the second read costs what is won (16 x 1024 steps of 1024,
-// forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs up to 512 workgroups; from there on eight
-// are faster, 76 against 80 at 64 x 1024 steps of 1024).
+// parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them, bf16,
+// forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and 356 / 150; 32768 steps of 2048
+// 942 / 111, of 64 948 / 12.4 and 1513 / 14.1.  With 128 workgroups and more forward and 192 backward the second read costs what is won (16 x
+// 1024 steps of 1024, forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs up to 512 workgroups; from
+// there on eight are faster, 76 against 80 at 64 x 1024 steps of 1024).
 struct ScanPlan { int waves, parts, part_len; long long groups; };
 static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool back)
 {
@@ -576,7 +594,7 @@ static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool 
     const long long trip = (long long)p.waves * STEPS, trips = (T + trip - 1) / trip;
     long long each = trips, best = 10 * trips;
     for (long long n = 2; have < few && p.waves == WAVES && n <= trips && n <= 4 * slots / have; ++n) {
-        const long long e = (trips + n - 1) / n, rounds = (have * n + slots - 1) / slots, cost = rounds * (14 * e + 3) + n / 8 + 8;
+        const long long e = (trips + n - 1) / n, rounds = (have * n + slots - 1) / slots, cost = rounds * (14 * e + 3) + n / 32 + 8;
         if ((trips + e - 1) / e == n && cost < best) { best = cost; each = e; }
     }
     if (trips > 0) p.parts = (int)((trips + each - 1) / each);

@@ -163,6 +163,20 @@ def test_states_in_place_of_many_parts():
             assert torch.equal(g.h, f.h) and torch.equal(again, f.last)
 
 
+@pytest.mark.parametrize("dt,d,full", [("bf16", 3, True), ("f32", 65, False)])
+def test_more_parts_than_wavefronts(dt, d, full):
+    """157 parts: each wavefront joins the maps of twenty of them, of the last one fewer."""
+    s = _data(1, 20001, d, DT[dt], 17, full)
+    f = qsr.gated_scan(s["x"], s["gate"], initial=s.get("initial"), keep=True, **_marks(s, False))
+    want, last, first = _exact(s, False)
+    _near(f.h, want["h"], want["h_"], "h")
+    _near(f.last, *last, "last")
+    dx, dgate, dinitial = qsr.gated_scan_backward(s["dh"], s["x"], s["gate"], f.states, last_grad=s.get("dlast"), **_marks(s, False))
+    _near(dx, want["dx"], want["dx_"], "dx")
+    _near(dgate, want["dgate"], want["dgate_"], "dgate")
+    _near(dinitial, *first, "dinitial")
+
+
 @pytest.mark.parametrize("dt", ["f32", "bf16"])
 @pytest.mark.parametrize("T", [9, 200, 3000])
 def test_pieces_of_a_sequence_backward(T, dt):
