@@ -593,9 +593,11 @@ static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool 
     p.waves = T <= STEPS ? 1 : !back && have >= few && have < 512 ? MANY_WAVES : WAVES;
     const long long trip = (long long)p.waves * STEPS, trips = (T + trip - 1) / trip;
     long long each = trips, best = 10 * trips;
-    for (long long n = 2; have < few && p.waves == WAVES && n <= trips && n <= 4 * slots / have; ++n) {
-        const long long e = (trips + n - 1) / n, rounds = (have * n + slots - 1) / slots, cost = rounds * (14 * e + 3) + n / 32 + 8;
-        if ((trips + e - 1) / e == n && cost < best) { best = cost; each = e; }
+    for (int round = 1; have < few && p.waves == WAVES && trips > 1 && round <= 4; ++round) {
+        const long long most = round * slots / have;           // more parts in as many rounds cost less
+        if (most < 2) continue;
+        const long long e = (trips + most - 1) / most, n = (trips + e - 1) / e, cost = (have * n + slots - 1) / slots * (14 * e + 3) + n / 32 + 8;
+        if (n > 1 && cost < best) { best = cost; each = e; }
     }
     if (trips > 0) p.parts = (int)((trips + each - 1) / each);
     p.part_len = (int)(each * trip);
