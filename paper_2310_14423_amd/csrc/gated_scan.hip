@@ -570,23 +570,30 @@ __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
 // ---------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------
-// Channels of a lane: four bytes of them, or one where a wavefront has them all (us with one / two, 300 x 500 steps of 64, forward and backward: 24.8 / 31.1
-// and 37.9 / 49.6)
-static int scan_channels(int type, long long d) { return type == QSR_TYPE_BF16 && d > 64 ? 2 : 1; }
+// Channels of a lane: four bytes of them, or one where a wavefront has them all, where workgroups are one to a compute unit then, without parts, and
+// where there are not as many with all tiles apart.  us with one / two, forward and backward: 300 x 500 steps of 64 channels 24.8 / 31.1 and 37.9 /
+// 49.6; 16 x 1024 of 1024 29.3 / 35.4 and 43.4 / 49.8, 13 x 1001 of 1003 27.3 / 37.9 and 43.3 / 53.2; 8 x 512 of 512 9.3 / 11.6 and 10.6 / 13.5; but
+// 24 x 700 of 1024 35.1 / 29.6 and 56.2 / 44.7, 8 x 1024 of 1024 24.0 / 19.4 and 32.3 / 26.7, 64 x 512 of 512 30.1 / 28.1 and 47.7 / 39.3.
+static int scan_channels(int type, long long B, long long T, long long d)
+{
+    if (type != QSR_TYPE_BF16 || d <= 64) return 1;
+    const long long ones = B * ((d + 63) / 64), tiles = ones * ((T + WAVES * STEPS - 1) / (WAVES * STEPS));
+    return T > 1 && ((ones > 192 && ones <= 256) || tiles <= 256) ? 1 : 2;
+}
 
 // A workgroup has all steps of 64 lanes' channels, or a part of them.  Parts cost a second read of two of three to five arrays and a
 // launch; they are taken where workgroups are too few otherwise.
 // What a trip of a workgroup costs, in tenths of its time: 10 without parts and 14 with them, a part's start 3, the second launch 8; the maps of the
-// parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them, bf16,
-// forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and 356 / 150; 32768 steps of 2048
+// parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them, bf16
+// and two channels of a lane, forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and 356 / 150; 32768 steps of 2048
 // 942 / 111, of 64 948 / 12.4 and 1513 / 14.1.  With 128 workgroups and more forward and 192 backward the second read costs what is won (16 x
 // 1024 steps of 1024, forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs up to 512 workgroups; from
 // there on eight are faster, 76 against 80 at 64 x 1024 steps of 1024).
-struct ScanPlan { int waves, parts, part_len; long long groups; };
+struct ScanPlan { int channels, waves, parts, part_len; long long groups; };
 static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool back)
 {
     ScanPlan p;
-    const int V = scan_channels(type, d);
+    const int V = p.channels = scan_channels(type, B, T, d);
     p.groups = (d + 64 * V - 1) / (64 * V);
     p.parts = 1;
     const long long have = B * p.groups, slots = back ? 256 : 512, few = back ? 192 : 128;
@@ -668,7 +675,7 @@ static hipError_t launch_scan(ScanArgs &a, int type, int input, long long B, boo
     const ScanPlan p = scan_plan(B, a.T, a.d, type, back);
     const bool comp = input == QSR_SCAN_COMPLEMENT;
     if (type == QSR_TYPE_F32) return comp ? launch_scan<float, 1, true>(a, p, B, back, s) : launch_scan<float, 1, false>(a, p, B, back, s);
-    if (scan_channels(type, a.d) == 2) return comp ? launch_scan<bf16_t, 2, true>(a, p, B, back, s) : launch_scan<bf16_t, 2, false>(a, p, B, back, s);
+    if (p.channels == 2) return comp ? launch_scan<bf16_t, 2, true>(a, p, B, back, s) : launch_scan<bf16_t, 2, false>(a, p, B, back, s);
     return comp ? launch_scan<bf16_t, 1, true>(a, p, B, back, s) : launch_scan<bf16_t, 1, false>(a, p, B, back, s);
 }
 

@@ -163,6 +163,30 @@ def test_states_in_place_of_many_parts():
             assert torch.equal(g.h, f.h) and torch.equal(again, f.last)
 
 
+@pytest.mark.parametrize("full", [False, True])
+@pytest.mark.parametrize("plain", [False, True])
+@pytest.mark.parametrize("B_,T,d", [(130, 16, 129), (90, 140, 130), (150, 290, 101), (100, 131, 333), (7, 2500, 700), (7, 2600, 641)])
+def test_two_channels_of_a_lane(B_, T, d, plain, full):
+    """Enough workgroups for them: one, eight and sixteen wavefronts, parts; even and odd rows, in tensors of their own and inside others."""
+    s = _data(B_, T, d, torch.bfloat16, 18, full)
+    marks = _marks(s, plain)
+    f = qsr.gated_scan(s["x"], s["gate"], initial=s.get("initial"), keep=True, **marks)
+    back = qsr.gated_scan_backward(s["dh"], s["x"], s["gate"], f.states, last_grad=s.get("dlast"), **marks)
+    want, last, first = _exact(s, plain)
+    _near(f.h, want["h"], want["h_"], "h")
+    _near(f.last, *last, "last")
+    _near(back[0], want["dx"], want["dx_"], "dx")
+    _near(back[1], want["dgate"], want["dgate_"], "dgate")
+    _near(back[2], *first, "dinitial")
+    both = torch.full((T, B_, 2 * d + 3), float("nan"), dtype=torch.bfloat16, device="cuda").transpose(0, 1)
+    x, gate = both[..., 1:1 + d], both[..., 2 + d:2 + 2 * d]
+    x.copy_(s["x"]), gate.copy_(s["gate"])
+    state = s["initial"].clone() if full else None
+    g = qsr.gated_scan(x, gate, initial=state, keep=True, state_out=state, **marks)
+    again = qsr.gated_scan_backward(s["dh"], x, gate, g.states, last_grad=s.get("dlast"), **marks)
+    assert all(torch.equal(p, q) for p, q in zip(f + tuple(back), g + tuple(again)))
+
+
 @pytest.mark.parametrize("dt,d,full", [("bf16", 3, True), ("f32", 65, False)])
 def test_more_parts_than_wavefronts(dt, d, full):
     """157 parts: each wavefront joins the maps of twenty of them, of the last one fewer."""
