@@ -31,6 +31,34 @@ struct LayerArgs {
     float eps;
 };
 
+// How a row of d elements is shared out: L lanes of W wavefronts, sixteen elements to a lane in bf16 where the row is long enough, eight in fp32.
+// A row that leaves half of its lanes empty is slower where there is a width between: us, forward and backward, with it / with the next power
+// of two, bf16: 15252 rows of 1100 31.9 / 33.0 and 41.7 / 48.5 (but 8192 of 2000 29.4 / 29.4 and 38.9 / 34.5), 3990 of 4204 30.2 / 34.5 and 36.7 /
+// 39.6 (but 2943 of 5700 30.4 / 30.7 and 41.4 / 37.6), 1398 of 12000 30.8 / 32.6 and 41.8 / 63.1: twelve wavefronts leave 168 registers to a lane,
+// sixteen 128; fp32: 3813 of 2200 29.1 / 28.6 and 32.5 / 37.5.
+struct LayerPlan { int L, W, side; };
+static LayerPlan layer_plan(long long d, int size)
+{
+    const long long unit = size == 2 ? 1024 : 512;
+    LayerPlan q;
+    q.L = d <= 128 ? 16 : d <= 256 ? 32 : 64;
+    q.W = d <= 512 || d <= unit ? 1 : d <= 2 * unit ? (size == 2 && d > 1536 ? 4 : 2) : d <= 4 * unit ? 4 : d <= 5 * unit ? 5 : d <= 8 * unit ? 8
+                                                                                         : size == 2 && d <= 12 * unit ? 12 : 16;
+    q.side = q.W == 1 ? 256 / q.L : 1;
+    return q;
+}
+#define LAYER_BY_WIDTH(T, d, F) do { constexpr int E_ = wide_of<T>(), N_ = sizeof(T) == 2 ? 16 / E_ : 8 / E_; \
+    if ((d) < E_) F(T, 16, 1, 0); else if ((d) <= 128) F(T, 16, 1, 8 / E_); else if ((d) <= 256) F(T, 32, 1, 8 / E_); \
+    else if ((d) <= 512) F(T, 64, 1, 8 / E_); \
+    else switch (layer_plan(d, (int)sizeof(T)).W) { \
+        case 1: F(T, 64, 1, 16 / E_); break; \
+        case 2: F(T, 64, 2, N_); break; \
+        case 4: if ((d) <= 2048) F(T, 64, 4, 8 / E_); else F(T, 64, 4, 16 / E_); break; \
+        case 5: F(T, 64, 5, N_); break; \
+        case 8: F(T, 64, 8, N_); break; \
+        case 12: F(T, 64, 12, 16 / E_); break; \
+        default: if ((d) <= 8192) F(T, 64, 16, 8 / E_); else F(T, 64, 16, 16 / E_); } } while (0)
+
 // `turn` counts the sums over a group of wavefronts, which take turns at their words
 template <typename T, int L, int W, int NV, bool FP8>
 __device__ __forceinline__ void layernorm_row(const LayerArgs &a, const RowPart<T, NV> &w, const RowPart<T, NV> &b, long long row, int lane,
@@ -128,15 +156,15 @@ __device__ __forceinline__ void group_sums(float &p, float &q, float (*red)[2][W
 }
 
 // A workgroup takes every gridDim.x-th row (W == 1: four of them at a time) and keeps its parts of the gradients of weight and bias in
-// registers.  There are two wavefronts to a SIMD at most (four in the widest rows), so that each may have half of its registers: with a quarter
+// registers.  There are two wavefronts to a SIMD at most (three and four in the widest rows), so that each may have half of its registers: with a quarter
 // the sixteen elements of bf16 rows go to memory and back, 8 x 12608 rows of 768 130 us instead of 116, 8192 rows of 4096 74 instead of
-// 56.  The next row's loads are under way while a row is worked on where that takes few registers, and where a workgroup of eight
-// wavefronts is alone on its compute unit (4096 rows of 8192 54 us, 60 without).
+// 56.  The next row's loads are under way while a row is worked on where that takes few registers, and where a workgroup of five to
+// eight wavefronts is alone on its compute unit (4096 rows of 8192 54 us, 60 without; 6 x 1915 of 4204 64, 88 without).
 template <typename T, int L, int W, int NV, bool BIAS>
-__global__ __launch_bounds__(rms_threads<W>(), W == 16 ? 4 : 2) void layernorm_back_kernel(LayerBackArgs a)
+__global__ __launch_bounds__(rms_threads<W>(), W > 8 ? (W + 3) / 4 : 2) void layernorm_back_kernel(LayerBackArgs a)
 {
     constexpr int E = wide_of<T>();
-    constexpr bool AHEAD = NV * (3 * E + 3 * 2 * 4) <= 48 || (W == 8 && E == 8);
+    constexpr bool AHEAD = NV * (3 * E + 3 * 2 * 4) <= 48 || (W > 4 && W <= 8 && E == 8);
     __shared__ float red[2][2][W];
     __shared__ float side_sum[W == 1 ? 3 * L * (NV * E + 1) : 1];
     constexpr int side = rms_side<L, W>();
@@ -253,25 +281,40 @@ static hipError_t launch_layer(const LayerArgs &a, int K, bool fp8, hipStream_t 
     // rows of 16384 54 us, 59 with a trip each; narrower ones are 1 to 3 % faster with a trip each)
     const long long wide = (512 + K - 1) / K;
 #define LAYER_FWD(T, L, W, NV) do { const long long trips = fwd_groups(a.rows, rms_side<L, W>()); \
-    const dim3 grid((unsigned)(W == 16 && trips > wide ? wide : trips), (unsigned)K); \
+    const dim3 grid((unsigned)(W > 8 && trips > wide ? wide : trips), (unsigned)K); \
     if (fp8) layernorm_kernel<T, L, W, NV, true><<<grid, rms_threads<W>(), 0, s>>>(a); \
     else layernorm_kernel<T, L, W, NV, false><<<grid, rms_threads<W>(), 0, s>>>(a); } while (0)
-    RMS_BY_WIDTH(T, a.d, LAYER_FWD);
+    LAYER_BY_WIDTH(T, a.d, LAYER_FWD);
 #undef LAYER_FWD
     return hipGetLastError();
+}
+
+// Workgroups of a worker in the backward pass: two wavefronts to each of the chip's SIMDs, four in the widest rows and five in narrow ones, and
+// not one more, where each has a place of its own and those behind it would wait for it to end (6 x 1915 rows of 4204 in bf16 63 us, 144 with
+// 43 workgroups of a worker instead of 42; 5 x 596 of 7488 in fp32 76, 102 with 52 instead of 51).  Each leaves a row of partial sums, and has
+// more than one row where some 160 of them remain: 2 x 455 rows of 1600 in bf16 10.4, 12.2 with a row each; 1000 of 4096 18.3, 22.5; 8 x 1472 of
+// 205 9.8, 12.0; but 5 x 171 of 554 8.5 with two, 7.5.  One, whose sums are the gradients already, for the rows of a few tokens.
+static long long layer_back_groups(int K, long long rows, long long d, int size)
+{
+    const LayerPlan q = layer_plan(d, size);
+    if (rows <= 2 * q.side) return 1;
+    const long long all = q.L < 64 ? 1280 : q.W == 2 ? 1024 : q.W <= 4 || (q.W == 5 && size == 4) ? 512 : 256;
+    const long long most = all / K > 1 ? all / K : 1, trips = (rows + q.side - 1) / q.side, few = q.W == 1 ? 2 : 4;
+    const long long own = K * trips / 160, each = own < 1 ? 1 : own < few ? own : few, need = (trips + each - 1) / each;
+    return most < need ? most : need;
 }
 
 template <typename T>
 static hipError_t launch_layer_back(LayerBackArgs &a, int K, float *workspace, float *dw, float *db, hipStream_t s)
 {
-    const long long groups = back_groups(K, a.rows, rms_plan(a.d, (int)sizeof(T)));
+    const long long groups = layer_back_groups(K, a.rows, a.d, (int)sizeof(T));
     const int cols = a.d * (db != nullptr ? 2 : 1);
     if (groups == 1) { a.part_w = dw; a.part_b = db; a.s_part = a.d; }
     else { a.part_w = workspace; a.part_b = workspace + a.d; a.s_part = cols; }
 #define LAYER_BACK(T, L, W, NV) do { const dim3 grid((unsigned)groups, (unsigned)K); \
     if (db != nullptr) layernorm_back_kernel<T, L, W, NV, true><<<grid, rms_threads<W>(), 0, s>>>(a); \
     else layernorm_back_kernel<T, L, W, NV, false><<<grid, rms_threads<W>(), 0, s>>>(a); } while (0)
-    RMS_BY_WIDTH(T, a.d, LAYER_BACK);
+    LAYER_BY_WIDTH(T, a.d, LAYER_BACK);
 #undef LAYER_BACK
     hipError_t e = hipGetLastError();
     if (e != hipSuccess || groups == 1) return e;
@@ -327,7 +370,7 @@ extern "C" int qsr_layernorm_workspace_bytes(int32_t K, int64_t rows, int64_t d,
     *bytes = 0;
     if (!sizes_ok(K, rows, d) || (type != QSR_TYPE_F32 && type != QSR_TYPE_BF16)) return QSR_EINVAL;
     if (d > RMS_MAX_D) return QSR_ELIMIT;
-    const long long groups = back_groups(K, rows, rms_plan(d, (int)size_of(type)));
+    const long long groups = layer_back_groups(K, rows, d, (int)size_of(type));
     *bytes = groups == 1 ? 0 : (size_t)K * (size_t)groups * (size_t)(2 * d) * sizeof(float);
     return QSR_OK;
 }

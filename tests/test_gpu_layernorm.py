@@ -109,6 +109,16 @@ def test_backward(K, rows, d, dt):
             assert db is None
 
 
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("K,rows,d", [(6, 90, 1100), (1, 3, 1536), (2, 2, 1537), (1, 40, 2048), (1, 3, 2560), (1, 2, 2561), (5, 90, 4204), (1, 3, 5120), (1, 2, 5121),
+                                      (2, 3, 9001), (6, 50, 12288), (1, 2, 12289), (3, 701, 1003), (7, 1000, 64), (3, 500, 700)])
+def test_more_widths(K, rows, d, dt):
+    """Widths between the powers of two; rows enough for several to a workgroup, and workers that do not divide the chip."""
+    test_forward(K, rows, d, dt)
+    test_codes(K, rows, d, dt)
+    test_backward(K, rows, d, dt)
+
+
 @pytest.mark.parametrize("K,rows,d", [(1, 1, 5), (2, 3, 17)])
 def test_gradient_against_differences(K, rows, d):
     """Central differences, in 64 bits, of sum(y * dy) + sum(s * dres): truncation h^2 = 1e-10, cancellation 1e-16 / h = 1e-11,
