@@ -30,7 +30,7 @@
 namespace qsr {
 
 constexpr int STEPS = QSR_SCAN_STEPS;
-constexpr int WAVES = 8, MANY_WAVES = 16;      // wavefronts to a workgroup, where sequences are longer than one of them takes
+constexpr int WAVES = 8, MANY_WAVES = 16;      // wavefronts to a workgroup, where sequences have steps for as many
 
 struct ScanArgs {
     const void *x, *f, *dh;
@@ -570,25 +570,30 @@ __global__ __launch_bounds__(64 * W, 2) void scan_back_kernel(ScanArgs a)
 // ---------------------------------------------------------------------------------------------------
 // host
 // ---------------------------------------------------------------------------------------------------
-// Channels of a lane: four bytes of them, or one where a wavefront has them all, where workgroups are one to a compute unit then, without parts, and
-// where there are not as many with all tiles apart.  us with one / two, forward and backward: 300 x 500 steps of 64 channels 24.8 / 31.1 and 37.9 /
-// 49.6; 16 x 1024 of 1024 29.3 / 35.4 and 43.4 / 49.8, 13 x 1001 of 1003 27.3 / 37.9 and 43.3 / 53.2; 8 x 512 of 512 9.3 / 11.6 and 10.6 / 13.5; but
-// 24 x 700 of 1024 35.1 / 29.6 and 56.2 / 44.7, 8 x 1024 of 1024 24.0 / 19.4 and 32.3 / 26.7, 64 x 512 of 512 30.1 / 28.1 and 47.7 / 39.3.
+// Channels of a lane: four bytes of them, or one where a wavefront has them all, where there are not as many workgroups as compute units with all
+// tiles apart, and where enough workgroups take at most half as many rounds again with one, which are shorter.  us with one / two, forward and
+// backward: 300 x 500 steps of 64 channels 24.8 / 31.1 and 37.9 / 49.6; 8 x 512 of 512 9.3 / 11.6 and 10.6 / 13.5; rounds 1 and 1: 16 x 1024 of 1024
+// 29.3 / 35.4 and 43.4 / 49.8, 13 x 1001 of 1003 27.3 / 37.9 and 43.3 / 53.2, 64 x 1000 of 160 25.3 / 33.1 and 38.7 / 44.0; 2 and 2: 100 x 1000 of 320
+// 51.5 / 63.3 and 80.8 / 97.5; 3 and 2: 64 x 500 of 700 37.0 / 42.0 and 67.7 / 68.7; but 2 and 1: 24 x 700 of 1024 35.1 / 29.6 and 56.2 / 44.7; too few
+// workgroups: 8 x 1024 of 1024 24.0 / 19.4 and 32.3 / 26.7.
 static int scan_channels(int type, long long B, long long T, long long d)
 {
     if (type != QSR_TYPE_BF16 || d <= 64) return 1;
-    const long long ones = B * ((d + 63) / 64), tiles = ones * ((T + WAVES * STEPS - 1) / (WAVES * STEPS));
-    return T > 1 && ((ones > 192 && ones <= 256) || tiles <= 256) ? 1 : 2;
+    if (T < 2) return 2;
+    const long long ones = B * ((d + 63) / 64), twos = B * ((d + 127) / 128), tiles = ones * ((T + WAVES * STEPS - 1) / (WAVES * STEPS));
+    return tiles <= 256 || (twos >= 96 && 2 * ((ones + 255) / 256) <= 3 * ((twos + 255) / 256)) ? 1 : 2;
 }
 
 // A workgroup has all steps of 64 lanes' channels, or a part of them.  Parts cost a second read of two of three to five arrays and a
 // launch; they are taken where workgroups are too few otherwise.
 // What a trip of a workgroup costs, in tenths of its time: 10 without parts and 14 with them, a part's start 3, the second launch 8; the maps of the
 // parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them, bf16
-// and two channels of a lane, forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and 356 / 150; 32768 steps of 2048
-// 942 / 111, of 64 948 / 12.4 and 1513 / 14.1.  With 128 workgroups and more forward and 192 backward the second read costs what is won (16 x
+// and two channels of a lane, forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and 356 /
+// 150; 32768 steps of 2048 942 / 111, of 64 948 / 12.4 and 1513 / 14.1.  With 128 workgroups and more forward and 192 backward the second read costs what is won (16 x
 // 1024 steps of 1024, forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs up to 512 workgroups; from
-// there on eight are faster, 76 against 80 at 64 x 1024 steps of 1024).
+// there on eight are faster, 76 against 80 at 64 x 1024 steps of 1024).  Short sequences have no more wavefronts than they
+// can use, since a workgroup that waits for a place waits for idle ones too: us with / with eight or sixteen, bf16, 1000 x 30 steps of 512 23 / 48 and 38 /
+// 110, 40 x 30 of 1000 5.0 / 15.5 and 6.5 / 15.6, 40 x 100 of 1024 8.4 / 15.8 forward.
 struct ScanPlan { int channels, waves, parts, part_len; long long groups; };
 static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool back)
 {
@@ -597,7 +602,7 @@ static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool 
     p.groups = (d + 64 * V - 1) / (64 * V);
     p.parts = 1;
     const long long have = B * p.groups, slots = back ? 256 : 512, few = back ? 192 : 128;
-    p.waves = T <= STEPS ? 1 : !back && have >= few && have < 512 ? MANY_WAVES : WAVES;
+    p.waves = T <= STEPS ? 1 : T <= 2 * STEPS ? 2 : T <= 4 * STEPS ? 4 : T > WAVES * STEPS && !back && have >= few && have < 512 ? MANY_WAVES : WAVES;
     const long long trip = (long long)p.waves * STEPS, trips = (T + trip - 1) / trip;
     long long each = trips, best = 10 * trips;
     for (int round = 1; have < few && p.waves == WAVES && trips > 1 && round <= 4; ++round) {
@@ -615,12 +620,16 @@ template <typename T, int V, bool COMP, bool STREAM>
 static void launch_back(const ScanArgs &a, const ScanPlan &p, dim3 grid, hipStream_t s)
 {
     if (p.waves == 1) scan_back_kernel<T, V, 1, COMP, STREAM><<<grid, 64, 0, s>>>(a);
+    else if (p.waves == 2) scan_back_kernel<T, V, 2, COMP, STREAM><<<grid, 128, 0, s>>>(a);
+    else if (p.waves == 4) scan_back_kernel<T, V, 4, COMP, STREAM><<<grid, 256, 0, s>>>(a);
     else scan_back_kernel<T, V, WAVES, COMP, STREAM><<<grid, 64 * WAVES, 0, s>>>(a);
 }
 template <typename T, int V, bool COMP, bool STREAM>
 static void launch_forward(const ScanArgs &a, const ScanPlan &p, dim3 grid, hipStream_t s)
 {
     if (p.waves == 1) scan_kernel<T, V, 1, COMP, STREAM><<<grid, 64, 0, s>>>(a);
+    else if (p.waves == 2) scan_kernel<T, V, 2, COMP, STREAM><<<grid, 128, 0, s>>>(a);
+    else if (p.waves == 4) scan_kernel<T, V, 4, COMP, STREAM><<<grid, 256, 0, s>>>(a);
     else if (p.waves == WAVES) scan_kernel<T, V, WAVES, COMP, STREAM><<<grid, 64 * WAVES, 0, s>>>(a);
     else scan_kernel<T, V, MANY_WAVES, COMP, STREAM><<<grid, 64 * MANY_WAVES, 0, s>>>(a);
 }

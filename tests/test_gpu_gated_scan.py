@@ -165,9 +165,10 @@ def test_states_in_place_of_many_parts():
 
 @pytest.mark.parametrize("full", [False, True])
 @pytest.mark.parametrize("plain", [False, True])
-@pytest.mark.parametrize("B_,T,d", [(130, 16, 129), (90, 140, 130), (150, 290, 101), (100, 131, 333), (7, 2500, 700), (7, 2600, 641)])
+@pytest.mark.parametrize("B_,T,d", [(100, 16, 255), (100, 20, 253), (100, 64, 255), (90, 140, 130), (150, 290, 101), (300, 131, 251), (7, 2500, 700),
+                                    (7, 2600, 641)])
 def test_two_channels_of_a_lane(B_, T, d, plain, full):
-    """Enough workgroups for them: one, eight and sixteen wavefronts, parts; even and odd rows, in tensors of their own and inside others."""
+    """Enough workgroups for them: one to sixteen wavefronts, parts; even and odd rows, in tensors of their own and inside others."""
     s = _data(B_, T, d, torch.bfloat16, 18, full)
     marks = _marks(s, plain)
     f = qsr.gated_scan(s["x"], s["gate"], initial=s.get("initial"), keep=True, **marks)
@@ -185,6 +186,15 @@ def test_two_channels_of_a_lane(B_, T, d, plain, full):
     g = qsr.gated_scan(x, gate, initial=state, keep=True, state_out=state, **marks)
     again = qsr.gated_scan_backward(s["dh"], x, gate, g.states, last_grad=s.get("dlast"), **marks)
     assert all(torch.equal(p, q) for p, q in zip(f + tuple(back), g + tuple(again)))
+
+
+@pytest.mark.parametrize("full", [False, True])
+@pytest.mark.parametrize("dt", ["f32", "bf16"])
+@pytest.mark.parametrize("B_,T,d", [(6, 18, 5), (2, 31, 64), (3, 32, 131), (6, 33, 3), (70, 47, 65), (2, 64, 300), (5, 65, 70), (6, 128, 20)])
+def test_short_sequences(B_, T, d, dt, full):
+    """Two and four wavefronts to a workgroup, with and without steps for all of them."""
+    for plain in (False, True):
+        test_both_passes(B_, T, d, dt, plain, full)
 
 
 @pytest.mark.parametrize("dt,d,full", [("bf16", 3, True), ("f32", 65, False)])
