@@ -586,14 +586,15 @@ static int scan_channels(int type, long long B, long long T, long long d)
 
 // A workgroup has all steps of 64 lanes' channels, or a part of them.  Parts cost a second read of two of three to five arrays and a
 // launch; they are taken where workgroups are too few otherwise.
-// What a trip of a workgroup costs, in tenths of its time: 10 without parts and 14 with them, a part's start 3, the second launch 8; the maps of the
-// parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them, bf16
-// and two channels of a lane, forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and 356 /
-// 150; 32768 steps of 2048 942 / 111, of 64 948 / 12.4 and 1513 / 14.1.  With 128 workgroups and more forward and 192 backward the second read costs what is won (16 x
-// 1024 steps of 1024, forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs up to 512 workgroups; from
-// there on eight are faster, 76 against 80 at 64 x 1024 steps of 1024).  Short sequences have no more wavefronts than they
-// can use, since a workgroup that waits for a place waits for idle ones too: us with / with eight or sixteen, bf16, 1000 x 30 steps of 512 23 / 48 and 38 /
-// 110, 40 x 30 of 1000 5.0 / 15.5 and 6.5 / 15.6, 40 x 100 of 1024 8.4 / 15.8 forward.
+// What a trip of a workgroup costs, in tenths of its time: 10 without parts and 14 with them, a part's start 3, the second launch 8; the maps of
+// the parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them,
+// bf16 and two channels of a lane, forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and
+// 356 / 150; 32768 steps of 2048 942 / 111, of 64 948 / 12.4 and 1513 / 14.1.  With 128 workgroups and more forward and 192 backward the second
+// read costs what is won (16 x 1024 steps of 1024, forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs
+// up to 512 workgroups; from there on eight are faster, 76 against 80 at 64 x 1024 steps of 1024).  Short sequences have no more wavefronts than
+// they can use, since a workgroup that waits for a place waits for idle ones too: us with / with eight or sixteen, bf16, 1000 x 30 steps of 512 23
+// / 48 and 38 / 110, 40 x 30 of 1000 5.0 / 15.5 and 6.5 / 15.6, 40 x 100 of 1024 8.4 / 15.8 forward.  Sixteen that have all steps at once are
+// faster than parts, 7.1 against 7.8 for 4 x 250 of 1000; with two trips they are not, 11.2 against 9.4 for 512 of 4096.
 struct ScanPlan { int channels, waves, parts, part_len; long long groups; };
 static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool back)
 {
@@ -602,7 +603,8 @@ static ScanPlan scan_plan(long long B, long long T, long long d, int type, bool 
     p.groups = (d + 64 * V - 1) / (64 * V);
     p.parts = 1;
     const long long have = B * p.groups, slots = back ? 256 : 512, few = back ? 192 : 128;
-    p.waves = T <= STEPS ? 1 : T <= 2 * STEPS ? 2 : T <= 4 * STEPS ? 4 : T > WAVES * STEPS && !back && have >= few && have < 512 ? MANY_WAVES : WAVES;
+    const bool many = !back && T > WAVES * STEPS && have < 512 && (have >= few || T <= MANY_WAVES * STEPS);
+    p.waves = T <= STEPS ? 1 : T <= 2 * STEPS ? 2 : T <= 4 * STEPS ? 4 : many ? MANY_WAVES : WAVES;
     const long long trip = (long long)p.waves * STEPS, trips = (T + trip - 1) / trip;
     long long each = trips, best = 10 * trips;
     for (int round = 1; have < few && p.waves == WAVES && trips > 1 && round <= 4; ++round) {
