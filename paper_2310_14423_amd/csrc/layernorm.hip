@@ -10,7 +10,7 @@
 // mean is large beside their deviation keep it.  rstd is 0 where mean((s - mean)^2) + eps is 0 as a float.
 // Bound by memory: every row is read once and lies in the registers of its lanes until all passes over it are done, weight and bias are read once a
 // workgroup.  bf16, with residual and bias: 8 x 12608 rows of 768 100 us, 6.2 TB/s, their gradients 111 us, 5.6 TB/s, and 5 us for the sums of
-// weight's and bias'.  fp32, without either: 3 x 1001 rows of 1003 7 us, 3.4 TB/s, gradients 12.4 and 4.4.  Four rows of 2048 to e4m3: 3.2 us, latency.
+// weight's and bias'.  fp32, without either: 3 x 1001 rows of 1003 7 us, 3.4 TB/s, gradients 12.0 and 4.2.  Four rows of 2048 to e4m3: 3.2 us, latency.
 #include <cmath>
 
 #include "norm_rows.h"
