@@ -277,11 +277,12 @@ __global__ __launch_bounds__(SUM_THREADS) void layernorm_sums_kernel(const float
 template <typename T>
 static hipError_t launch_layer(const LayerArgs &a, int K, bool fp8, hipStream_t s)
 {
-    // a trip for each workgroup, but for the widest rows, whose weight and bias are as much as a row: two workgroups to a compute unit (2048
-    // rows of 16384 54 us, 59 with a trip each; narrower ones are 1 to 3 % faster with a trip each)
-    const long long wide = (512 + K - 1) / K;
+    // A trip for each workgroup, but for the widest rows, whose weight and bias are as much as a row: one workgroup to a compute unit, and none
+    // behind them (us with that / with two / with a trip each: 2048 rows of 16384 55.5 / 57.6 / 60.5, 5 x 1000 of 12000 82 / 83 / 95, and 100
+    // with one of each worker more than two make; fp32 with eight elements to a lane, 5 x 596 of 7488, 71 / 69 / 65)
+    const long long wide = 256 / K > 1 ? 256 / K : 1;
 #define LAYER_FWD(T, L, W, NV) do { const long long trips = fwd_groups(a.rows, rms_side<L, W>()); \
-    const dim3 grid((unsigned)(W > 8 && trips > wide ? wide : trips), (unsigned)K); \
+    const dim3 grid((unsigned)(W > 8 && NV * wide_of<T>() == 16 && trips > wide ? wide : trips), (unsigned)K); \
     if (fp8) layernorm_kernel<T, L, W, NV, true><<<grid, rms_threads<W>(), 0, s>>>(a); \
     else layernorm_kernel<T, L, W, NV, false><<<grid, rms_threads<W>(), 0, s>>>(a); } while (0)
     LAYER_BY_WIDTH(T, a.d, LAYER_FWD);
