@@ -290,8 +290,9 @@ static hipError_t launch_layer(const LayerArgs &a, int K, bool fp8, hipStream_t 
     return hipGetLastError();
 }
 
-// Workgroups of a worker in the backward pass: two wavefronts to each of the chip's SIMDs, four in the widest rows and five in narrow ones, and
-// not one more, where each has a place of its own and those behind it would wait for it to end (6 x 1915 rows of 4204 in bf16 63 us, 144 with
+// Workgroups of a worker in the backward pass: two wavefronts to each of the chip's SIMDs, four in the widest rows and in narrow ones of bf16,
+// which have little in flight (4 x 20000 rows of 200 30.9 us, with two 38.3, with five 36.5; in fp32 30000 of 250 29.1 with four, 26.7 with two),
+// and not one more, where each has a place of its own and those behind it would wait for it to end (6 x 1915 rows of 4204 in bf16 63 us, 144 with
 // 43 workgroups of a worker instead of 42; 5 x 596 of 7488 in fp32 76, 102 with 52 instead of 51).  Each leaves a row of partial sums, and has
 // more than one row where some 160 of them remain: 2 x 455 rows of 1600 in bf16 10.4, 12.2 with a row each; 1000 of 4096 18.3, 22.5; 8 x 1472 of
 // 205 9.8, 12.0; but 5 x 171 of 554 8.5 with two, 7.5.  One, whose sums are the gradients already, for the rows of a few tokens.
@@ -299,7 +300,7 @@ static long long layer_back_groups(int K, long long rows, long long d, int size)
 {
     const LayerPlan q = layer_plan(d, size);
     if (rows <= 2 * q.side) return 1;
-    const long long all = q.L < 64 ? 1280 : q.W == 2 ? 1024 : q.W <= 4 || (q.W == 5 && size == 4) ? 512 : 256;
+    const long long all = (q.L < 64 && size == 2) || q.W == 2 ? 1024 : q.W <= 4 || (q.W == 5 && size == 4) ? 512 : 256;
     const long long most = all / K > 1 ? all / K : 1, trips = (rows + q.side - 1) / q.side, few = q.W == 1 ? 2 : 4;
     const long long own = K * trips / 160, each = own < 1 ? 1 : own < few ? own : few, need = (trips + each - 1) / each;
     return most < need ? most : need;
