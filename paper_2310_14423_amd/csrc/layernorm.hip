@@ -6,8 +6,10 @@
 // and backward, from h as it is kept, with n = (h - mean) rstd, u = dy w and dres what comes down the residual stream:
 //   dx = rstd (u - mean(u) - n mean(u n)) + dres  (the gradient of x and of res)
 //   dw_k = sum over the worker's rows of dy n;  db_k = sum of dy
-// All arithmetic is fp32.  The deviation is taken from the row in the registers, about its mean, and not from a sum of squares: rows whose
-// mean is large beside their deviation keep it.  rstd is 0 where mean((s - mean)^2) + eps is 0 as a float.
+// All arithmetic is fp32.  The row in the registers is taken about the quotient of its sum, which roundings leave some steps of the floats beside
+// the mean; the mean of what remains puts that right, and the deviation is mean(t^2) - mean(t)^2 of the remainders t: rows whose mean is large
+// beside their deviation keep it, and rows of equal numbers have none, exactly (their remainders are whole steps j, j < 32, so that sums of j and
+// of j^2 over 16384 of them are exact too).  rstd is 0 where the deviation's square + eps is 0 as a float.
 // Bound by memory: every row is read once and lies in the registers of its lanes until all passes over it are done, weight and bias are read once a
 // workgroup.  bf16, with residual and bias: 8 x 12608 rows of 768 100 us, 6.2 TB/s, their gradients 111 us, 5.6 TB/s, and 5 us for the sums of
 // weight's and bias'.  fp32, without either: 3 x 1001 rows of 1003 7 us, 3.4 TB/s, gradients 12.0 and 4.2.  Four rows of 2048 to e4m3: 3.2 us, latency.
@@ -59,10 +61,28 @@ static LayerPlan layer_plan(long long d, int size)
         case 12: F(T, 64, 12, 16 / E_); break; \
         default: if ((d) <= 8192) F(T, 64, 16, 8 / E_); else F(T, 64, 16, 16 / E_); } } while (0)
 
+// Two sums over the lanes of a row with one barrier
+template <int L, int W>
+__device__ __forceinline__ void group_sums(float &p, float &q, float (*red)[2][W], int turn)
+{
+    if (W == 1) {
+        p = group_sum<L, 1>(p, nullptr, 0);
+        q = group_sum<L, 1>(q, nullptr, 0);
+        return;
+    }
+    p = wave_sum(p);
+    q = wave_sum(q);
+    if ((threadIdx.x & 63) == 0) { red[turn & 1][0][threadIdx.x >> 6] = p; red[turn & 1][1][threadIdx.x >> 6] = q; }
+    __syncthreads();
+    p = q = 0.f;
+#pragma unroll
+    for (int i = 0; i < W; ++i) { p += red[turn & 1][0][i]; q += red[turn & 1][1][i]; }
+}
+
 // `turn` counts the sums over a group of wavefronts, which take turns at their words
 template <typename T, int L, int W, int NV, bool FP8>
 __device__ __forceinline__ void layernorm_row(const LayerArgs &a, const RowPart<T, NV> &w, const RowPart<T, NV> &b, long long row, int lane,
-                                              float (*red)[W], int &turn)
+                                              float (*red)[W], float (*pair)[2][W], int &turn)
 {
     constexpr int E = wide_of<T>();
     Row<T, NV> x, res;
@@ -81,21 +101,27 @@ __device__ __forceinline__ void layernorm_row(const LayerArgs &a, const RowPart<
         q += lane + c * L * W < runs ? part : 0.f;
     }
     if (a.sum != nullptr) store_row<T, L, W, NV, false>((T *)a.sum + row * a.s_sum, lane, a.d, s);
-    const float mean = group_sum<L, W>(q, red, turn++) / (float)a.d;
-    each<T, NV>([&](float &y) { y -= mean; }, s);
+    const float near = group_sum<L, W>(q, red, turn++) / (float)a.d;
+    each<T, NV>([&](float &y) { y -= near; }, s);
+    float p = lane < rest ? s.t : 0.f;
     q = lane < rest ? s.t * s.t : 0.f;
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
-        float part = 0.f;
+        float part = 0.f, squares = 0.f;
 #pragma unroll
-        for (int u = 0; u < E; ++u) part = fmaf(s.v[c][u], s.v[c][u], part);
-        q += lane + c * L * W < runs ? part : 0.f;
+        for (int u = 0; u < E; ++u) { part += s.v[c][u]; squares = fmaf(s.v[c][u], s.v[c][u], squares); }
+        p += lane + c * L * W < runs ? part : 0.f;
+        q += lane + c * L * W < runs ? squares : 0.f;
     }
-    const float var = group_sum<L, W>(q, red, turn++) / (float)a.d + a.eps;
+    group_sums<L, W>(p, q, pair, turn++);
+    // where squares leave the range of floats, mean(t) is nothing beside them
+    const float off = q < INFINITY ? p / (float)a.d : 0.f;
+    float var = fmaf(-off, off, q / (float)a.d);
+    var = (var < 0.f ? 0.f : var) + a.eps;                                 // (a NaN stays)
     const float rstd = var == 0.f ? 0.f : 1.f / sqrtf(var);                // equal numbers without eps: the bias, and no gradient
-    if (lane == 0 && a.mean != nullptr) a.mean[row] = mean;
+    if (lane == 0 && a.mean != nullptr) a.mean[row] = near + off;
     if (lane == 0 && a.rstd != nullptr) a.rstd[row] = rstd;
-    each<T, NV>([&](float &y, float f, float g) { y = fmaf(y * rstd, f, g); }, s, w, b);
+    each<T, NV>([&](float &y, float f, float g) { y = fmaf((y - off) * rstd, f, g); }, s, w, b);
     if (!FP8) {
         store_row<T, L, W, NV, false>((T *)a.y + row * a.s_y, lane, a.d, s);
         return;
@@ -115,7 +141,7 @@ __device__ __forceinline__ void layernorm_row(const LayerArgs &a, const RowPart<
 template <typename T, int L, int W, int NV, bool FP8>
 __global__ __launch_bounds__(rms_threads<W>()) void layernorm_kernel(LayerArgs a)
 {
-    __shared__ float red[2][W];
+    __shared__ float red[2][W], pair[2][2][W];
     constexpr int side = rms_side<L, W>();
     const int k = blockIdx.y, lane = rms_lane<L, W>(), place = rms_place<L, W>();
     int turn = 0;
@@ -124,7 +150,7 @@ __global__ __launch_bounds__(rms_threads<W>()) void layernorm_kernel(LayerArgs a
     if (a.b != nullptr) load_words<T, L, W, NV>(a.b + k * a.s_b, lane, a.d, b);
     else each<T, NV>([](float &x) { x = 0.f; }, b);
     for (long long r = (long long)blockIdx.x * side + place; r < a.rows; r += (long long)gridDim.x * side)
-        layernorm_row<T, L, W, NV, FP8>(a, w, b, k * a.rows + r, lane, red, turn);
+        layernorm_row<T, L, W, NV, FP8>(a, w, b, k * a.rows + r, lane, red, pair, turn);
 }
 
 struct LayerBackArgs {
@@ -136,24 +162,6 @@ struct LayerBackArgs {
     long long rows, s_part, s_dy, s_h, s_dres, s_dx, s_w;
     int d;
 };
-
-// Two sums over the lanes of a row with one barrier
-template <int L, int W>
-__device__ __forceinline__ void group_sums(float &p, float &q, float (*red)[2][W], int turn)
-{
-    if (W == 1) {
-        p = group_sum<L, 1>(p, nullptr, 0);
-        q = group_sum<L, 1>(q, nullptr, 0);
-        return;
-    }
-    p = wave_sum(p);
-    q = wave_sum(q);
-    if ((threadIdx.x & 63) == 0) { red[turn & 1][0][threadIdx.x >> 6] = p; red[turn & 1][1][threadIdx.x >> 6] = q; }
-    __syncthreads();
-    p = q = 0.f;
-#pragma unroll
-    for (int i = 0; i < W; ++i) { p += red[turn & 1][0][i]; q += red[turn & 1][1][i]; }
-}
 
 // A workgroup takes every gridDim.x-th row (W == 1: four of them at a time) and keeps its parts of the gradients of weight and bias in
 // registers.  There are two wavefronts to a SIMD at most (three and four in the widest rows), so that each may have half of its registers: with a quarter
