@@ -377,7 +377,8 @@ int qsr_rmsnorm_backward(const qsr_rmsnorm_backward_args *args, void *workspace,
  * bias, sum, mean, rstd and y_type as in qsr_rmsnorm: bias may be NULL (none), sum is s in the rows' type (may be x or residual itself)
  * or NULL, mean and rstd are [K * rows] floats or NULL, y_type is the rows' type, or QSR_TYPE_E4M3 with scale [K * rows], scale = max|y| / 448 of
  * the row's finite entries.  Where mean((s - mean)^2) + eps is 0 as a float (a row of equal numbers, with eps = 0) rstd is 0, y is
- * the bias and the row has no gradient; where it is infinite rstd is 0 too.  A row with a NaN or an infinity has NaN for all of y.
+ * the bias and the row has no gradient; where it is infinite rstd is 0 too.  A row with a NaN or an infinity has NaN for all of y; a finite
+ * number that is further than the largest float from its row's mean has NaN for y, and its row's gradients are NaN.
  * QSR_ELIMIT above d = 16384. */
 typedef struct {
     int32_t K, type, y_type;

@@ -92,16 +92,18 @@ __device__ __forceinline__ void layernorm_row(const LayerArgs &a, const RowPart<
     each<T, NV>([](float &y, float v) { y = v; }, s, x);
     if (a.res != nullptr) each<T, NV>([](float &y, float v) { y += v; }, s, res);
     const int runs = a.d / E, rest = a.d - runs * E;
-    float q = lane < rest ? s.t : 0.f;
+    // (sums leave the range of floats where their mean does not: by a power of two, whose roundings, of tiny numbers, the second sum puts right)
+    constexpr float DOWN = 1.f / 65536.f, UP = 65536.f;
+    float q = lane < rest ? s.t * DOWN : 0.f;
 #pragma unroll
     for (int c = 0; c < NV; ++c) {
         float part = 0.f;
 #pragma unroll
-        for (int u = 0; u < E; ++u) part += s.v[c][u];
+        for (int u = 0; u < E; ++u) part = fmaf(s.v[c][u], DOWN, part);
         q += lane + c * L * W < runs ? part : 0.f;
     }
     if (a.sum != nullptr) store_row<T, L, W, NV, false>((T *)a.sum + row * a.s_sum, lane, a.d, s);
-    const float near = group_sum<L, W>(q, red, turn++) / (float)a.d;
+    const float near = group_sum<L, W>(q, red, turn++) / (float)a.d * UP;
     each<T, NV>([&](float &y) { y -= near; }, s);
     float p = lane < rest ? s.t : 0.f;
     q = lane < rest ? s.t * s.t : 0.f;
