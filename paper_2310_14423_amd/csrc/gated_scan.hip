@@ -320,7 +320,7 @@ __global__ __launch_bounds__(64 * W, 4) void scan_kernel(ScanArgs a)
     if (a.last != nullptr && q.part == a.parts - 1 && wave == 0) q.store_floats(a.last + (long long)q.b * a.d, carry);
 }
 
-// One step of every sequence: a thread has V channels of one
+// One step of every sequence: a thread has V channels of one.  Of a sequence without steps x and gate are not read, as with more steps.
 template <typename T, int V, bool COMP>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
 {
@@ -329,12 +329,15 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
     const long long b = id / each;
     const int first = (int)(id - b * each) * V, at = min(first, a.d - V), skip = first - at;
     typedef typename Wide<T, V>::vec Vec;
-    const Vec x = *(const Vec *)((const char *)a.x + b * a.b_x + at * (long long)sizeof(T));
-    const Vec f = *(const Vec *)((const char *)a.f + b * a.b_f + at * (long long)sizeof(T));
+    const bool live = a.lengths == nullptr || a.lengths[b] > 0, cut = a.reset != nullptr && a.reset[b] != 0;
+    Vec x = (Vec)((T)0.f), f = x;
+    if (live) {
+        x = *(const Vec *)((const char *)a.x + b * a.b_x + at * (long long)sizeof(T));
+        f = *(const Vec *)((const char *)a.f + b * a.b_f + at * (long long)sizeof(T));
+    }
     float h[V], y[V];
 #pragma unroll
     for (int u = 0; u < V; ++u) h[u] = a.initial != nullptr ? a.initial[b * a.d + at + u] : 0.f;
-    const bool live = a.lengths == nullptr || a.lengths[b] > 0, cut = a.reset != nullptr && a.reset[b] != 0;
     T *const to = (T *)((char *)a.h + b * a.b_h) + at;
 #pragma unroll
     for (int u = 0; u < V; ++u) {
