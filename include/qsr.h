@@ -409,7 +409,8 @@ int qsr_layernorm_workspace_bytes(int32_t K, int64_t rows, int64_t d, int32_t ty
 int qsr_layernorm_backward(const qsr_layernorm_backward_args *args, void *workspace, size_t workspace_bytes, void *stream);
 
 /* Rows of K workers' tables by tokens: y_i = scale * table_k[token_i], worker k's tokens being k * tokens_each .. (k + 1) * tokens_each - 1.
- * A token outside 0..vocab-1 stands for none: a row of zeros.  type: the table's, y_type: either of QSR_TYPE_F32 and QSR_TYPE_BF16.
+ * A token outside 0..vocab-1 stands for none: a row of zeros.  type: the table's, y_type: either of QSR_TYPE_F32 and QSR_TYPE_BF16.  y shares no
+ * memory with table and tokens.
  * QSR_ELIMIT above 2^27 tokens of a worker. */
 typedef struct {
     int32_t K, type, y_type, reserved;
@@ -424,7 +425,8 @@ int qsr_embedding(const qsr_embedding_args *args, void *stream);
 
 /* Its gradient: grad_k[v] = scale * sum of y_grad_i over the worker's tokens v, all of the table (0 for rows that no token names), or,
  * with accumulate = 1, added to what grad holds in the rows that tokens name, the others left as they are.  Sums are floats in a fixed
- * order, rounded once to grad_type.  type: y_grad's.  The workspace is 16-byte aligned. */
+ * order, rounded once to grad_type.  type: y_grad's.  grad shares no memory with y_grad and tokens (QSR_EINVAL).  The workspace is 16-byte
+ * aligned. */
 typedef struct {
     int32_t K, type, grad_type, accumulate;
     int64_t tokens_each, vocab, d;

@@ -769,6 +769,26 @@ static int run_elements(int type, int64_t d)
     return d < E ? 1 : E;
 }
 
+// Whether n rows of `len` bytes, `stride` apart from `at` on, share memory with K tables of V rows of `row` bytes, `step` apart, `worker` from
+// table to table.  Rows between the table's, as far apart as those, share none; others that begin and end within a table are taken to.
+static bool shares(const void *at, int64_t n, int64_t stride, int64_t len, const void *table, int K, int64_t worker, int64_t V, int64_t step, int64_t row)
+{
+    typedef __int128 Wide;                     // (strides are whatever the caller gave)
+    const Wide p = (Wide)(uintptr_t)at, t = (Wide)(uintptr_t)table, extent = (Wide)(V - 1) * step + row;
+    if (n == 1) stride = step;
+    auto apart = [&](Wide from, Wide to) { return p >= to || p + (Wide)(n - 1) * stride + len <= from; };
+    if (apart(t, t + (Wide)(K - 1) * worker + extent)) return false;
+    for (int k = 0; k < K; ++k) {
+        const Wide from = t + (Wide)k * worker, to = from + extent;
+        if (apart(from, to)) continue;
+        const Wide i = p + len > from ? 0 : (from - p - len) / stride + 1;                 // the first row that ends behind `from`
+        if (i >= n || p + i * stride >= to) continue;
+        const Wide within = ((p - from) % step + step) % step;
+        if (stride != step || within < row || within + len > step) return true;
+    }
+    return false;
+}
+
 extern "C" int qsr_embedding(const qsr_embedding_args *q, void *stream)
 {
     if (!q || !sizes_ok(q->K, q->tokens_each, q->vocab, q->d) || !is_type(q->type) || !is_type(q->y_type)) return QSR_EINVAL;
@@ -807,6 +827,12 @@ extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void
     if (rc != QSR_OK) return rc;
     if (need > 0 && (!workspace || off(workspace, 16))) return QSR_EINVAL;
     if (workspace_bytes < need) return QSR_ENOMEM;
+    // rows of the table are cleared or written before all of y_grad and tokens has been read
+    const int64_t es = (int64_t)size_of(q->type), gs = (int64_t)size_of(q->grad_type), far = q->K > 1 ? q->worker_stride : 0;
+    if (q->tokens_each > 0 && (shares(q->y_grad, q->K * q->tokens_each, q->y_grad_stride * es, q->d * es, q->grad, q->K, far * gs, q->vocab, q->grad_stride * gs,
+                                      q->d * gs) ||
+                               shares(q->tokens, 1, 8, q->K * q->tokens_each * 8, q->grad, q->K, far * gs, q->vocab, q->grad_stride * gs, q->d * gs)))
+        return QSR_EINVAL;
     const hipStream_t s = (hipStream_t)stream;
     const int K = q->K, E = run_elements(q->type, q->d);
     const long long N = q->tokens_each;

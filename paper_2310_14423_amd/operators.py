@@ -164,8 +164,8 @@ def embedding(tokens, table, scale=1.0, out="same", stream=None):
 def embedding_backward(y_grad, tokens, table, scale=1.0, out=None, accumulate=False, stream=None):
     """The gradient of embedding's table for y_grad (float32 or bfloat16, rows of any even stride): scale times the sum of the rows of
     y_grad of each token, zero for the others, shaped and typed as table, of which nothing else is used.  out: a tensor for it, float32 or
-    bfloat16.  accumulate: it is added to what `out` holds (a table that the head shares, several batches); rows that no token names are
-    left alone.  Sums are in a fixed order."""
+    bfloat16, that shares no memory with y_grad and tokens (QSRError).  accumulate: it is added to what `out` holds (a table that the head
+    shares, several batches); rows that no token names are left alone.  Sums are in a fixed order."""
     if _calls is None:
         _setup()
     s, place = _place(table, stream)
