@@ -759,6 +759,9 @@ extern "C" int qsr_gated_scan(const qsr_gated_scan_args *q, void *workspace, siz
     if (rc != QSR_OK) return rc;
     if (need > 0 && (!workspace || off(workspace, 8))) return QSR_EINVAL;
     if (workspace_bytes < need) return QSR_ENOMEM;
+    // a workgroup may write its part of `last` before another one has read the same place as another channel's or sequence's initial state
+    const uintptr_t first = (uintptr_t)q->initial, last = (uintptr_t)q->last, apart = first < last ? last - first : first - last;
+    if (first != 0 && last != 0 && apart != 0 && apart < (uintptr_t)q->batch * (uintptr_t)q->d * 4) return QSR_EINVAL;
     ScanArgs a{};
     a.x = q->x; a.f = q->gate; a.h = q->h;
     a.initial = q->initial; a.last = q->last; a.states = q->states;

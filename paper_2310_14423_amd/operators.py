@@ -190,7 +190,7 @@ def gated_scan(x, gate, initial=None, reset=None, lengths=None, input="complemen
       reset      [..., T] bool: steps that take no state from before them (documents that are packed into one sequence)
       lengths    [...] int64: steps that there are; what is behind them is not read, h is 0 there
       keep       return `states` for the backward pass
-      state_out  a float32 tensor [..., d] for `last`, which may be initial
+      state_out  a float32 tensor [..., d] for `last`, which may be initial, and shares no memory with the arguments otherwise
     Returns (h, last, states): h in x's type, last [..., d] the states behind the sequences' ends, from which the next steps go on (one
     token at a time: T = 1), states or None."""
     if _calls is None:

@@ -33,3 +33,19 @@ def test_workers_with_a_token_each():
     want = qsr.embedding_backward(dy.clone(), tok, out.clone())
     qsr.embedding_backward(dy, tok, out, out=out)
     assert torch.equal(out, want)
+
+
+@pytest.mark.parametrize("T", [1, 40, 5000])
+def test_states_beside_the_initial_ones(T):
+    """In one buffer: side by side, the same, and one sequence on (refused)."""
+    g = torch.Generator().manual_seed(3)
+    x, f, states = torch.randn(3, T, 33, generator=g).cuda(), torch.randn(3, T, 33, generator=g).cuda(), torch.randn(6, 33, generator=g).cuda()
+    want = qsr.gated_scan(x, f, initial=states[:3].clone())
+    before = states.clone()
+    for out in (states[1:4], states[2:5]):
+        with pytest.raises(qsr.QSRError) as e:
+            qsr.gated_scan(x, f, initial=states[:3], state_out=out)
+        assert e.value.code == -1 and torch.equal(states, before)
+    for out in (states[3:], states[:3]):
+        got = qsr.gated_scan(x, f, initial=states[:3], state_out=out)
+        assert got.last is out and torch.equal(out, want.last) and torch.equal(got.h, want.h)

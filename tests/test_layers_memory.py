@@ -27,3 +27,11 @@ def test_gradient_of_a_table(over):
     a.update(over)
     a = abi.EmbeddingBackwardArgs(**a)
     assert qsr.lib().qsr_embedding_backward(C.byref(a), C.c_void_p(P << 6), C.c_size_t(1 << 40), None) == -1
+
+
+@pytest.mark.parametrize("last", [P + 4, P - 4, P + 4 * 10, P - 4 * 29, P + 4 * 29])
+@pytest.mark.parametrize("steps", [1, 20, 5000])
+def test_states_that_are_partly_the_initial_ones(last, steps):
+    a = abi.GatedScanArgs(type=0, input=0, batch=3, steps=steps, d=10, x=P << 4, gate=P << 5, h=P << 6, initial=P, last=last, x_stride=30, gate_stride=30, h_stride=30,
+                          x_batch_stride=10, gate_batch_stride=10, h_batch_stride=10)
+    assert qsr.lib().qsr_gated_scan(C.byref(a), C.c_void_p(P << 7), C.c_size_t(1 << 40), None) == -1
