@@ -155,6 +155,14 @@ __device__ __forceinline__ void sums_before(int *counts, int *waves)
     __syncthreads();
 }
 
+// What a wavefront's lanes have read and written in LDS stays before what they read and write behind this: LDS takes a wavefront's accesses in
+// their order, so that the compiler alone has to keep to it, and no instruction is needed
+__device__ __forceinline__ void wave_in_order()
+{
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+}
+
 // A wavefront's next EACH * 64 keys, of which `left` are there: each one's place among those of its digit, from `count` on, which goes on.
 // (No atomics: the keys of frequent tokens would wait for each other.)
 template <int EACH>
@@ -170,9 +178,9 @@ __device__ __forceinline__ void rank_keys(const uint32_t (&key)[EACH], int left,
         same_digit(digit, in, bits, before, all);
         const int here = count[digit];
         rank[i] = here + before;
-        __builtin_amdgcn_wave_barrier();
+        wave_in_order();
         if (in && before == 0) count[digit] = here + all;
-        __builtin_amdgcn_wave_barrier();
+        wave_in_order();
     }
 }
 
@@ -562,9 +570,9 @@ __global__ __launch_bounds__(EMBED_THREADS) void embedding_direct_kernel(DirectA
         same_digit(row, in, 6, before, all);
         const int at = to[wave][row];
         if (in) list[at + before] = entry;
-        __builtin_amdgcn_wave_barrier();
+        wave_in_order();
         if (in && before == 0) to[wave][row] = at + all;
-        __builtin_amdgcn_wave_barrier();
+        wave_in_order();
     }
     __syncthreads();
     const int groups = EMBED_THREADS / a.lanes, group = tid / a.lanes, place = tid & (a.lanes - 1), M = start[64], each = (M + groups - 1) / groups;

@@ -24,3 +24,15 @@ def test_sequences_without_steps_are_not_read():
     rows = source[source.index("void load_rows("):source.index("// A lane's place:")]
     assert rows.count("load_word<T, V>(") == 2 and "if (n >= STEPS) {" in rows and "if (s < n) w[s] = load_word<T, V>(" in rows
     assert source.count("load_word<T, V>(") == 2
+
+
+def test_lanes_that_exchange_words_keep_their_order_by_a_fence():
+    """Words in LDS that one lane of a wavefront writes and another reads, without a barrier of the workgroup: the order is kept by a fence
+    of the wavefront, since a wave barrier by itself says nothing about memory."""
+    source = open(os.path.join(CSRC, "embedding.hip")).read()
+    barriers = re.findall(r"^.*\n.*__builtin_amdgcn_wave_barrier\(\);", source, re.M)
+    assert barriers and all('__builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");' in b for b in barriers)
+    for kernel in ("rank_keys", "embedding_direct_kernel"):
+        text = _kernel(source, kernel)
+        # read, fence, written, fence
+        assert re.search(r"= (count\[digit\]|to\[wave\]\[row\]);.*?wave_in_order\(\);\s+if \(in && before == 0\) .*?;\s+wave_in_order\(\);", text, re.S)
