@@ -353,7 +353,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanArgs a)
 }
 
 // The maps of parts: a wavefront goes through a run of its part's steps, from its end.  Forward: all parts but the last, and the initial
-// state.  Backward: e before a part from e behind it, all parts but the first.
+// state.  Backward: e before a part from e behind it, all parts but the first; COMP makes no difference.
 template <typename T, int V, bool COMP, bool BACK>
 __global__ __launch_bounds__(64 * WAVES) void scan_maps_kernel(ScanArgs a)
 {
@@ -663,7 +663,7 @@ static hipError_t launch_scan(ScanArgs &a, const ScanPlan &p, long long B, bool 
         a.near = !(lines(a.f, a.b_f, a.s_f) && (back ? lines(a.dh, a.b_dh, a.s_dh) : lines(a.x, a.b_x, a.s_x)));
         const TileGrid g = tile_grid((a.tiles + 7) / 8 * 8, 64 * WAVES);
         if (g.x == 0) return hipErrorInvalidConfiguration;
-        if (back) scan_maps_kernel<T, V, COMP, true><<<dim3(g.x, g.y), 64 * WAVES, 0, s>>>(a);
+        if (back) scan_maps_kernel<T, V, false, true><<<dim3(g.x, g.y), 64 * WAVES, 0, s>>>(a);
         else scan_maps_kernel<T, V, COMP, false><<<dim3(g.x, g.y), 64 * WAVES, 0, s>>>(a);
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;

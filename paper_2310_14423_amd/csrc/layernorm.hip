@@ -49,17 +49,18 @@ static LayerPlan layer_plan(long long d, int size)
     q.side = q.W == 1 ? 256 / q.L : 1;
     return q;
 }
+// F(T, L, W, NV) for it; what no width of a type has is not built
 #define LAYER_BY_WIDTH(T, d, F) do { constexpr int E_ = wide_of<T>(), N_ = sizeof(T) == 2 ? 16 / E_ : 8 / E_; \
     if ((d) < E_) F(T, 16, 1, 0); else if ((d) <= 128) F(T, 16, 1, 8 / E_); else if ((d) <= 256) F(T, 32, 1, 8 / E_); \
     else if ((d) <= 512) F(T, 64, 1, 8 / E_); \
     else switch (layer_plan(d, (int)sizeof(T)).W) { \
-        case 1: F(T, 64, 1, 16 / E_); break; \
+        case 1: if constexpr (sizeof(T) == 2) F(T, 64, 1, 16 / E_); break; \
         case 2: F(T, 64, 2, N_); break; \
-        case 4: if ((d) <= 2048) F(T, 64, 4, 8 / E_); else F(T, 64, 4, 16 / E_); break; \
+        case 4: if constexpr (sizeof(T) == 2) { if ((d) > 2048) { F(T, 64, 4, 16 / E_); break; } } F(T, 64, 4, 8 / E_); break; \
         case 5: F(T, 64, 5, N_); break; \
         case 8: F(T, 64, 8, N_); break; \
-        case 12: F(T, 64, 12, 16 / E_); break; \
-        default: if ((d) <= 8192) F(T, 64, 16, 8 / E_); else F(T, 64, 16, 16 / E_); } } while (0)
+        case 12: if constexpr (sizeof(T) == 2) F(T, 64, 12, 16 / E_); break; \
+        default: if constexpr (sizeof(T) == 4) { if ((d) <= 8192) { F(T, 64, 16, 8 / E_); break; } } F(T, 64, 16, 16 / E_); } } while (0)
 
 // Two sums over the lanes of a row with one barrier
 template <int L, int W>
