@@ -443,9 +443,9 @@ int qsr_embedding_backward(const qsr_embedding_backward_args *args, void *worksp
  *   h_t = a_t * h_{t-1} + (1 - a_t) * x_t (QSR_SCAN_COMPLEMENT), or a_t * h_{t-1} + x_t (QSR_SCAN_PLAIN);  h_{-1} = initial
  * State and arithmetic are float; h is the state in x's type.  initial: [batch][d] floats, or NULL (0).  last: [batch][d], the state behind a
  * sequence's last step, or NULL; may be initial itself, but share no part of its memory otherwise (QSR_EINVAL), and none of other arguments'.
- * A step with a nonzero reset takes no state from before it.  lengths: steps of a sequence that
- * there are (less than 0 is none, more than `steps` is all); x and gate behind them are not read, h behind them is 0, last is the
- * state at the end.  states: [batch][ceil(steps / QSR_SCAN_STEPS)][d] floats for the backward pass, the state that every
+ * A step with a nonzero reset takes no state from before it; without one a channel is not finite behind an infinity or a NaN.  lengths: steps
+ * of a sequence that there are (less than 0 is none, more than `steps` is all); x and gate behind them are not read, h behind them is 0,
+ * last is the state at the end.  states: [batch][ceil(steps / QSR_SCAN_STEPS)][d] floats for the backward pass, the state that every
  * QSR_SCAN_STEPS-th step begins with, or NULL.  reset, lengths: without gaps.  The rows of h share no element, with each other or with
  * x and gate.  QSR_ELIMIT above 2^30 steps, 2^28 channels, or 2^24 elements from step to step. */
 enum { QSR_SCAN_STEPS = 16 };

@@ -8,17 +8,20 @@
 // STEPS steps of 64 lanes' channels into its registers, finds their map, learns from the maps of the wavefronts before it, through LDS, what
 // state its own steps begin with, and goes through them once more: x and f are read from memory once.  Where sequences and channels
 // give too few workgroups, sequences are cut into parts, whose maps a launch before finds, for which x and f are read a second time.
-// Backward, h is not read but made again from the states kept at every STEPS-th step in fp32: 1/4 or 1/8 of the reads of h, and
+// Backward, h is not read but made again from the states kept at every STEPS-th step in fp32: 1/8 of the reads of h in bf16, 1/16 in fp32, and
 // nothing of h's rounding in the gradients.
 // A reset cuts a map off from what was before: A = -1 stands for that (A is never negative), so that an infinity or a NaN ends there too.
+// Without one a channel that has met an infinity stays infinite or becomes NaN (a map whose A is too small for a float makes NaN of it).
 // All arithmetic is fp32.
 // Rows are addressed as buffers (what is the same for a wavefront stays in scalar registers: forward a fifth fewer vector instructions than with
 // pointers, 85 -> 76 us below).  Bound by memory at 64 x 1024 steps of 1024 in bf16: forward 74 us, 5.7 TB/s, backward 150 us, 4.6 TB/s with one
 // workgroup of eight wavefronts to a compute unit (190 registers a lane; at 128 they go to memory and back, 230 us).  32768 steps of 2048 on
 // 512 workgroups: maps 44 us, 6.0 TB/s, and 65 us; 2 x 16384 of 768 19 + 33 us, backward 18 + 49.  fp32, 13 sequences of up to 1001
-// steps of 1003: 26 and 38 us, the time of the longest one.  Four single steps of 2048: 3 us, latency.
-// What the second read costs could be saved by workgroups that wait for each other's maps while they hold their steps in registers: forward
-// that leaves two of them to a compute unit, each idle for the way of a map through memory; backward one.
+// steps of 1003: 26 and 38 us, from memory 37 and 49, the time of the longest one: all of 1001 steps take 41 and 52, with 1024 channels, whose
+// rows are whole lines, 35 and 49 (208 workgroups, one to a compute unit, whose tiles follow each other).  Four single steps of 2048: 3 us, latency.
+// What the second read costs could be saved by workgroups that wait for each other's maps while they hold their steps in registers; that
+// was not tried.  Thirds and quarters of the sequence at a time, so that the second read is from the last-level cache, are slower than the
+// whole (32768 steps of 2048 131 us, 141 and 152).
 #include <cmath>
 #include <initializer_list>
 #include <type_traits>
@@ -590,7 +593,8 @@ static int scan_channels(int type, long long B, long long T, long long d)
 // A workgroup has all steps of 64 lanes' channels, or a part of them.  Parts cost a second read of two of three to five arrays and a
 // launch; they are taken where workgroups are too few otherwise.
 // What a trip of a workgroup costs, in tenths of its time: 10 without parts and 14 with them, a part's start 3, the second launch 8; the maps of
-// the parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward.  us without parts / with them,
+// the parts before, which each part joins, count a little.  Workgroups run 512 at a time forward and 256 backward with two channels a lane; with
+// one, more of them fit (56 registers of a lane forward, 128 backward in "plain"), which the rule does not count.  us without parts / with them,
 // bf16 and two channels of a lane, forward and backward: 8 x 512 steps of 512 channels 17.0 / 12.5 and 26.5 / 14.9; 9 x 7000 of 700 243 / 100 and
 // 356 / 150; 32768 steps of 2048 942 / 111, of 64 948 / 12.4 and 1513 / 14.1.  With 128 workgroups and more forward and 192 backward the second
 // read costs what is won (16 x 1024 steps of 1024, forward: 37 with parts, 32.3 with sixteen wavefronts to a workgroup, which fill the chip's SIMDs

@@ -12,7 +12,9 @@
 // of j^2 over 16384 of them are exact too).  rstd is 0 where the deviation's square + eps is 0 as a float.
 // Bound by memory: every row is read once and lies in the registers of its lanes until all passes over it are done, weight and bias are read once a
 // workgroup.  bf16, with residual and bias: 8 x 12608 rows of 768 100 us, 6.2 TB/s, their gradients 111 us, 5.6 TB/s, and 5 us for the sums of
-// weight's and bias'.  fp32, without either: 3 x 1001 rows of 1003 7 us, 3.4 TB/s, gradients 12.0 and 4.2.  Four rows of 2048 to e4m3: 3.2 us, latency.
+// weight's and bias'.  fp32, without either: 3 x 1001 rows of 1003 7.3 us, 3.3 TB/s, gradients 12.2 and 3.9.  To e4m3, from bf16 with residual and
+// bias: four rows of 2048 3.3 us, latency; 8192 of 4096 46 us, 5.1 TB/s; 8 x 8192 of 768 65 us, 5.4 TB/s.  2048 rows of 16384 with residual and
+// bias: bf16 51 us, 5.3 TB/s, fp32 91 us, 5.9 TB/s; their gradients 83 us, 3.2 TB/s, and 162 us, 3.3 TB/s, at the limit of a lane's registers.
 #include <cmath>
 
 #include "norm_rows.h"
@@ -166,10 +168,11 @@ struct LayerBackArgs {
     int d;
 };
 
-// A workgroup takes every gridDim.x-th row (W == 1: four of them at a time) and keeps its parts of the gradients of weight and bias in
-// registers.  There are two wavefronts to a SIMD at most (three and four in the widest rows), so that each may have half of its registers: with a quarter
+// A workgroup takes every gridDim.x-th row (W == 1: 256 / L of them at a time) and keeps its parts of the gradients of weight and bias in
+// registers.  A wavefront may have half of a SIMD's registers (a third and a quarter with twelve and sixteen wavefronts): with a quarter
 // the sixteen elements of bf16 rows go to memory and back, 8 x 12608 rows of 768 130 us instead of 116, 8192 rows of 4096 74 instead of
-// 56.  The next row's loads are under way while a row is worked on where that takes few registers, and where a workgroup of five to
+// 56.  With sixteen wavefronts some do: above 12288 columns in bf16 24 bytes of a lane, 100 with a bias, above 8192 in fp32 104 and 172
+// (2048 rows of 9001 with a bias 124 us, 2.4 TB/s).  The next row's loads are under way while a row is worked on where that takes few registers, and where a workgroup of five to
 // eight wavefronts is alone on its compute unit (4096 rows of 8192 54 us, 60 without; 6 x 1915 of 4204 64, 88 without).
 template <typename T, int L, int W, int NV, bool BIAS>
 __global__ __launch_bounds__(rms_threads<W>(), W > 8 ? (W + 3) / 4 : 2) void layernorm_back_kernel(LayerBackArgs a)
@@ -301,7 +304,7 @@ static hipError_t launch_layer(const LayerArgs &a, int K, bool fp8, hipStream_t 
     return hipGetLastError();
 }
 
-// Workgroups of a worker in the backward pass: two wavefronts to each of the chip's SIMDs, four in the widest rows and in narrow ones of bf16,
+// Workgroups of a worker in the backward pass, one at least: two wavefronts to each of the chip's SIMDs, four in the widest rows and in narrow ones of bf16,
 // which have little in flight (4 x 20000 rows of 200 30.9 us, with two 38.3, with five 36.5; in fp32 30000 of 250 29.1 with four, 26.7 with two),
 // and not one more, where each has a place of its own and those behind it would wait for it to end (6 x 1915 rows of 4204 in bf16 63 us, 144 with
 // 43 workgroups of a worker instead of 42; 5 x 596 of 7488 in fp32 76, 102 with 52 instead of 51).  Each leaves a row of partial sums, and has

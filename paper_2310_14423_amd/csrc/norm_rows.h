@@ -186,8 +186,8 @@ static RmsPlan rms_plan(long long d, int size)
 // F(T, L, W, NV) for it: sixteen elements to a lane in bf16 where the row is long enough, eight in fp32 (a third row in the backward
 // pass would not fit the registers).  us with eight in bf16: 16384 rows of 4096 to e4m3 88 (77.7), 8 x 12608 rows of 768 forward and
 // backward 229 (207); with sixteen in fp32, backward: 8192 rows of 4096 106 (94), 4 x 4854 rows of 611 52 (46).  At its limit of 128
-// registers the backward pass keeps 5 or 6 of them in memory with sixteen in bf16, and 18 in fp32 above 8192, where a workgroup of 1024
-// lanes leaves no other choice: 4096 rows of 16384 take 192 us, 5.6 TB/s, and of 8192 93, 5.8.
+// registers the backward pass of the root-mean-square norm keeps 5 or 6 of them in memory with sixteen in bf16, and 18 in fp32 above 8192,
+// where a workgroup of 1024 lanes leaves no other choice: 4096 rows of 16384 take 192 us, 5.6 TB/s, and of 8192 93, 5.8.
 #define RMS_BY_WIDTH(T, d, F) do { constexpr int E_ = wide_of<T>(); \
     if ((d) < E_) F(T, 16, 1, 0); else if ((d) <= 128) F(T, 16, 1, 8 / E_); else if ((d) <= 256) F(T, 32, 1, 8 / E_); \
     else if ((d) <= 512) F(T, 64, 1, 8 / E_); \

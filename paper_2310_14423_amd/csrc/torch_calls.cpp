@@ -87,6 +87,7 @@ const float *numbers(const at::Tensor &t, const at::Tensor &x, int64_t each, con
 
 // A new tensor on x's device, which is the current one (operators.py), from the allocator that x's memory is from: 0.3 us, where at::empty's
 // way through the dispatcher makes it 0.7, with up to ten of them in a call and its backward pass.  Memory from elsewhere has none.
+// Dispatch modes do not see it, and torch's deterministic algorithms do not fill it: the library writes all of a result.
 at::Tensor fresh(const at::Tensor &x, c10::IntArrayRef size, at::ScalarType type)
 {
     c10::Allocator *const allocator = x.storage().unsafeGetStorageImpl()->allocator();
