@@ -779,19 +779,19 @@ static int run_elements(int type, int64_t d)
 
 // Whether n rows of `len` bytes, `stride` apart from `at` on, share memory with K tables of V rows of `row` bytes, `step` apart, `worker` from
 // table to table.  Rows between the table's, as far apart as those, share none; others that begin and end within a table are taken to.
-static bool shares(const void *at, int64_t n, int64_t stride, int64_t len, const void *table, int K, int64_t worker, int64_t V, int64_t step, int64_t row)
+typedef __int128 Bytes;                        // (strides are whatever the caller gave)
+static bool shares(const void *at, Bytes n, Bytes stride, Bytes len, const void *table, int K, Bytes worker, Bytes V, Bytes step, Bytes row)
 {
-    typedef __int128 Wide;                     // (strides are whatever the caller gave)
-    const Wide p = (Wide)(uintptr_t)at, t = (Wide)(uintptr_t)table, extent = (Wide)(V - 1) * step + row;
+    const Bytes p = (Bytes)(uintptr_t)at, t = (Bytes)(uintptr_t)table, extent = (V - 1) * step + row;
     if (n == 1) stride = step;
-    auto apart = [&](Wide from, Wide to) { return p >= to || p + (Wide)(n - 1) * stride + len <= from; };
-    if (apart(t, t + (Wide)(K - 1) * worker + extent)) return false;
+    auto apart = [&](Bytes from, Bytes to) { return p >= to || p + (n - 1) * stride + len <= from; };
+    if (apart(t, t + (K - 1) * worker + extent)) return false;
     for (int k = 0; k < K; ++k) {
-        const Wide from = t + (Wide)k * worker, to = from + extent;
+        const Bytes from = t + k * worker, to = from + extent;
         if (apart(from, to)) continue;
-        const Wide i = p + len > from ? 0 : (from - p - len) / stride + 1;                 // the first row that ends behind `from`
+        const Bytes i = p + len > from ? 0 : (from - p - len) / stride + 1;                // the first row that ends behind `from`
         if (i >= n || p + i * stride >= to) continue;
-        const Wide within = ((p - from) % step + step) % step;
+        const Bytes within = ((p - from) % step + step) % step;
         if (stride != step || within < row || within + len > step) return true;
     }
     return false;
@@ -836,10 +836,9 @@ extern "C" int qsr_embedding_backward(const qsr_embedding_backward_args *q, void
     if (need > 0 && (!workspace || off(workspace, 16))) return QSR_EINVAL;
     if (workspace_bytes < need) return QSR_ENOMEM;
     // rows of the table are cleared or written before all of y_grad and tokens has been read
-    const int64_t es = (int64_t)size_of(q->type), gs = (int64_t)size_of(q->grad_type), far = q->K > 1 ? q->worker_stride : 0;
-    if (q->tokens_each > 0 && (shares(q->y_grad, q->K * q->tokens_each, q->y_grad_stride * es, q->d * es, q->grad, q->K, far * gs, q->vocab, q->grad_stride * gs,
-                                      q->d * gs) ||
-                               shares(q->tokens, 1, 8, q->K * q->tokens_each * 8, q->grad, q->K, far * gs, q->vocab, q->grad_stride * gs, q->d * gs)))
+    const Bytes es = (Bytes)size_of(q->type), gs = (Bytes)size_of(q->grad_type), tokens = (Bytes)q->K * q->tokens_each, apart = q->K > 1 ? gs * q->worker_stride : 0;
+    if (tokens > 0 && (shares(q->y_grad, tokens, es * q->y_grad_stride, es * q->d, q->grad, q->K, apart, q->vocab, gs * q->grad_stride, gs * q->d) ||
+                       shares(q->tokens, 1, 8, 8 * tokens, q->grad, q->K, apart, q->vocab, gs * q->grad_stride, gs * q->d)))
         return QSR_EINVAL;
     const hipStream_t s = (hipStream_t)stream;
     const int K = q->K, E = run_elements(q->type, q->d);

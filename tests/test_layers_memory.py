@@ -19,7 +19,7 @@ P = 1 << 20         # an address that nothing reads
     dict(K=1, grad_stride=25, y_grad=P + 4 * 9, y_grad_stride=25), dict(K=1, grad_stride=25, y_grad=P + 4 * 16, y_grad_stride=25),   # rows beside rows
     dict(K=1, grad_stride=25, y_grad=P + 4 * 10, y_grad_stride=24),                                     # beside the first one, within the second
     dict(tokens_each=3000, y_grad=P + 4 * 10),                                                          # by a sort, too
-    dict(y_grad=P + 4 * 69, y_grad_stride=1 << 60),
+    dict(y_grad=P + 4 * 69, y_grad_stride=1 << 62),
 ])
 def test_gradient_of_a_table(over):
     a = dict(K=2, type=0, grad_type=0, accumulate=0, tokens_each=3, vocab=7, d=10, y_grad=P << 4, tokens=P << 5, grad=P, y_grad_stride=10,
